@@ -360,6 +360,100 @@ int saw_flatten_dequant(const saw_cache_t* cache, const int32_t* page_table,
                         int64_t token_stride_elems, saw_stream_t stream);
 
 /*
+ * Attention of packed prompts over their own keys and values (Sec. 4.1 leaves prefill attention to 16-bit K/V): the call that stands
+ * in front of saw_rotate_quant_store, or behind saw_flatten_dequant when a prefix comes out of the cache.
+ *
+ *   out_i = sum_j softmax_j(sm_scale q_i . k_j) v_j   over the keys that query i of its sequence may see
+ *
+ *   q           device, [T_q][n_q_heads][head_dim] of dtype (SAW_F16 | SAW_BF16), q_stride elements between tokens
+ *   k, v        device, [T_k][n_kv_heads][head_dim] of dtype, k_stride / v_stride elements between tokens
+ *               (strides: at least a token's elements, multiples of 8; bases 16-byte aligned)
+ *   cu_q, cu_k  device, [B + 1] int32, not decreasing: sequence b has the queries cu_q[b] .. cu_q[b + 1] - 1 and the keys
+ *               cu_k[b] .. cu_k[b + 1] - 1.  Either number may be zero.  Offsets are clamped to [0, T_q] and [0, T_k].
+ *   max_k_len   host-side upper bound on a sequence's keys, <= 0: T_k.  It only decides how the work is split.
+ *   causal      0: every query sees all keys of its sequence.  Otherwise the last query sees all of them and every query before it
+ *               one less than its successor: query i of n_q sees keys 0 .. n_k - n_q + i (the ends are aligned, so that a prefix of
+ *               keys without queries may stand in front).  Queries that see nothing get zeros.
+ *   out         device, dense [T_q][n_q_heads][head_dim] of dtype, 16-byte aligned; must not overlap the inputs.  Rows of no
+ *               sequence (from cu_q[B] on, or in front of cu_q[0]) are left as they were.
+ *   workspace   device scratch of at least saw_prompt_workspace_bytes(...) bytes, 16-byte aligned; contents are overwritten;
+ *               concurrent calls need separate workspaces.
+ * Logits, their maxima and sums and the output sums are fp32; the weights enter the product with V in dtype's precision
+ * (relative rounding 2^-9 for bf16, 2^-12 for fp16, of the order of the output's own).  A masked key counts for nothing whatever it
+ * and its value hold (NaN and infinities too).  A row whose logits are all -infinity gets zeros.
+ * T_q == 0 is a no-op.  head_dim 64 or 128; n_q_heads / n_kv_heads in {1, 2, 4, 8}; B <= 65535; T_q, T_k < 2^31.
+ */
+size_t saw_prompt_workspace_bytes(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, int64_t T_q, int32_t B, int64_t max_k_len);
+int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads,
+                    int64_t T_q, int64_t T_k, int64_t q_stride, int64_t k_stride, int64_t v_stride, const int32_t* cu_q,
+                    const int32_t* cu_k, int32_t B, int64_t max_k_len, int32_t causal, float sm_scale, void* out, void* workspace,
+                    size_t workspace_bytes, saw_stream_t stream);
+
+/*
+ * Attention of several new tokens of every sequence over the INT4 cache, which holds them already (Sec. 4.1 and App. A.4, as
+ * saw_paged_decode_attn, for more than one query a sequence): a chunk of a prompt, or draft tokens to verify.
+ *
+ *   q           device, [T][n_q_heads][head_dim] of dtype (SAW_F16 | SAW_BF16), q_stride elements between tokens (as above)
+ *   cu_q        device, [B + 1] int32 as above: sequence b has n_b = cu_q[b + 1] - cu_q[b] queries, its last n_b tokens
+ *   seq_lens    device, [B] int32: tokens in the cache, the new ones included.  Query i sees positions 0 .. seq_lens[b] - n_b + i;
+ *               one that sees nothing gets zeros.  Lengths are clamped to max_seq_len (<= 0: max_pages_per_seq * page_size).
+ *   out         device, dense [T][n_q_heads][head_dim] of dtype, 16-byte aligned; rows of no sequence are left as they were.
+ *   workspace   at least saw_paged_prompt_workspace_bytes(...) bytes, 16-byte aligned, one per call in flight.
+ * The codes enter the products exactly, the rotated query as fp16 scaled by its row's largest channel (2^-12 of that), the weights
+ * as bf16 (2^-9) for bf16 calls and as two bf16 limbs (2^-17) for fp16 ones; sums are fp32.  Page ids of visible tokens outside
+ * [0, num_pages) are read as page 0.  Alignment of the pools as for the decode calls.  T == 0 is a no-op.
+ */
+size_t saw_paged_prompt_workspace_bytes(const saw_cache_t* cache, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len);
+int saw_paged_prompt_attn(const saw_cache_t* cache, const void* q, int32_t dtype, int64_t T, int64_t q_stride, int32_t n_q_heads,
+                          const int32_t* cu_q, int32_t B, const int32_t* page_table, int32_t max_pages_per_seq,
+                          const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, void* out, void* workspace,
+                          size_t workspace_bytes, saw_stream_t stream);
+
+/*
+ * The attention weight that every cached token gets from the queries of such a call, for deciding what to evict:
+ *
+ *   scores[b][g][j] = prev[b][g][j] + sum over the queries i of sequence b that see position j, and over the query heads of kv
+ *                     head g, of softmax_j(sm_scale q~_i . k^_j)
+ *
+ *   q, dtype, cu_q, page_table, seq_lens, max_seq_len, sm_scale   as in saw_paged_prompt_attn (one query a sequence: a decode step)
+ *   prev        device, [B][n_kv_heads][score_stride] float32, or NULL for zeros.  May be `scores` itself (to accumulate in place).
+ *   scores      device, [B][n_kv_heads][score_stride] float32; positions from seq_lens[b] (clamped) on are left as they were.
+ *   score_stride  floats between rows, at least max_seq_len (its value where <= 0 stands for it).
+ *   workspace   at least saw_attn_weights_workspace_bytes(...) bytes, 16-byte aligned.
+ * All in fp32 (queries as two fp16 limbs, 2^-22 of a row's largest channel); the sums have a fixed order.  A query that sees
+ * nothing adds nothing.  T == 0 leaves prev + 0.
+ */
+size_t saw_attn_weights_workspace_bytes(const saw_cache_t* cache, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len);
+int saw_paged_attn_weights(const saw_cache_t* cache, const void* q, int32_t dtype, int64_t T, int64_t q_stride, int32_t n_q_heads,
+                           const int32_t* cu_q, int32_t B, const int32_t* page_table, int32_t max_pages_per_seq,
+                           const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, const float* prev, float* scores,
+                           int64_t score_stride, void* workspace, size_t workspace_bytes, saw_stream_t stream);
+
+/*
+ * Eviction: of every (sequence, kv head) the last `recent` tokens and the heaviest of the others are kept, `budget` in all, and their
+ * codes and (scale, zero) pairs are copied, in their old order, to the positions 0, 1, ... of the pages in dst_table.  A sequence
+ * of at most `budget` tokens is copied whole.  The heads of a sequence keep different tokens but the same number of them, so that the
+ * sequence stays one page-table row; the bytes are moved as they are (attention does not depend on positions).
+ *
+ *   scores      device, [B][n_kv_heads][score_stride] float32.  Of equal scores the lowest position is kept; -0 equals 0; NaN ranks
+ *               below everything.
+ *   page_table, seq_lens, max_seq_len   the cache as it is (score_stride >= max_seq_len, or what <= 0 stands for)
+ *   dst_table   device, [B][dst_pages_per_seq] int32, dst_pages_per_seq * page_size >= budget.  The pages must be of the same pools,
+ *               each listed once, and none of them may be a page that a kept token is read from: sources are only read, so pages
+ *               that other sequences share stay valid.  A token whose source or destination page id is outside [0, num_pages) is not
+ *               copied; slots from min(seq_lens[b], budget) on are left as they were.
+ *   budget, recent   1 <= budget, 0 <= recent <= budget
+ *   new_lens    device, [B] int32: min(seq_lens[b], budget)
+ *   kept        device, [B][n_kv_heads][budget] int32: the old positions of the kept tokens, ascending; -1 from new_lens[b] on
+ *   scores_out  device, [B][n_kv_heads][score_out_stride >= budget] float32 or NULL: the kept tokens' scores, 0 from new_lens[b] to
+ *               budget; must not overlap `scores`.
+ */
+int saw_evict_pages(const saw_cache_t* cache, const float* scores, int64_t score_stride, const int32_t* page_table,
+                    int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t B, int32_t max_seq_len, int32_t budget, int32_t recent,
+                    const int32_t* dst_table, int32_t dst_pages_per_seq, int32_t* new_lens, int32_t* kept, float* scores_out,
+                    int64_t score_out_stride, saw_stream_t stream);
+
+/*
  * 16-bit-KV comparison path (the unquantised cache the paper measures INT4 against):
  * pages are [num_pages][n_kv_heads][page_size][head_dim] of `dtype` (SAW_F16 | SAW_BF16),
  * no rotation, no metadata.  Same argument meaning as the INT4 calls; `cache` supplies

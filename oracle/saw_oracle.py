@@ -352,3 +352,85 @@ def attention_plain(q: np.ndarray, K: np.ndarray, V: np.ndarray, sm_scale: float
         g = j // G
         out[j] = _softmax_rows(((K[:, g, :] @ q[j]) * scale)[None, :])[0] @ V[:, g, :]
     return out
+
+
+# --------------------------------------------------------------------------
+# Several queries a sequence; accumulated weights; eviction
+# --------------------------------------------------------------------------
+def _weights_of(x: np.ndarray) -> np.ndarray:
+    """Softmax over the last axis of logits whose hidden entries are -inf; a row without any finite or +inf entry has no weights."""
+    m = x.max(axis=-1, keepdims=True, initial=-np.inf)
+    with np.errstate(invalid="ignore"):
+        e = np.exp(x - np.where(m == -np.inf, 0.0, m))
+    total = e.sum(axis=-1, keepdims=True)
+    return e / np.where(total == 0, 1.0, total)
+
+
+def _visible(n_q: int, n_k: int, causal: bool) -> np.ndarray:
+    """``[n_q][n_k]``: the last query sees every key, each one before it one key less."""
+    if not causal:
+        return np.ones((n_q, n_k), bool)
+    return np.arange(n_k)[None, :] <= np.arange(n_q)[:, None] + n_k - n_q
+
+
+def prompt_attn(q, k, v, cu_q, cu_k, causal=True, sm_scale=None) -> np.ndarray:
+    """Packed attention in fp64: ``q [Tq][Hq][d]``, ``k, v [Tk][Hkv][d]``, offsets ``[B + 1]``.  Hidden keys and their values are left
+    out of the sums, so that whatever they hold has no effect.  Rows of no sequence stay zero."""
+    q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
+    Hq, d = q.shape[1:]
+    G = Hq // k.shape[1]
+    scale = 1.0 / np.sqrt(np.float64(d)) if sm_scale is None or sm_scale <= 0 else float(sm_scale)
+    out = np.zeros(q.shape)
+    for b in range(len(cu_q) - 1):
+        qb, kb, vb = q[cu_q[b]:cu_q[b + 1]], k[cu_k[b]:cu_k[b + 1]], v[cu_k[b]:cu_k[b + 1]]
+        see = _visible(len(qb), len(kb), causal)
+        for j in range(Hq):
+            for i in range(len(qb)):
+                at = see[i]
+                if at.any():
+                    w = _weights_of((kb[at, j // G] @ qb[i, j]) * scale)
+                    out[cu_q[b] + i, j] = w @ vb[at, j // G]
+    return out
+
+
+def paged_weights(cache, q, cu_q, page_table, seq_lens, had_block, rotate_mask=ROT_K | ROT_V, sm_scale=None, signs=None, dense=None):
+    """``(b, kv head, query head, weights [n_b][L_b])`` of packed queries that are the last ``n_b`` tokens of their sequence."""
+    q = np.asarray(q, np.float64)
+    G = q.shape[1] // cache["n_kv_heads"]
+    scale = 1.0 / np.sqrt(np.float64(q.shape[2])) if sm_scale is None or sm_scale <= 0 else float(sm_scale)
+    for b in range(len(seq_lens)):
+        qb, L = q[cu_q[b]:cu_q[b + 1]], int(seq_lens[b])
+        if rotate_mask & ROT_K:
+            qb = rotate(qb, had_block, signs, dense)
+        khat = _gather(cache, "k", page_table[b], 0, L)
+        see = _visible(len(qb), L, True)
+        for j in range(q.shape[1]):
+            yield b, j // G, j, _weights_of(np.where(see, (qb[:, j] @ khat[:, j // G].T) * scale, -np.inf))
+
+
+def paged_prompt_attn(cache, q, cu_q, page_table, seq_lens, had_block, rotate_mask=ROT_K | ROT_V, sm_scale=None, signs=None, dense=None):
+    """Packed queries over the INT4 cache as stored (``paged_decode_attn`` for several queries a sequence)."""
+    out = np.zeros(np.shape(q), np.float64)
+    for b, g, j, w in paged_weights(cache, q, cu_q, page_table, seq_lens, had_block, rotate_mask, sm_scale, signs, dense):
+        o = w @ _gather(cache, "v", page_table[b], 0, int(seq_lens[b]))[:, g]
+        out[cu_q[b]:cu_q[b + 1], j] = unrotate(o, had_block, signs, dense) if rotate_mask & ROT_V else o
+    return out
+
+
+def paged_attn_weights(cache, q, cu_q, page_table, seq_lens, scores, had_block, rotate_mask=ROT_K | ROT_V, sm_scale=None, signs=None,
+                       dense=None):
+    """``scores [B][Hkv][n]`` plus the weights of the queries, summed over queries and the heads of a group."""
+    out = np.array(scores, np.float64)
+    for b, g, _, w in paged_weights(cache, q, cu_q, page_table, seq_lens, had_block, rotate_mask, sm_scale, signs, dense):
+        out[b, g, :int(seq_lens[b])] += w.sum(0)
+    return out
+
+
+def evict_kept(scores, length: int, budget: int, recent: int) -> np.ndarray:
+    """Positions kept of one (sequence, kv head): the last ``recent`` and the heaviest others, ``budget`` in all, ascending; ties go to
+    the lowest position, NaN ranks below everything."""
+    if length <= budget:
+        return np.arange(length)
+    old = length - recent
+    rank = sorted(range(old), key=lambda j: (1, 0.0, j) if np.isnan(scores[j]) else (0, -float(scores[j]), j))
+    return np.sort(np.concatenate([np.asarray(rank[:budget - recent], np.int64), np.arange(old, length)]))

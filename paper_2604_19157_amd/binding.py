@@ -86,6 +86,14 @@ def lib() -> ctypes.CDLL:
         L.saw_kv16_store.argtypes = [cp, vp, vp, i32, vp, vp, i64, i64, vp, i32, i32, vp, vp]
         L.saw_kv16_paged_decode_attn.argtypes = [cp, vp, vp, i32, vp, i32, i32, i32, vp, i32, vp, i32, f32,
                                                  vp, i32, vp, sz, i32, vp]
+        for n in ("saw_prompt_workspace_bytes", "saw_paged_prompt_workspace_bytes", "saw_attn_weights_workspace_bytes"):
+            getattr(L, n).restype = sz
+        L.saw_prompt_workspace_bytes.argtypes = [i32, i32, i32, i64, i32, i64]
+        L.saw_paged_prompt_workspace_bytes.argtypes = L.saw_attn_weights_workspace_bytes.argtypes = [cp, i32, i64, i32, i64]
+        L.saw_prompt_attn.argtypes = [vp, vp, vp, i32, i32, i32, i32, i64, i64, i64, i64, i64, vp, vp, i32, i64, i32, f32, vp, vp, sz, vp]
+        L.saw_paged_prompt_attn.argtypes = [cp, vp, i32, i64, i64, i32, vp, i32, vp, i32, vp, i32, f32, vp, vp, sz, vp]
+        L.saw_paged_attn_weights.argtypes = [cp, vp, i32, i64, i64, i32, vp, i32, vp, i32, vp, i32, f32, vp, vp, i64, vp, sz, vp]
+        L.saw_evict_pages.argtypes = [cp, vp, i64, vp, i32, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, i64, vp]
         _lib = L
     return _lib
 
@@ -314,6 +322,77 @@ def flatten_dequant(cache: Cache, page_table, seq, pos_begin, pos_end, unrotate=
         return k_out, v_out
     _check((_native or _marshal()).flatten(cache, page_table, seq, pos_begin, pos_end, unrotate, k_out, v_out), "saw_flatten_dequant")
     return k_out, v_out
+
+
+def prompt_workspace_bytes(q, k, n_seqs, max_k_len=0) -> int:
+    """Scratch of prompt_attn for q ``[T_q][Hq][d]`` and k ``[T_k][Hkv][d]`` in ``n_seqs`` sequences."""
+    return int(lib().saw_prompt_workspace_bytes(q.shape[2], q.shape[1], k.shape[1], q.shape[0], n_seqs, max_k_len or k.shape[0]))
+
+
+def prompt_attn(q, k, v, cu_q, cu_k=None, max_k_len=0, causal=True, sm_scale=0.0, out=None, workspace=None):
+    """saw_prompt_attn: packed q ``[T_q][Hq][d]``, k and v ``[T_k][Hkv][d]`` (one 16-bit type, heads dense, tokens at any stride that is a
+    multiple of 8), cu_q and cu_k ``[B + 1]`` int32 offsets (cu_k None: as many keys as queries); returns ``out [T_q][Hq][d]``."""
+    if cu_k is None:
+        cu_k = cu_q
+    if out is None:
+        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(max(prompt_workspace_bytes(q, k, cu_q.numel() - 1, max_k_len), 16), dtype=torch.uint8, device=q.device)
+    _check((_native or _marshal()).prompt(q, k, v, cu_q, cu_k, max_k_len, causal, sm_scale, out, workspace), "saw_prompt_attn")
+    return out
+
+
+def paged_prompt_workspace_bytes(cache: Cache, q, n_seqs, max_seq_len) -> int:
+    st = cache.struct()
+    return int(lib().saw_paged_prompt_workspace_bytes(ctypes.byref(st), q.shape[1], q.shape[0], n_seqs, max_seq_len))
+
+
+def paged_prompt_attn(cache: Cache, q, cu_q, page_table, seq_lens, max_seq_len=0, sm_scale=0.0, out=None, workspace=None):
+    """saw_paged_prompt_attn: packed q ``[T][Hq][d]`` (fp16/bf16), cu_q ``[B + 1]`` int32 offsets, seq_lens ``[B]`` the cached tokens with the
+    new ones; returns ``out [T][Hq][d]`` of q's type."""
+    if out is None:
+        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    if workspace is None:
+        bound = max_seq_len if max_seq_len > 0 else page_table.shape[1] * cache.page_size
+        workspace = torch.empty(max(paged_prompt_workspace_bytes(cache, q, cu_q.numel() - 1, bound), 16), dtype=torch.uint8, device=q.device)
+    _check((_native or _marshal()).paged_prompt(cache, q, cu_q, page_table, seq_lens, max_seq_len, sm_scale, out, workspace),
+           "saw_paged_prompt_attn")
+    return out
+
+
+def attn_weights_workspace_bytes(cache: Cache, q, n_seqs, max_seq_len) -> int:
+    st = cache.struct()
+    return int(lib().saw_attn_weights_workspace_bytes(ctypes.byref(st), q.shape[1], q.shape[0], n_seqs, max_seq_len))
+
+
+def paged_attn_weights(cache: Cache, q, cu_q, page_table, seq_lens, prev=None, scores=None, max_seq_len=0, sm_scale=0.0, workspace=None):
+    """saw_paged_attn_weights: the weights that the cached tokens get from q ``[T][Hq][d]``, added to ``prev [B][Hkv][n]`` fp32 (None:
+    zeros; it may be ``scores``); returns ``scores``, laid out as prev, zeros behind a sequence's end if it is made here."""
+    bound = max_seq_len if max_seq_len > 0 else page_table.shape[1] * cache.page_size
+    if scores is None:
+        shape = prev.shape if prev is not None else (cu_q.numel() - 1, cache.n_kv_heads, bound)
+        scores = torch.zeros(shape, dtype=torch.float32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(max(attn_weights_workspace_bytes(cache, q, cu_q.numel() - 1, bound), 16), dtype=torch.uint8, device=q.device)
+    _check((_native or _marshal()).attn_weights(cache, q, cu_q, page_table, seq_lens, prev, scores, max_seq_len, sm_scale, workspace),
+           "saw_paged_attn_weights")
+    return scores
+
+
+def evict_pages(cache: Cache, scores, page_table, seq_lens, dst_table, budget, recent=0, max_seq_len=0, new_lens=None, kept=None,
+                scores_out=None):
+    """saw_evict_pages: keeps ``budget`` tokens of every (sequence, kv head) by ``scores [B][Hkv][n]`` fp32, the last ``recent`` among them,
+    and copies them to the pages of ``dst_table``; returns ``(new_lens [B], kept [B][Hkv][budget], scores_out [B][Hkv][>= budget])``."""
+    B, dev = seq_lens.numel(), scores.device
+    if new_lens is None:
+        new_lens = torch.empty(B, dtype=torch.int32, device=dev)
+    if kept is None:
+        kept = torch.empty((B, cache.n_kv_heads, budget), dtype=torch.int32, device=dev)
+    if scores_out is None:
+        scores_out = torch.empty((B, cache.n_kv_heads, budget), dtype=torch.float32, device=dev)
+    _check((_native or _marshal()).evict(cache, scores, page_table, seq_lens, dst_table, budget, recent, max_seq_len, new_lens, kept, scores_out),
+           "saw_evict_pages")
+    return new_lens, kept, scores_out
 
 
 class Kv16Cache:

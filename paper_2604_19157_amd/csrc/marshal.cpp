@@ -289,8 +289,135 @@ PyObject* kv16_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Every tensor of the calls below is on the GPU whose stream takes the call: an address of another device or of the host would fault there.
+template <typename... T>
+void on_this_gpu(const T&... t) {
+  check((t.is_cuda() && ...), "every tensor is on the GPU");
+  const auto device = c10::hip::getCurrentHIPStream().device_index();
+  check(((t.get_device() == device) && ...), "every tensor is on the current device");
+}
+int32_t in_int32(PyObject* o) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw Raised();
+  check(v >= INT32_MIN && v <= INT32_MAX, "a count is beyond 32 bits");
+  return (int32_t)v;
+}
+bool heads_dense(const at::Tensor& t) { return t.dim() == 3 && (t.size(2) <= 1 || t.stride(2) == 1) && (t.size(1) <= 1 || t.stride(1) == t.size(2)); }
+int64_t token_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2); }
+const int32_t* offsets(const at::Tensor& t, int64_t n, const char* what) {
+  check(is_i32(t) && t.dim() == 1 && t.is_contiguous() && t.numel() == n, what);
+  return (const int32_t*)t.data_ptr();
+}
+const int32_t* table_of(const at::Tensor& t, int64_t rows) {
+  check(is_i32(t) && t.dim() == 2 && t.is_contiguous() && t.size(0) == rows, "a page table is a contiguous int32 tensor with a row per sequence");
+  return (const int32_t*)t.data_ptr();
+}
+// a record of scores [B][n_kv_heads][n], rows dense and evenly spaced; the distance between rows
+float* record_of(const at::Tensor& t, int64_t B, int64_t heads, int64_t& stride, const char* what) {
+  check(t.scalar_type() == at::kFloat && t.dim() == 3 && t.size(0) == B && t.size(1) == heads && t.is_contiguous(), what);
+  stride = t.size(2);
+  return (float*)t.data_ptr();
+}
+
+// (q, k, v, cu_q, cu_k, max_k_len, causal, sm_scale, out, workspace)
+PyObject* prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 10, [&](Held&) {
+    const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]), &cq = tensor(a[3]), &ck = tensor(a[4]), &out = tensor(a[8]), &ws = tensor(a[9]);
+    check(heads_dense(q) && heads_dense(k) && heads_dense(v) && q.scalar_type() == k.scalar_type() && k.scalar_type() == v.scalar_type() &&
+              k.sizes() == v.sizes() && q.size(2) == k.size(2),
+          "q is [T_q][n_q_heads][head_dim], k and v are [T_k][n_kv_heads][head_dim], of one type, heads dense");
+    check(out.is_contiguous() && out.scalar_type() == q.scalar_type() && out.sizes() == q.sizes(), "out is dense, of q's type and shape");
+    check(cq.numel() >= 2, "cu_q has an entry per sequence and one more");
+    const int32_t *const oq = offsets(cq, cq.numel(), "cu_q is a contiguous int32 vector"), *const ok = offsets(ck, cq.numel(), "cu_k is a contiguous int32 vector of cu_q's length");
+    const int type = code_of(q.scalar_type());
+    const int64_t bound = PyLong_AsLongLong(a[5]);
+    if (bound == -1 && PyErr_Occurred()) throw Raised();
+    const int causal = PyObject_IsTrue(a[6]);
+    if (causal < 0) throw Raised();
+    const float scale = as_float(a[7]);
+    check(ws.is_contiguous(), "the workspace is contiguous");
+    on_this_gpu(q, k, v, cq, ck, out, ws);
+    return run(saw_prompt_attn, q.data_ptr(), k.data_ptr(), v.data_ptr(), type, (int32_t)q.size(2), (int32_t)q.size(1), (int32_t)k.size(1),
+               q.size(0), k.size(0), token_stride(q), token_stride(k), token_stride(v), oq, ok, (int32_t)(cq.numel() - 1), bound, causal, scale,
+               out.data_ptr(), ws.data_ptr(), (size_t)ws.nbytes(), stream());
+  });
+}
+
+// (cache, q, cu_q, page_table, seq_lens, max_seq_len, sm_scale, out, workspace)
+PyObject* paged_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 9, [&](Held& held) {
+    saw_cache_t c;
+    cache_of(a[0], c, held);
+    const at::Tensor &q = tensor(a[1]), &cq = tensor(a[2]), &pt = tensor(a[3]), &lens = tensor(a[4]), &out = tensor(a[7]), &ws = tensor(a[8]);
+    check(heads_dense(q) && q.size(2) == c.head_dim, "q is [T][n_q_heads][head_dim], heads dense");
+    check(out.is_contiguous() && out.scalar_type() == q.scalar_type() && out.sizes() == q.sizes(), "out is dense, of q's type and shape");
+    const int64_t B = lens.numel();
+    const int32_t *const oq = offsets(cq, B + 1, "cu_q is a contiguous int32 vector, an entry longer than seq_lens"),
+                  *const sl = offsets(lens, B, "seq_lens is a contiguous int32 vector"), *const table = table_of(pt, B);
+    const int type = code_of(q.scalar_type());
+    const int32_t bound = in_int32(a[5]);
+    const float scale = as_float(a[6]);
+    check(ws.is_contiguous(), "the workspace is contiguous");
+    on_this_gpu(q, cq, pt, lens, out, ws);
+    return run(saw_paged_prompt_attn, &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
+               (int32_t)pt.size(1), sl, bound, scale, out.data_ptr(), ws.data_ptr(), (size_t)ws.nbytes(), stream());
+  });
+}
+
+// (cache, q, cu_q, page_table, seq_lens, prev or None, scores, max_seq_len, sm_scale, workspace)
+PyObject* attn_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 10, [&](Held& held) {
+    saw_cache_t c;
+    cache_of(a[0], c, held);
+    const at::Tensor &q = tensor(a[1]), &cq = tensor(a[2]), &pt = tensor(a[3]), &lens = tensor(a[4]), &scores = tensor(a[6]), &ws = tensor(a[9]);
+    check(heads_dense(q) && q.size(2) == c.head_dim, "q is [T][n_q_heads][head_dim], heads dense");
+    const int64_t B = lens.numel();
+    int64_t stride, before;
+    float* const to = record_of(scores, B, c.n_kv_heads, stride, "scores is a contiguous float32 tensor [B][n_kv_heads][n]");
+    const float* prev = nullptr;
+    if (a[5] != Py_None) {
+      prev = record_of(tensor(a[5]), B, c.n_kv_heads, before, "prev is a contiguous float32 tensor [B][n_kv_heads][n]");
+      check(before == stride, "prev is laid out as scores");
+    }
+    const int32_t *const oq = offsets(cq, B + 1, "cu_q is a contiguous int32 vector, an entry longer than seq_lens"),
+                  *const sl = offsets(lens, B, "seq_lens is a contiguous int32 vector"), *const table = table_of(pt, B);
+    const int type = code_of(q.scalar_type());
+    const int32_t bound = in_int32(a[7]);
+    const float scale = as_float(a[8]);
+    check(ws.is_contiguous(), "the workspace is contiguous");
+    on_this_gpu(q, cq, pt, lens, scores, ws);
+    if (prev) on_this_gpu(tensor(a[5]));
+    return run(saw_paged_attn_weights, &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
+               (int32_t)pt.size(1), sl, bound, scale, prev, to, stride, ws.data_ptr(), (size_t)ws.nbytes(), stream());
+  });
+}
+
+// (cache, scores, page_table, seq_lens, dst_table, budget, recent, max_seq_len, new_lens, kept, scores_out or None)
+PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 11, [&](Held& held) {
+    saw_cache_t c;
+    cache_of(a[0], c, held);
+    const at::Tensor &scores = tensor(a[1]), &pt = tensor(a[2]), &lens = tensor(a[3]), &dst = tensor(a[4]), &now = tensor(a[8]), &kept = tensor(a[9]);
+    const int64_t B = lens.numel();
+    const int32_t budget = in_int32(a[5]), recent = in_int32(a[6]), bound = in_int32(a[7]);
+    int64_t stride, out_stride = 0;
+    const float* const from = record_of(scores, B, c.n_kv_heads, stride, "scores is a contiguous float32 tensor [B][n_kv_heads][n]");
+    float* out = nullptr;
+    if (a[10] != Py_None) out = record_of(tensor(a[10]), B, c.n_kv_heads, out_stride, "scores_out is a contiguous float32 tensor [B][n_kv_heads][n]");
+    check(is_i32(kept) && kept.is_contiguous() && kept.dim() == 3 && kept.size(0) == B && kept.size(1) == c.n_kv_heads && kept.size(2) == budget,
+          "kept is a contiguous int32 tensor [B][n_kv_heads][budget]");
+    const int32_t *const sl = offsets(lens, B, "seq_lens is a contiguous int32 vector"), *const table = table_of(pt, B), *const to = table_of(dst, B);
+    int32_t* const nl = (int32_t*)offsets(now, B, "new_lens is a contiguous int32 vector of seq_lens' length");
+    on_this_gpu(scores, pt, lens, dst, now, kept);
+    if (out) on_this_gpu(tensor(a[10]));
+    return run(saw_evict_pages, &c, from, stride, table, (int32_t)pt.size(1), sl, (int32_t)B, bound, budget, recent, to, (int32_t)dst.size(1), nl,
+               (int32_t*)kept.data_ptr(), out, out_stride, stream());
+  });
+}
+
 #define FAST(f) {#f, (PyCFunction)(void*)f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(store), FAST(store_layers), FAST(decode), FAST(append), FAST(flatten), FAST(kv16_decode),
+                         FAST(prompt), FAST(paged_prompt), FAST(attn_weights), FAST(evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -4,6 +4,7 @@
 
 #include <mutex>
 
+#include "saw_check.h"
 #include "saw_decode.h"
 
 // Split-KV scratch of saw_paged_decode_attn_static, the entry point for callers that cannot
@@ -33,15 +34,6 @@ int run_decode(const saw_cache_t* c, bool kv16, const void* k_pages, const void*
                const SplitPlan& plan, const void* k_new, const void* v_new, int kv_new_dtype,
                const int32_t* order, hipStream_t st);
 
-static bool aligned16(const void* p) { return (((uintptr_t)p) & 15u) == 0; }
-
-static bool shape_ok(const saw_cache_t* c) {
-  if (c->page_size != 16) return false;
-  if (c->head_dim != 64 && c->head_dim != 128) return false;
-  if (c->n_kv_heads < 1 || c->num_pages < 1) return false;
-  return true;
-}
-
 // (The times beside the INT4 lines from here on are those the lines were drawn by, with products of bf16 limbs, when a batch took 2.6 times
 // the vector instructions.  Calls take 0.86 of them now in the mean; the lines were not drawn again.)
 //
@@ -60,18 +52,6 @@ static bool cut_plan(int B, int units, int slots, int waves, SplitPlan* plan) {
   plan->cut = w;
   plan->cut_min = kMin;
   plan->cut_waves = waves;
-  return true;
-}
-
-static bool block_ok(const saw_cache_t* c) {
-  const int h = c->had_block;
-  if (!(h == 1 || h == 16 || h == 32 || h == 64 || h == 128)) return false;
-  if (h > c->head_dim) return false;
-  if (c->rotate_mask & ~(SAW_ROT_K | SAW_ROT_V)) return false;
-  // sign bits exist for the head's channels only
-  if (c->head_dim == 64 && (c->sign_bits[2] | c->sign_bits[3])) return false;
-  // the learned rotation is built for head_dim 128, its prepared buffer read with 16-byte loads
-  if (c->dense_rot && (c->head_dim != kDenseD || !aligned16(c->dense_rot))) return false;
   return true;
 }
 

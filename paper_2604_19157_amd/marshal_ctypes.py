@@ -85,3 +85,87 @@ def kv16_decode(cache, q, page_table, seq_lens, max_seq_len, sm_scale, out, work
                                               b._ptr(q), b._DT[q.dtype], B, Hq, b._ptr(page_table), page_table.shape[1],
                                               b._ptr(seq_lens), max_seq_len, float(sm_scale), b._ptr(out), b._DT[out.dtype],
                                               b._ptr(workspace), workspace.numel(), num_splits, b._stream())
+
+
+def _on_this_gpu(*tensors):
+    assert all(t.is_cuda for t in tensors), "every tensor is on the GPU"
+    assert all(t.get_device() == torch.cuda.current_device() for t in tensors), "every tensor is on the current device"
+
+
+def _heads_dense(t):
+    return t.dim() == 3 and (t.shape[2] <= 1 or t.stride(2) == 1) and (t.shape[1] <= 1 or t.stride(1) == t.shape[2])
+
+
+def _token_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _vector(t, n):
+    return t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.numel() == n
+
+
+def _table(t, rows):
+    return t.dtype == torch.int32 and _rows(t) and t.shape[0] == rows
+
+
+def _record(t, B, heads):
+    return t.dtype == torch.float32 and t.dim() == 3 and t.is_contiguous() and t.shape[0] == B and t.shape[1] == heads
+
+
+def _counts(*values):
+    assert all(-2**31 <= v < 2**31 for v in values), "a count is beyond 32 bits"
+
+
+def _like(out, q):
+    return out.is_contiguous() and out.dtype == q.dtype and out.shape == q.shape
+
+
+def prompt(q, k, v, cu_q, cu_k, max_k_len, causal, sm_scale, out, workspace):
+    assert _heads_dense(q) and _heads_dense(k) and _heads_dense(v) and q.dtype == k.dtype == v.dtype
+    assert k.shape == v.shape and q.shape[2] == k.shape[2] and _like(out, q) and cu_q.numel() >= 2
+    assert _vector(cu_q, cu_q.numel()) and _vector(cu_k, cu_q.numel()) and workspace.is_contiguous()
+    _on_this_gpu(q, k, v, cu_q, cu_k, out, workspace)
+    return b.lib().saw_prompt_attn(b._ptr(q), b._ptr(k), b._ptr(v), b._DT[q.dtype], q.shape[2], q.shape[1], k.shape[1], q.shape[0],
+                                   k.shape[0], _token_stride(q), _token_stride(k), _token_stride(v), b._ptr(cu_q), b._ptr(cu_k),
+                                   cu_q.numel() - 1, max_k_len, int(bool(causal)), float(sm_scale), b._ptr(out), b._ptr(workspace),
+                                   workspace.nbytes, b._stream())
+
+
+def paged_prompt(cache, q, cu_q, page_table, seq_lens, max_seq_len, sm_scale, out, workspace):
+    B = seq_lens.numel()
+    _counts(max_seq_len)
+    assert _heads_dense(q) and q.shape[2] == cache.head_dim and _like(out, q)
+    assert _vector(cu_q, B + 1) and _vector(seq_lens, B) and _table(page_table, B) and workspace.is_contiguous()
+    _on_this_gpu(q, cu_q, page_table, seq_lens, out, workspace)
+    st = cache.struct()
+    return b.lib().saw_paged_prompt_attn(ctypes.byref(st), b._ptr(q), b._DT[q.dtype], q.shape[0], _token_stride(q), q.shape[1], b._ptr(cu_q),
+                                         B, b._ptr(page_table), page_table.shape[1], b._ptr(seq_lens), max_seq_len, float(sm_scale),
+                                         b._ptr(out), b._ptr(workspace), workspace.nbytes, b._stream())
+
+
+def attn_weights(cache, q, cu_q, page_table, seq_lens, prev, scores, max_seq_len, sm_scale, workspace):
+    B = seq_lens.numel()
+    _counts(max_seq_len)
+    assert _heads_dense(q) and q.shape[2] == cache.head_dim and _record(scores, B, cache.n_kv_heads)
+    assert prev is None or (_record(prev, B, cache.n_kv_heads) and prev.shape == scores.shape)
+    assert _vector(cu_q, B + 1) and _vector(seq_lens, B) and _table(page_table, B) and workspace.is_contiguous()
+    _on_this_gpu(q, cu_q, page_table, seq_lens, scores, workspace, *([] if prev is None else [prev]))
+    st = cache.struct()
+    return b.lib().saw_paged_attn_weights(ctypes.byref(st), b._ptr(q), b._DT[q.dtype], q.shape[0], _token_stride(q), q.shape[1],
+                                          b._ptr(cu_q), B, b._ptr(page_table), page_table.shape[1], b._ptr(seq_lens), max_seq_len,
+                                          float(sm_scale), b._ptr(prev), b._ptr(scores), scores.shape[2], b._ptr(workspace),
+                                          workspace.nbytes, b._stream())
+
+
+def evict(cache, scores, page_table, seq_lens, dst_table, budget, recent, max_seq_len, new_lens, kept, scores_out):
+    B = seq_lens.numel()
+    _counts(budget, recent, max_seq_len)
+    assert _record(scores, B, cache.n_kv_heads) and (scores_out is None or _record(scores_out, B, cache.n_kv_heads))
+    assert kept.dtype == torch.int32 and kept.is_contiguous() and kept.shape == (B, cache.n_kv_heads, budget)
+    assert _vector(seq_lens, B) and _vector(new_lens, B) and _table(page_table, B) and _table(dst_table, B)
+    _on_this_gpu(scores, page_table, seq_lens, dst_table, new_lens, kept, *([] if scores_out is None else [scores_out]))
+    st = cache.struct()
+    return b.lib().saw_evict_pages(ctypes.byref(st), b._ptr(scores), scores.shape[2], b._ptr(page_table), page_table.shape[1],
+                                   b._ptr(seq_lens), B, max_seq_len, budget, recent, b._ptr(dst_table), dst_table.shape[1],
+                                   b._ptr(new_lens), b._ptr(kept), b._ptr(scores_out), 0 if scores_out is None else scores_out.shape[2],
+                                   b._stream())
