@@ -289,6 +289,17 @@ PyObject* kv16_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (weak: beside a library that lacks these entry points the module still loads and serves the calls above)
+#pragma weak saw_prompt_attn
+#pragma weak saw_paged_prompt_attn
+#pragma weak saw_paged_attn_weights
+#pragma weak saw_evict_pages
+template <typename F>
+F present(F f) {
+  check(f != nullptr, "the library beside this module lacks the call");
+  return f;
+}
+
 // Every tensor of the calls below is on the GPU whose stream takes the call: an address of another device or of the host would fault there.
 template <typename... T>
 void on_this_gpu(const T&... t) {
@@ -337,7 +348,7 @@ PyObject* prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float scale = as_float(a[7]);
     check(ws.is_contiguous(), "the workspace is contiguous");
     on_this_gpu(q, k, v, cq, ck, out, ws);
-    return run(saw_prompt_attn, q.data_ptr(), k.data_ptr(), v.data_ptr(), type, (int32_t)q.size(2), (int32_t)q.size(1), (int32_t)k.size(1),
+    return run(present(&saw_prompt_attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), type, (int32_t)q.size(2), (int32_t)q.size(1), (int32_t)k.size(1),
                q.size(0), k.size(0), token_stride(q), token_stride(k), token_stride(v), oq, ok, (int32_t)(cq.numel() - 1), bound, causal, scale,
                out.data_ptr(), ws.data_ptr(), (size_t)ws.nbytes(), stream());
   });
@@ -359,7 +370,7 @@ PyObject* paged_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float scale = as_float(a[6]);
     check(ws.is_contiguous(), "the workspace is contiguous");
     on_this_gpu(q, cq, pt, lens, out, ws);
-    return run(saw_paged_prompt_attn, &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
+    return run(present(&saw_paged_prompt_attn), &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
                (int32_t)pt.size(1), sl, bound, scale, out.data_ptr(), ws.data_ptr(), (size_t)ws.nbytes(), stream());
   });
 }
@@ -387,7 +398,7 @@ PyObject* attn_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
     check(ws.is_contiguous(), "the workspace is contiguous");
     on_this_gpu(q, cq, pt, lens, scores, ws);
     if (prev) on_this_gpu(tensor(a[5]));
-    return run(saw_paged_attn_weights, &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
+    return run(present(&saw_paged_attn_weights), &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
                (int32_t)pt.size(1), sl, bound, scale, prev, to, stride, ws.data_ptr(), (size_t)ws.nbytes(), stream());
   });
 }
@@ -410,7 +421,7 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t* const nl = (int32_t*)offsets(now, B, "new_lens is a contiguous int32 vector of seq_lens' length");
     on_this_gpu(scores, pt, lens, dst, now, kept);
     if (out) on_this_gpu(tensor(a[10]));
-    return run(saw_evict_pages, &c, from, stride, table, (int32_t)pt.size(1), sl, (int32_t)B, bound, budget, recent, to, (int32_t)dst.size(1), nl,
+    return run(present(&saw_evict_pages), &c, from, stride, table, (int32_t)pt.size(1), sl, (int32_t)B, bound, budget, recent, to, (int32_t)dst.size(1), nl,
                (int32_t*)kept.data_ptr(), out, out_stride, stream());
   });
 }
