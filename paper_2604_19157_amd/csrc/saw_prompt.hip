@@ -191,10 +191,10 @@ int launch_weights(const PromptParams& p, int D, hipStream_t st) {
   const int64_t rows = p.T_q * p.n_q_heads;
   const dim3 grid((unsigned)((rows + 3) / 4)), block(256), wgrid((p.bound + 3) / 4, p.n_kv_heads, p.B);
   if (D == 128) {
-    row_stats_kernel<128><<<grid, block, 0, st>>>(p);
+    if (rows) row_stats_kernel<128><<<grid, block, 0, st>>>(p);
     weights_kernel<128><<<wgrid, block, 0, st>>>(p);
   } else {
-    row_stats_kernel<64><<<grid, block, 0, st>>>(p);
+    if (rows) row_stats_kernel<64><<<grid, block, 0, st>>>(p);
     weights_kernel<64><<<wgrid, block, 0, st>>>(p);
   }
   return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;

@@ -1,0 +1,274 @@
+"""saw_paged_prompt_attn and saw_paged_attn_weights against attention in 64 bits over the dequantised cache, within bounds worked out per
+output (packed_cases)."""
+import numpy as np
+import pytest
+import torch
+
+import gpu_cases as gc
+import packed_cases as pc
+from oracle import saw_oracle as O
+from paper_2604_19157_amd import synth
+
+pytestmark = pytest.mark.gpu
+BF, FP = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def saw():
+    from paper_2604_19157_amd import binding
+    binding.lib()
+    return binding
+
+
+class Case:
+    def __init__(self, saw, n, lens, Hkv=2, G=4, d=128, h=128, mask=3, dtype=BF, signs=False, dense=False, seed=0):
+        """A cache of random codes, scales and zero-points (any number is a stored value), queries scaled so that logits spread over a few units."""
+        rng = np.random.default_rng(seed)
+        self.n, self.lens, self.h, self.mask, self.d, self.G, self.Hkv = n, np.asarray(lens, np.int32), h, mask, d, G, Hkv
+        pages = [(x + 15) // 16 for x in lens]
+        num = sum(pages) + 3
+        perm = rng.permutation(num).astype(np.int32)
+        self.pt = np.full((len(lens), max(max(pages), 1)), num + 99, np.int32)
+        at = 0
+        for b, p in enumerate(pages):
+            self.pt[b, :p] = perm[at:at + p]
+            at += p
+        self.ref = O.new_cache(num, Hkv, 16, d)
+        for w in "kv":
+            self.ref[w + "_codes"][...] = rng.integers(0, 256, self.ref[w + "_codes"].shape)
+            m = self.ref[w + "_meta"]
+            m[..., 0] = rng.uniform(0.02, 0.3, m.shape[:-1])
+            m[..., 1] = np.where(rng.random(m.shape[:-1]) < 0.1, rng.integers(-60, 80, m.shape[:-1]), rng.integers(4, 12, m.shape[:-1]))
+        self.signs = synth.random_signs(d, seed + 1) if signs else None
+        self.dense = synth.random_orthogonal(d, seed + 2) if dense else None
+        self.cu = pc.offsets(n)
+        self.q = pc.rand((self.cu[-1], Hkv * G, d), seed + 3, dtype, 0.5)
+        self.cache = saw.Cache(num, Hkv, d, h, mask, signs=self.signs, dense=self.dense)
+        for name in ("k_codes", "v_codes", "k_meta", "v_meta"):
+            t = getattr(self.cache, name)
+            t.copy_(torch.from_numpy(np.ascontiguousarray(self.ref[name])).reshape(t.shape))
+        self.args = (self.q.cuda(), torch.from_numpy(self.cu).cuda(), torch.from_numpy(self.pt).cuda(), torch.from_numpy(self.lens).cuda())
+
+    def weights(self):
+        """(b, rows, kv head, query head, weights, largest |q||k| sum and |logit| of each row)"""
+        rot = self.mask & 1
+        for b, (n, L) in enumerate(zip(self.n, self.lens.tolist())):
+            if n == 0 or L == 0:
+                continue
+            rows = slice(self.cu[b], self.cu[b + 1])
+            q = self.q[rows].double().numpy()
+            if rot:
+                q = O.rotate(q, self.h, self.signs, self.dense)
+            k = O._gather(self.ref, "k", self.pt[b], 0, L)
+            for j in range(self.q.shape[1]):
+                yield (b, rows, j // self.G, j) + pc.weights64(q[:, j], k[:, j // self.G], pc.visible(n, L), self.d ** -0.5)
+
+    def attention(self):
+        u = pc.U[self.q.dtype]
+        out, tol = np.zeros(self.q.shape), np.zeros(self.q.shape)
+        for b, rows, g, j, w, top, big in self.weights():
+            L = int(self.lens[b])
+            v = O._gather(self.ref, "v", self.pt[b], 0, L)[:, g]
+            o, A = w @ v, w @ np.abs(v)
+            # (the weights' part of the bound in the rotated space: rotating back mixes a block's channels, |x R^T| <= |x| sqrt(channels mixed))
+            if self.mask & 2:
+                mix = self.d if self.dense is not None else self.h
+                blocks = A.reshape(len(A), -1, mix) if mix > 1 else A[..., None]
+                A = np.repeat(np.sqrt((blocks ** 2).sum(-1)), mix, axis=-1).reshape(A.shape)
+                o = O.unrotate(o, self.h, self.signs, self.dense)
+            out[rows, j] = o
+            tol[rows, j] = pc.bound(o, A, top, big, L, self.d, u, u if self.q.dtype == BF else 2.0 ** -16, 2.0 ** -11 + 2.0 ** -20)
+        return out, tol
+
+
+SHAPES = [([1], [1]), ([1, 1, 1], [70, 1, 200]), ([3, 0, 5], [40, 9, 5]), ([33, 64], [100, 64]), ([130], [333]), ([2, 17], [900, 1030]), ([5, 5, 5], [513, 640, 64])]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d,G", [(128, 1), (128, 4), (128, 8), (64, 2), (64, 8)])
+@pytest.mark.parametrize("n,lens", SHAPES, ids=str)
+def test_attention(saw, n, lens, d, G, dtype):
+    c = Case(saw, n, lens, G=G, d=d, h=d, dtype=dtype, seed=len(n) + d)
+    want, tol = c.attention()
+    pc.check(saw.paged_prompt_attn(c.cache, *c.args), want, tol)
+
+
+OPTIONS = [dict(h=1), dict(h=16), dict(h=32, mask=1), dict(h=64, mask=2), dict(h=128, signs=True), dict(h=128, dense=True),
+           dict(h=1, dense=True), dict(h=64, dense=True, signs=True, mask=1), dict(d=64, h=16), dict(d=64, h=64, signs=True), dict(d=64, h=1)]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("options", OPTIONS, ids=str)
+def test_rotations(saw, options, dtype):
+    c = Case(saw, [7, 1, 40], [60, 300, 40], dtype=dtype, seed=4, **options)
+    want, tol = c.attention()
+    pc.check(saw.paged_prompt_attn(c.cache, *c.args), want, tol)
+
+
+def test_queries_in_front_of_all_tokens_and_empty_sequences(saw):
+    """More queries than tokens: the first rows see nothing and are zero; rows of no sequence stay as they were."""
+    c = Case(saw, [6, 4, 0, 2], [2, 0, 7, 2])
+    q = torch.cat([c.args[0], pc.rand((3, 8, 128), 9, BF).cuda()])
+    out = torch.full_like(q, 5.0)
+    saw.paged_prompt_attn(c.cache, q, *c.args[1:], out=out)
+    want, tol = c.attention()
+    pc.check(out[:12], want, tol)
+    assert torch.count_nonzero(out[:4]) == 0 and torch.count_nonzero(out[6:10]) == 0 and bool((out[12:] == 5).all())
+
+
+def test_agrees_with_the_decode_call(saw):
+    """One query a sequence is a decode step: both are within their bounds of the same numbers."""
+    c = Case(saw, [1] * 6, [1, 15, 16, 333, 800, 64])
+    want, tol = c.attention()
+    got = saw.paged_prompt_attn(c.cache, *c.args)
+    pc.check(got, want, tol)
+    dec = saw.paged_decode_attn(c.cache, c.args[0], c.args[2].clamp(max=c.cache.num_pages - 1), c.args[3], out_dtype=BF)
+    pc.check(dec, want, tol)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_slots_and_pages_that_are_not_seen_count_for_nothing(saw, bad):
+    """Slots behind a sequence's end hold anything; tokens that a query does not see too."""
+    c = Case(saw, [40, 3], [50, 21])
+    clean = saw.paged_prompt_attn(c.cache, *c.args)
+    for pool in (c.cache.k_meta, c.cache.v_meta):
+        pool[c.pt[0, 3], :, 2:] = bad               # positions 50 on
+        pool[c.pt[1, 1], :, 5:] = bad
+    assert torch.equal(saw.paged_prompt_attn(c.cache, *c.args), clean)
+    for pool in (c.cache.k_meta, c.cache.v_meta):
+        keep = pool.clone()
+        pool[c.pt[0, 2], :, 8] = bad                # position 40: rows 30 .. 39 see it
+        got = saw.paged_prompt_attn(c.cache, *c.args)
+        assert torch.equal(got[:30], clean[:30]) and torch.equal(got[40:], clean[40:])
+        assert not torch.isfinite(got[30:40].float()).any()
+        pool.copy_(keep)
+
+
+def test_page_ids_out_of_range_read_page_0(saw):
+    c = Case(saw, [20], [60])
+    pt = c.args[2].clone()
+    pt[0, 1] = -7
+    pt[0, 2] = 1 << 30
+    got = saw.paged_prompt_attn(c.cache, c.args[0], c.args[1], pt, c.args[3])
+    pt[0, 1:3] = 0
+    assert torch.equal(got, saw.paged_prompt_attn(c.cache, c.args[0], c.args[1], pt, c.args[3]))
+
+
+def test_bound_of_the_lengths(saw):
+    """Lengths are clamped to max_seq_len, queries stay the last tokens of what is left."""
+    c = Case(saw, [5, 2], [100, 30])
+    got = saw.paged_prompt_attn(c.cache, *c.args, max_seq_len=48)
+    c.lens = np.minimum(c.lens, 48)
+    want, tol = c.attention()
+    pc.check(got, want, tol)
+
+
+def test_queries_at_a_stride(saw):
+    c = Case(saw, [9, 31], [60, 31])
+    wide = torch.zeros((40, 8 * 128 + 64), dtype=BF, device="cuda")
+    view = wide[:, 32:32 + 8 * 128].unflatten(1, (8, 128))
+    view.copy_(c.args[0])
+    assert torch.equal(saw.paged_prompt_attn(c.cache, view, *c.args[1:]), saw.paged_prompt_attn(c.cache, *c.args))
+
+
+def test_captured_and_replayed(saw):
+    c = Case(saw, [5, 5, 33], [700, 64, 90])
+    q = c.args[0].clone()
+    ws = torch.empty(max(saw.paged_prompt_workspace_bytes(c.cache, q, 3, 704), saw.attn_weights_workspace_bytes(c.cache, q, 3, 704)), dtype=torch.uint8, device="cuda")
+    out, scores, prev = torch.empty_like(q), torch.zeros((3, 2, 704), device="cuda"), torch.rand((3, 2, 704), device="cuda")
+
+    def both():
+        saw.paged_prompt_attn(c.cache, q, *c.args[1:], max_seq_len=704, out=out, workspace=ws)
+        saw.paged_attn_weights(c.cache, q, *c.args[1:], prev=prev, scores=scores, max_seq_len=704, workspace=ws)
+
+    both()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+    for i in range(3):
+        q.copy_(pc.rand(q.shape, 20 + i, BF, 0.5))
+        ws.fill_(0xff)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), scores.clone()
+        both()
+        torch.cuda.synchronize()
+        assert torch.equal(out, got[0]) and torch.equal(scores, got[1])
+
+
+# ---- accumulated weights ----
+def _scores(c, prev):
+    """(scores, bound): a weight is off by at most w (exp(2 e) - 1 + 2^-20 + n 2^-22); then sums of as many terms as there are rows, in fp32."""
+    out, tol = prev.astype(np.float64), np.zeros(prev.shape)
+    rows = 1
+    for b, at, g, j, w, top, big in c.weights():
+        L = int(c.lens[b])
+        e = top * (c.d * 2.0 ** -23 + 2.0 ** -21) + big * 2.0 ** -22
+        out[b, g, :L] += w.sum(0)
+        tol[b, g, :L] += (w * (np.expm1(2 * e) + 2.0 ** -20 + L * 2.0 ** -22)[:, None]).sum(0)
+        rows = max(rows, c.G * (at.stop - at.start))
+    return out, (tol + np.abs(out) * (rows + 2) * 2.0 ** -24) * 1.01 + 1e-30
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d,G", [(128, 1), (128, 4), (128, 8), (64, 2), (64, 8)])
+@pytest.mark.parametrize("n,lens", SHAPES, ids=str)
+def test_weights(saw, n, lens, d, G, dtype):
+    c = Case(saw, n, lens, G=G, d=d, h=d, dtype=dtype, seed=len(n) + d)
+    prev = np.random.default_rng(1).random((len(n), 2, max(lens) + 21)).astype(np.float32)
+    want, tol = _scores(c, prev)
+    start = torch.full(prev.shape, 11.0, device="cuda")
+    got = saw.paged_attn_weights(c.cache, *c.args, prev=torch.from_numpy(prev).cuda(), scores=start, max_seq_len=max(lens)).cpu()
+    for b, L in enumerate(lens):
+        pc.check(got[b, :, :L], want[b, :, :L], tol[b, :, :L], b)
+        assert bool((got[b, :, L:] == 11).all())
+
+
+@pytest.mark.parametrize("options", OPTIONS, ids=str)
+def test_weights_under_rotations(saw, options):
+    c = Case(saw, [7, 1, 40], [60, 300, 40], seed=4, **options)
+    prev = np.zeros((3, 2, 304), np.float32)
+    want, tol = _scores(c, prev)
+    got = saw.paged_attn_weights(c.cache, *c.args, max_seq_len=304)
+    pc.check(got, want, tol)
+
+
+def test_weights_add_up_in_place_and_to_the_number_of_rows(saw):
+    """Every row's weights sum to one; a second call on the record itself doubles it."""
+    c = Case(saw, [4, 1, 0, 3], [300, 17, 9, 2])
+    scores = torch.zeros((4, 2, 304), device="cuda")
+    saw.paged_attn_weights(c.cache, *c.args, prev=scores, scores=scores, max_seq_len=304)
+    once = scores.clone()
+    total = once.double().sum(-1).cpu().numpy()
+    # (the last sequence's first query sees nothing)
+    assert np.abs(total - np.array([[16, 16], [4, 4], [0, 0], [8, 8]])).max() < 1e-4
+    saw.paged_attn_weights(c.cache, *c.args, prev=scores, scores=scores, max_seq_len=304)
+    assert torch.allclose(scores, 2 * once, rtol=2.0 ** -23, atol=0)
+
+
+def test_weights_without_queries_keep_the_record(saw):
+    c = Case(saw, [0, 0], [30, 5])
+    prev = torch.rand((2, 2, 32), device="cuda")
+    got = saw.paged_attn_weights(c.cache, *c.args, prev=prev, max_seq_len=32)
+    assert torch.equal(got[0, :, :30], prev[0, :, :30]) and torch.equal(got[1, :, :5], prev[1, :, :5])
+    assert torch.count_nonzero(got[1, :, 5:]) == 0
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_weights_of_slots_that_are_not_seen(saw, bad):
+    c = Case(saw, [3], [21])
+    clean = saw.paged_attn_weights(c.cache, *c.args, max_seq_len=32)
+    c.cache.k_meta[c.pt[0, 1], :, 5:] = bad
+    assert torch.equal(saw.paged_attn_weights(c.cache, *c.args, max_seq_len=32), clean)
+
+
+@pytest.mark.parametrize("n,lens,G", [([1, 1], [5000, 9000], 4), ([1], [20000], 8), ([2, 33], [7000, 3001], 2), ([1] * 40, list(range(100, 1300, 30)), 4)], ids=str)
+def test_long_contexts_split(saw, n, lens, G):
+    c = Case(saw, n, lens, G=G, seed=2)
+    want, tol = c.attention()
+    pc.check(saw.paged_prompt_attn(c.cache, *c.args), want, tol)
+    prev = np.zeros((len(n), 2, max(lens)), np.float32)
+    want, tol = _scores(c, prev)
+    pc.check(saw.paged_attn_weights(c.cache, *c.args, prev=torch.from_numpy(prev).cuda(), max_seq_len=max(lens)), want, tol)
