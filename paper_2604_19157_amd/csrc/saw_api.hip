@@ -289,7 +289,7 @@ static bool make_plan(const saw_cache_t* c, int B, int G, bool fixed, int max_pa
 }
 
 // ---- calls of packed queries and eviction ----
-int launch_prompt(const PromptParams&, int D, bool int4, hipStream_t);
+int launch_prompt(PromptParams, int D, bool int4, hipStream_t);
 int launch_weights(const PromptParams&, int D, hipStream_t);
 int launch_evict(const EvictParams&, int B, int D, hipStream_t);
 size_t prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len);

@@ -32,6 +32,8 @@ struct PromptParams {
   float* scores;
   int64_t score_stride;
   float* ws;
+  uint16_t* query;            // rotated queries in the workspace, fp16, and what each row was divided by
+  float* query_scale;
 };
 
 // Tokens of sequence b, whatever the offsets hold: inside [0, T] and not reversed.

@@ -1,4 +1,6 @@
 // Attention of packed queries: softmax(q K^T s) V with K and V of 16 bits or read from the INT4 pages.
+#include <type_traits>
+
 #include "saw_prompt_tile.h"
 
 namespace saw {
@@ -51,18 +53,75 @@ __device__ void unrotate_row(const PromptParams& p, float* x, int D, int lane) {
   }
 }
 
-template <typename M>
-__device__ __forceinline__ float widen(uint16_t x);
-template <> __device__ __forceinline__ float widen<MathBf16>(uint16_t x) { return bf16_to_f32(x); }
-template <> __device__ __forceinline__ float widen<MathF16>(uint16_t x) { return f16_to_f32(x); }
+// ---------------------------------------------------------------------------------------------------------------------------------
+// Rotated queries for the INT4 pages: one wavefront a row of 128 channels or two heads of 64.  A row leaves as fp16 times 2^-e, its
+// largest channel in [2^14, 2^15): relative rounding 2^-11 whatever the row's size, down to 2^-39 of the largest.
+//   ws: [rows][D] fp16 | [rows] float 2^e
+template <int D>
+__global__ __launch_bounds__(256) void prompt_query_kernel(PromptParams p) {
+  constexpr int E = D / 64;
+  __shared__ __attribute__((aligned(16))) float rows[4][128];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t n = p.T_q * p.n_q_heads, row = (int64_t)blockIdx.x * 4 + wave;
+  if (row >= n) return;
+  const int64_t at = row / p.n_q_heads * p.q_stride + row % p.n_q_heads * D;
+  float* const x = rows[wave];
+  if (E == 1) x[lane + 64] = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[lane + 64 * e] = load_elem(p.q, p.dtype, at + lane + 64 * e);
+  wave_sync();
+  rotate_row(p, x, D, lane);
+  float top = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[lane + 64 * e]));
+  top = max_xor32(max_xor16(row_allmax_positive(top)));
+  const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14;
+  const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+  uint16_t* const q = p.query + row * D;
+#pragma unroll
+  for (int e = 0; e < E; ++e) q[lane + 64 * e] = f32_to_f16(x[lane + 64 * e] * down);
+  if (lane == 0) p.query_scale[row] = __uint_as_float((uint32_t)(127 + ex) << 23);
+}
+
+// Keys and values of a tile on their way from the INT4 pages to shared memory: 16-byte pieces of 32 codes and the pairs of their tokens,
+// requested a tile ahead.
+template <int D, int NW>
+struct CodePieces {
+  static constexpr int kPieces = 2 * kTileKeys * (D / 32), kEach = kPieces / (64 * NW);
+  static_assert(kEach * 64 * NW == kPieces, "whole pieces per thread");
+  u32x4 codes[kEach];
+  f32x2 pair[kEach];
+  f32x2 key_pair;           // of key `lane` of the tile, for the tile's exponent
+};
+
+// x s - s z of 32 codes, as 16-bit values in channel order, to four places of a row
+template <typename M, int D, bool VALUE>
+__device__ __forceinline__ void put_piece(char* tile, int row, int piece, u32x4 w, float s, float sz) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t even = w[i] & 0x0f0f0f0fu, odd = (w[i] >> 4) & 0x0f0f0f0fu;
+    u32x4 x;
+    x.x = M::pack(fmaf((float)(even & 0xff), s, -sz), fmaf((float)(odd & 0xff), s, -sz));
+    x.y = M::pack(fmaf((float)((even >> 8) & 0xff), s, -sz), fmaf((float)((odd >> 8) & 0xff), s, -sz));
+    x.z = M::pack(fmaf((float)((even >> 16) & 0xff), s, -sz), fmaf((float)((odd >> 16) & 0xff), s, -sz));
+    x.w = M::pack(fmaf((float)(even >> 24), s, -sz), fmaf((float)(odd >> 24), s, -sz));
+    const int chunk = 4 * piece + i;
+    *(u32x4*)(tile + row * (2 * D) + 16 * (VALUE ? v_place(row, chunk) : k_place(row, chunk))) = x;
+  }
+}
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Prompt attention over 16-bit keys and values.
-// A block takes 32 rows per wavefront and goes over the keys in tiles of 64, which come from memory straight into a double buffer in
-// shared memory (each transfer has a whole tile's products to arrive in); one barrier a tile.
-template <int D, typename M, int NW>
+// Attention of packed rows.  A block takes 32 rows per wavefront and goes over the keys in tiles of 64, double-buffered in shared memory,
+// one barrier a tile.  Keys and values of 16 bits come from memory straight into the buffer (each transfer has a whole tile's
+// products to arrive in).  Those of the INT4 pages are requested a tile ahead into registers and written behind the tile's products:
+// K as fp16 times a power of two of the tile (its largest value just below 2^15, so that fp16 holds any scale; relative rounding 2^-11),
+// V as bf16 (2^-8, the output's own), each once per block and not once per row.
+template <int D, int KV, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
   constexpr int R = 32 * NW, kRow = 2 * D, kTile = kTileKeys * kRow, kInstr = kTile / 1024, kRpi = 1024 / kRow;
+  constexpr bool kInt4 = KV == kKvInt4;
+  using M1 = typename std::conditional<KV == kKvBf16, MathBf16, MathF16>::type;      // queries and keys
+  using M2 = typename std::conditional<KV == kKvF16, MathF16, MathBf16>::type;       // weights and values
   __shared__ __attribute__((aligned(1024))) char lds[2][2][kTile];       // [buffer][K, V]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % p.n_kv_heads;
@@ -70,8 +129,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
   const int64_t tile = (int64_t)gridDim.x / p.n_kv_heads - 1 - blockIdx.x / p.n_kv_heads;
   RowTile rt;
   if (!find_row_tile(p, tile, R, lane, rt)) return;
-  int k0, len;
-  packed_range(p.cu_k, rt.b, p.T_k, k0, len);
+  int k0 = 0, len;
+  if constexpr (kInt4) len = min(max(p.seq_lens[rt.b], 0), p.bound);
+  else packed_range(p.cu_k, rt.b, p.T_k, k0, len);
   const int shift = __builtin_ctz(p.group);
   auto sees_of = [&](int row) { return p.causal ? max(min(len, len - rt.n + (row >> shift) + 1), 0) : len; };   // (of a row of the sequence)
   const int last = rt.row0 + rt.rows - 1;
@@ -84,10 +144,15 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
 
   const int64_t token = rt.begin + (min(row, last) >> shift);
   const int head = h * p.group + (row & (p.group - 1));
+  const int64_t at = token * p.n_q_heads + head;
   u32x4 qf[D / 16];
+  float scale = p.scale;
+  {
+    const uint16_t* const src = kInt4 ? p.query + at * D : (const uint16_t*)p.q + token * p.q_stride + (int64_t)head * D;
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks)
-    qf[ks] = *(const u32x4*)((const uint16_t*)p.q + token * p.q_stride + (int64_t)head * D + 16 * ks + 8 * (lane >> 5));
+    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const u32x4*)(src + 16 * ks + 8 * (lane >> 5));
+    if (kInt4) scale *= p.query_scale[at];
+  }
   RowState<D> st;
   st.m = -INFINITY; st.ref = 0.f; st.sum = 0.f;
 #pragma unroll
@@ -95,31 +160,92 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) st.o[t][r] = 0.f;
 
+  auto products = [&](int buf, int t, float tile_scale) {
+    if (t * kTileKeys >= wend) return;
+    f32x16 s[2];
+    u32x4 pf[4];
+    tile_logits<D, M1>(lds[buf][0], qf, s, lane);
+    if ((t + 1) * kTileKeys > wfull) tile_mask(s, sees - t * kTileKeys, lane);
+    tile_weights<D, M2>(s, tile_scale, st, pf);
+    tile_values<D, M2>(lds[buf][1], pf, st, lane);
+  };
+
   const uint16_t* const kp = (const uint16_t*)p.k + (int64_t)k0 * p.k_stride + (int64_t)h * D;
   const uint16_t* const vp = (const uint16_t*)p.v + (int64_t)k0 * p.v_stride + (int64_t)h * D;
-  auto load = [&](int buf, int t) {
+  if constexpr (!kInt4) {
+    auto load = [&](int buf, int t) {
 #pragma unroll
-    for (int j = 0; j < kInstr / NW; ++j) {
-      const int in = wave * (kInstr / NW) + j;                             // 1024 bytes: kRpi rows
-      const int r = in * kRpi + lane / (D / 8), place = lane % (D / 8);
-      const int64_t key = min(t * kTileKeys + r, len - 1);                 // (behind the end: the last key again, masked)
-      __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)(kp + key * p.k_stride + 8 * k_place(r, place)), (LDS_AS void*)(lds[buf][0] + in * 1024), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)(vp + key * p.v_stride + 8 * v_place(r, place)), (LDS_AS void*)(lds[buf][1] + in * 1024), 16, 0, 0);
+      for (int j = 0; j < kInstr / NW; ++j) {
+        const int in = wave * (kInstr / NW) + j;                             // 1024 bytes: kRpi rows
+        const int r = in * kRpi + lane / (D / 8), place = lane % (D / 8);
+        const int64_t key = min(t * kTileKeys + r, len - 1);                 // (behind the end: the last key again, masked)
+        __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)(kp + key * p.k_stride + 8 * k_place(r, place)), (LDS_AS void*)(lds[buf][0] + in * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)(vp + key * p.v_stride + 8 * v_place(r, place)), (LDS_AS void*)(lds[buf][1] + in * 1024), 16, 0, 0);
+      }
+    };
+    if (t0 < t1) load(0, t0);
+    for (int t = t0; t < t1; ++t) {
+      const int buf = (t - t0) & 1;
+      __builtin_amdgcn_s_waitcnt(0x0F70);                                   // vmcnt(0): this wavefront's part of tile t is there
+      lds_barrier();                                                        // ... everybody's is, and nobody reads the other buffer any more
+      if (t + 1 < t1) load(buf ^ 1, t + 1);
+      products(buf, t, scale);
     }
-  };
-  if (t0 < t1) load(0, t0);
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    __builtin_amdgcn_s_waitcnt(0x0F70);                                   // vmcnt(0): this wavefront's part of tile t is there
-    lds_barrier();                                                        // ... everybody's is, and nobody reads the other buffer any more
-    if (t + 1 < t1) load(buf ^ 1, t + 1);
-    if (t * kTileKeys < wend) {
-      f32x16 s[2];
-      u32x4 pf[4];
-      tile_logits<D, M>(lds[buf][0], qf, s, lane);
-      if ((t + 1) * kTileKeys > wfull) tile_mask(s, sees - t * kTileKeys, lane);
-      tile_weights<D, M>(s, p.scale, st, pf);
-      tile_values<D, M>(lds[buf][1], pf, st, lane);
+  } else {
+    using Pieces = CodePieces<D, NW>;
+    const int32_t* const pages = p.page_table + (int64_t)rt.b * p.max_pages;
+    const int threads = 64 * NW;
+    // (a tile is four pages; ids of pages behind the sequence's last are not looked at)
+    auto vector_of = [&](const int (&page)[4], int key) {                    // of a key of the tile
+      const int i = key >> 4, id = i == 0 ? page[0] : i == 1 ? page[1] : i == 2 ? page[2] : page[3];
+      return ((int64_t)id * p.n_kv_heads + h) * 16 + (key & 15);
+    };
+    auto request = [&](int t, Pieces& c) {
+      int page[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        page[i] = pages[min(4 * t + i, (len - 1) >> 4)];
+        if (page[i] < 0 || page[i] >= p.num_pages) page[i] = 0;
+      }
+#pragma unroll
+      for (int j = 0; j < Pieces::kEach; ++j) {
+        const int piece = j * threads + threadIdx.x, value = piece >= Pieces::kPieces / 2, i = value ? piece - Pieces::kPieces / 2 : piece;
+        const int key = i / (D / 32);
+        const int64_t vec = vector_of(page, key);
+        c.codes[j] = ((const u32x4*)((value ? p.v_codes : p.k_codes) + vec * (D / 2)))[i % (D / 32)];
+        c.pair[j] = ((const f32x2*)(value ? p.v_meta : p.k_meta))[vec];
+        if (t * kTileKeys + key >= len) c.pair[j] = f32x2{0.f, 0.f};         // (slots behind the end may hold anything)
+      }
+      c.key_pair = ((const f32x2*)p.k_meta)[vector_of(page, lane)];
+      if (t * kTileKeys + lane >= len) c.key_pair = f32x2{0.f, 0.f};
+    };
+    auto put = [&](int buf, const Pieces& c) {                               // returns the tile's power of two
+      float top = fmaxf(fabsf(c.key_pair.x * c.key_pair.y), fabsf(c.key_pair.x * (15.f - c.key_pair.y)));
+      if (!(top < INFINITY)) top = 0.f;
+      top = max_xor32(max_xor16(row_allmax_positive(top)));
+      const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -100) - 14;
+      const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+#pragma unroll
+      for (int j = 0; j < Pieces::kEach; ++j) {
+        const int piece = j * threads + threadIdx.x, value = piece >= Pieces::kPieces / 2, i = value ? piece - Pieces::kPieces / 2 : piece;
+        const float s = c.pair[j].x, sz = s * c.pair[j].y;
+        if (value) put_piece<M2, D, true>(lds[buf][1], i / (D / 32), i % (D / 32), c.codes[j], s, sz);
+        else put_piece<M1, D, false>(lds[buf][0], i / (D / 32), i % (D / 32), c.codes[j], s * down, sz * down);
+      }
+      return __uint_as_float((uint32_t)(127 + ex) << 23);
+    };
+    Pieces c;
+    float tile_scale = 1.f;
+    if (t0 < t1) {
+      request(t0, c);
+      tile_scale = put(0, c);
+    }
+    for (int t = t0; t < t1; ++t) {
+      const int buf = (t - t0) & 1;
+      lds_barrier();
+      if (t + 1 < t1) request(t + 1, c);
+      products(buf, t, scale * tile_scale);
+      if (t + 1 < t1) tile_scale = put(buf ^ 1, c);
     }
   }
   const float sum = add_xor32(st.sum);
@@ -130,45 +256,49 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
   for (int t = 0; t < D / 32; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) odd = fmaf(st.o[t][r], 0.f, odd);
-  const bool split = gridDim.y > 1;
-  float* const records = p.ws + (int64_t)blockIdx.y * p.T_q * p.n_q_heads * D;
-  float2* const ml = (float2*)(p.ws + (int64_t)gridDim.y * p.T_q * p.n_q_heads * D) + (int64_t)blockIdx.y * p.T_q * p.n_q_heads;
+  const bool split = kInt4 || gridDim.y > 1;
+  const int64_t rows = p.T_q * p.n_q_heads;
+  float* const records = p.ws + (int64_t)blockIdx.y * rows * D;
+  float2* const ml = (float2*)(p.ws + (int64_t)gridDim.y * rows * D) + (int64_t)blockIdx.y * rows;
   if (__any(odd != odd)) {
     constexpr int E = D / 64;
+    const RowSource<D, KV> src = {p, rt.b, h, k0, lane};
     for (int i = 0; i < 32 && w0 + i <= last; ++i) {
       const int64_t tok = rt.begin + ((w0 + i) >> shift);
       const int hd = h * p.group + ((w0 + i) & (p.group - 1));
+      const int64_t mine = tok * p.n_q_heads + hd;
       const int end = min(sees_of(w0 + i), t1 * kTileKeys);
       float q[E], acc[E], m = -INFINITY, den = 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        q[e] = widen<M>(((const uint16_t*)p.q)[tok * p.q_stride + (int64_t)hd * D + lane + 64 * e]) * p.scale;
+        if constexpr (kInt4) q[e] = f16_to_f32(p.query[mine * D + lane + 64 * e]) * p.query_scale[mine] * p.scale;
+        else q[e] = load_elem(p.q, p.dtype, tok * p.q_stride + (int64_t)hd * D + lane + 64 * e) * p.scale;
         acc[e] = 0.f;
       }
       for (int j = t0 * kTileKeys; j < end; ++j) {
-        float x = 0.f;
+        float k[E], v[E], x = 0.f;
+        src.load(false, j, k);
+        src.load(true, j, v);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x = fmaf(q[e], widen<M>(kp[j * p.k_stride + lane + 64 * e]), x);
+        for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
         x = add_xor32(add_xor16(row_allsum(x)));
         const float top = fmaxf(m, x), ref = top == -INFINITY ? 0.f : top;
         const float alpha = fast_exp2(m - ref), w = fast_exp2(x - ref);
         m = top;
         den = fmaf(den, alpha, w);
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(acc[e], alpha, w * widen<M>(vp[j * p.v_stride + lane + 64 * e]));
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(acc[e], alpha, w * v[e]);
       }
-      const int64_t at = tok * p.n_q_heads + hd;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        if (split) records[at * D + lane + 64 * e] = acc[e];
-        else store_elem(p.out, p.dtype, at * D + lane + 64 * e, den == 0.f ? 0.f : acc[e] / den);
+        if (split) records[mine * D + lane + 64 * e] = acc[e];
+        else store_elem(p.out, p.dtype, mine * D + lane + 64 * e, den == 0.f ? 0.f : acc[e] / den);
       }
-      if (split && lane == 0) ml[at] = make_float2(m, den);
+      if (split && lane == 0) ml[mine] = make_float2(m, den);
     }
     return;
   }
   if (row > last) return;
-  const int64_t at = token * p.n_q_heads + head;
   if (split) {
     if (lane < 32) ml[at] = make_float2(st.m, sum);
     if (sum != 0.f)
@@ -185,13 +315,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
 #pragma unroll
     for (int r = 0; r < 16; r += 4)
       *(u32x2*)((uint16_t*)p.out + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) =
-          u32x2{M::pack(st.o[t][r] * inv, st.o[t][r + 1] * inv), M::pack(st.o[t][r + 2] * inv, st.o[t][r + 3] * inv)};
+          u32x2{M2::pack(st.o[t][r] * inv, st.o[t][r + 1] * inv), M2::pack(st.o[t][r + 2] * inv, st.o[t][r + 3] * inv)};
 }
 
 // Joins the partial records of a row: one wavefront a row.
-template <int D>
+template <int D, bool INT4>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int splits) {
   constexpr int E = D / 64;
+  __shared__ __attribute__((aligned(16))) float rotated[4][128];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t rows = p.T_q * p.n_q_heads, row = (int64_t)blockIdx.x * 4 + wave;
   if (row >= rows) return;
@@ -215,7 +346,19 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int s
     for (int e = 0; e < E; ++e) o[e] = fmaf(w, p.ws[(s * rows + row) * D + E * lane + e], o[e]);
   }
 #pragma unroll
-  for (int e = 0; e < E; ++e) store_elem(p.out, p.dtype, row * D + E * lane + e, den == 0.f ? 0.f : o[e] / den);
+  for (int e = 0; e < E; ++e) o[e] = den == 0.f ? 0.f : o[e] / den;
+  if (INT4 && (p.rot_v || p.dense_v)) {
+    float* const x = rotated[wave];
+    if (E == 1) x[lane + 64] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[E * lane + e] = o[e];
+    wave_sync();
+    unrotate_row(p, x, D, lane);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = x[E * lane + e];
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) store_elem(p.out, p.dtype, row * D + E * lane + e, o[e]);
 }
 
 // How a call is handed out: wavefronts of a block and splits of the keys.
@@ -229,58 +372,6 @@ static PromptPlan prompt_plan(int G, int Hkv, int64_t T, int B, int64_t max_k_le
   return r;
 }
 static size_t record_bytes(int D, int64_t rows, int splits) { return (size_t)rows * splits * (D + 2) * 4; }
-
-template <int D, int KV>
-__global__ __launch_bounds__(256) void attn_rows_kernel(PromptParams p) {
-  constexpr int E = D / 64;
-  __shared__ __attribute__((aligned(16))) float rows[4][128];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
-  if (row >= p.T_q * p.n_q_heads) return;
-  const int64_t token = row / p.n_q_heads;
-  const int head = (int)(row % p.n_q_heads);
-  int b = -1, begin = 0, n = 0;
-  for (int i = 0; i < p.B && b < 0; ++i) {
-    packed_range(p.cu_q, i, p.T_q, begin, n);
-    if (token >= begin && token < begin + n) b = i;
-  }
-  if (b < 0) return;
-  int k0 = 0, len;
-  if (KV == kKvInt4) len = min(max(p.seq_lens[b], 0), p.bound);
-  else packed_range(p.cu_k, b, p.T_k, k0, len);
-  const int i = (int)(token - begin);
-  const int sees = p.causal ? min(len, len - n + i + 1) : len;
-  const RowSource<D, KV> src = {p, b, head / p.group, k0, lane};
-  float* const x = rows[wave];
-  const uint16_t* const qr = (const uint16_t*)p.q + token * p.q_stride + (int64_t)head * D;
-  if (E == 1) x[lane + 64] = 0.f;
-  for (int e = 0; e < E; ++e) x[lane + 64 * e] = p.dtype == SAW_BF16 ? bf16_to_f32(qr[lane + 64 * e]) : f16_to_f32(qr[lane + 64 * e]);
-  wave_sync();
-  if (KV == kKvInt4) rotate_row(p, x, D, lane);
-  float q[E], acc[E], m = -INFINITY, den = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) { q[e] = x[lane + 64 * e] * p.scale; acc[e] = 0.f; }
-  for (int j = 0; j < sees; ++j) {
-    float k[E], v[E], t = 0.f;
-    src.load(false, j, k);
-    src.load(true, j, v);
-#pragma unroll
-    for (int e = 0; e < E; ++e) t = fmaf(q[e], k[e], t);
-    t = add_xor32(add_xor16(row_allsum(t)));
-    const float top = fmaxf(m, t);
-    const float ref = top == -INFINITY ? 0.f : top;
-    const float alpha = fast_exp2(m - ref), w = fast_exp2(t - ref);
-    m = top;
-    den = fmaf(den, alpha, w);
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(acc[e], alpha, w * v[e]);
-  }
-  wave_sync();
-  for (int e = 0; e < E; ++e) x[lane + 64 * e] = den == 0.f ? 0.f : acc[e] / den;
-  wave_sync();
-  if (KV == kKvInt4) unrotate_row(p, x, D, lane);
-  for (int e = 0; e < E; ++e) store_elem(p.out, p.dtype, row * D + lane + 64 * e, x[lane + 64 * e]);
-}
 
 // (max, sum) of every row's logits, for the weights
 template <int D>
@@ -351,28 +442,31 @@ __global__ __launch_bounds__(256) void weights_kernel(PromptParams p) {
   if (lane == 0) p.scores[at] = (p.prev ? p.prev[at] : 0.f) + total;
 }
 
-template <int D, typename M>
-static void launch_prompt16(const PromptParams& p, const PromptPlan& plan, hipStream_t st) {
-  const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, 32 * plan.waves, p.B) * p.n_kv_heads), plan.splits);
-  prompt_kernel<D, M, 4><<<grid, dim3(256), 0, st>>>(p);
-  if (plan.splits > 1) prompt_merge_kernel<D><<<dim3((unsigned)((p.T_q * p.n_q_heads + 3) / 4)), dim3(256), 0, st>>>(p, plan.splits);
+template <int D, int KV>
+static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream_t st) {
+  const int64_t rows = p.T_q * p.n_q_heads;
+  const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, 32 * plan.waves, p.B) * p.n_kv_heads), plan.splits), by_row((unsigned)((rows + 3) / 4)), block(256);
+  if (KV == kKvInt4) prompt_query_kernel<D><<<by_row, block, 0, st>>>(p);
+  prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
+  if (KV == kKvInt4 || plan.splits > 1) prompt_merge_kernel<D, KV == kKvInt4><<<by_row, block, 0, st>>>(p, plan.splits);
 }
 
-int launch_prompt(const PromptParams& p, int D, bool int4, hipStream_t st) {
+int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
   const int64_t rows = p.T_q * p.n_q_heads;
+  const PromptPlan plan = prompt_plan(p.group, p.n_kv_heads, p.T_q, p.B, p.bound);
+  if (row_tiles(p.T_q, p.group, 32 * plan.waves, p.B) * p.n_kv_heads > 0x7fffffffLL || rows / 4 >= 0x7fffffffLL) return SAW_EINVAL;
   if (int4) {
-    const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
-    if (D == 128) attn_rows_kernel<128, kKvInt4><<<grid, block, 0, st>>>(p);
-    else attn_rows_kernel<64, kKvInt4><<<grid, block, 0, st>>>(p);
+    // (behind the records: rows of D + 2 floats)
+    p.query_scale = p.ws + ((D + 2) * rows * plan.splits + 3) / 4 * 4;
+    p.query = (uint16_t*)(p.query_scale + (rows + 3) / 4 * 4);
+    if (D == 128) launch_rows<128, kKvInt4>(p, plan, st);
+    else launch_rows<64, kKvInt4>(p, plan, st);
+  } else if (D == 128) {
+    if (p.dtype == SAW_BF16) launch_rows<128, kKvBf16>(p, plan, st);
+    else launch_rows<128, kKvF16>(p, plan, st);
   } else {
-    const PromptPlan plan = prompt_plan(p.group, p.n_kv_heads, p.T_q, p.B, p.bound);
-    if (D == 128) {
-      if (p.dtype == SAW_BF16) launch_prompt16<128, MathBf16>(p, plan, st);
-      else launch_prompt16<128, MathF16>(p, plan, st);
-    } else {
-      if (p.dtype == SAW_BF16) launch_prompt16<64, MathBf16>(p, plan, st);
-      else launch_prompt16<64, MathF16>(p, plan, st);
-    }
+    if (p.dtype == SAW_BF16) launch_rows<64, kKvBf16>(p, plan, st);
+    else launch_rows<64, kKvF16>(p, plan, st);
   }
   return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;
 }
@@ -394,7 +488,11 @@ size_t prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len)
   const PromptPlan plan = prompt_plan(Hq / Hkv, Hkv, T, B, max_k_len);
   return 16 + (plan.splits > 1 ? record_bytes(D, T * Hq, plan.splits) : 0);
 }
-size_t paged_prompt_bytes(int, int, int, int64_t, int, int64_t) { return 16; }
+size_t paged_prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len) {
+  const PromptPlan plan = prompt_plan(Hq / Hkv, Hkv, T, B, max_k_len);
+  const int64_t rows = T * Hq;
+  return 32 + record_bytes(D, rows, plan.splits) + (size_t)(rows + 3) / 4 * 16 + (size_t)rows * D * 2;
+}
 size_t weights_bytes(int D, int Hq, int, int64_t T, int, int64_t) { return 16 + (size_t)T * Hq * (D + 2) * 4; }
 
 }  // namespace saw

@@ -3,10 +3,11 @@
 Bounds.  With u the half step of the output's type (bf16 2^-8, fp16 2^-11), w the exact weights of a row, A = sum_j w_j |v_j| per channel and
 e the most that a logit can be off, an output is off by at most
     u |o| + A (u_p + exp(2 e) - 1 + 2^-20 + n 2^-22)          (1 + a few u for products of these)
-  u_p      rounding of a weight before the product with V (its type's half step; two bf16 limbs: 2^-16)
+  u_p      rounding of a weight before the product with V (its type's half step; over the INT4 pages weight and value enter as bf16, 2^-7)
   2 e      in the exponent: a weight's logit and its sum's, off in opposite directions
   2^-20    the exponential and the division;  n 2^-22   sums of n terms in fp32, of weights and of the product (each at most n 2^-23)
-and e = scale (sum_c |q_c k_c|) (d 2^-23 + u_q) + 2^-22 |logit|, u_q the rounding of a rotated query (two fp16 limbs: 2^-21; none: 0).
+and e = scale (sum_c |q_c k_c|) (d 2^-23 + u_q) + 2^-22 |logit|, u_q the rounding of query and key
+before their product (over the INT4 pages fp16 each, 2^-10; two fp16 limbs of the query: 2^-21; 16-bit keys: 0).
 """
 import numpy as np
 import torch
@@ -43,8 +44,9 @@ def visible(n, L, causal=True):
     return np.arange(L)[None, :] <= np.arange(n)[:, None] + L - n
 
 
-def bound(o, A, top, big, n, d, u, u_p, u_q=0.0):
-    e = top * (d * 2.0 ** -23 + u_q) + big * 2.0 ** -22
+def bound(o, A, top, big, n, d, u, u_p, u_q=0.0, more=0.0):
+    """more: a further part of e"""
+    e = top * (d * 2.0 ** -23 + u_q) + big * 2.0 ** -22 + more
     rel = u_p + np.expm1(2 * e) + 2.0 ** -20 + n * 2.0 ** -22
     return (u * np.abs(o) + A * rel[:, None]) * (1 + 4 * u) + 1e-30
 
