@@ -2,6 +2,7 @@
 #include <type_traits>
 
 #include "saw_prompt_tile.h"
+#include "saw_rotate_row.h"
 
 namespace saw {
 
@@ -31,27 +32,6 @@ struct RowSource {
     }
   }
 };
-
-// q R and o R^T of one row in LDS (128 floats; of 64 channels the first half)
-__device__ void rotate_row(const PromptParams& p, float* x, int D, int lane) {
-  if (p.rot_k) {
-    if (p.has_signs)
-      for (int c = lane; c < D; c += 64) x[c] = apply_sign(p.signs, c, x[c]);
-    wave_sync();
-    wave_lds_fwht128<1>(x, p.had_block, lane);
-    for (int c = lane; c < D; c += 64) x[c] *= had_norm(p.had_block);
-    wave_sync();
-  }
-  if (p.dense_k) wave_lds_matvec128<1>(x, p.dense, lane);
-}
-__device__ void unrotate_row(const PromptParams& p, float* x, int D, int lane) {
-  if (p.dense_v) wave_lds_matvec128<1>(x, p.dense + kDenseD * kDenseD, lane);
-  if (p.rot_v) {
-    wave_lds_fwht128<1>(x, p.had_block, lane);
-    for (int c = lane; c < D; c += 64) x[c] = apply_sign(p.signs, c, x[c] * had_norm(p.had_block));
-    wave_sync();
-  }
-}
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Rotated queries for the INT4 pages: one wavefront a row of 128 channels or two heads of 64.  A row leaves as fp16 times 2^-e, its
@@ -373,75 +353,6 @@ static PromptPlan prompt_plan(int G, int Hkv, int64_t T, int B, int64_t max_k_le
 }
 static size_t record_bytes(int D, int64_t rows, int splits) { return (size_t)rows * splits * (D + 2) * 4; }
 
-// (max, sum) of every row's logits, for the weights
-template <int D>
-__global__ __launch_bounds__(256) void row_stats_kernel(PromptParams p) {
-  constexpr int E = D / 64;
-  __shared__ __attribute__((aligned(16))) float rows[4][128];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
-  if (row >= p.T_q * p.n_q_heads) return;
-  const int64_t token = row / p.n_q_heads;
-  const int head = (int)(row % p.n_q_heads);
-  int b = -1, begin = 0, n = 0;
-  for (int i = 0; i < p.B && b < 0; ++i) {
-    packed_range(p.cu_q, i, p.T_q, begin, n);
-    if (token >= begin && token < begin + n) b = i;
-  }
-  if (b < 0) return;
-  const int len = min(max(p.seq_lens[b], 0), p.bound);
-  const int sees = min(len, len - n + (int)(token - begin) + 1);
-  const RowSource<D, kKvInt4> src = {p, b, head / p.group, 0, lane};
-  float* const x = rows[wave];
-  const uint16_t* const qr = (const uint16_t*)p.q + token * p.q_stride + (int64_t)head * D;
-  if (E == 1) x[lane + 64] = 0.f;
-  for (int e = 0; e < E; ++e) x[lane + 64 * e] = p.dtype == SAW_BF16 ? bf16_to_f32(qr[lane + 64 * e]) : f16_to_f32(qr[lane + 64 * e]);
-  wave_sync();
-  rotate_row(p, x, D, lane);
-  float* const out = p.ws + row * (D + 2);
-  float q[E], m = -INFINITY, den = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) { q[e] = x[lane + 64 * e] * p.scale; out[2 + lane + 64 * e] = q[e]; }
-  for (int j = 0; j < sees; ++j) {
-    float k[E], t = 0.f;
-    src.load(false, j, k);
-#pragma unroll
-    for (int e = 0; e < E; ++e) t = fmaf(q[e], k[e], t);
-    t = add_xor32(add_xor16(row_allsum(t)));
-    const float top = fmaxf(m, t);
-    const float ref = top == -INFINITY ? 0.f : top;
-    den = fmaf(den, fast_exp2(m - ref), fast_exp2(t - ref));
-    m = top;
-  }
-  if (lane == 0) { out[0] = m == -INFINITY ? 0.f : m; out[1] = den; }
-}
-
-// a wavefront per (sequence, kv head, position): the sum over the rows that see it
-template <int D>
-__global__ __launch_bounds__(256) void weights_kernel(PromptParams p) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int b = blockIdx.z, h = blockIdx.y, j = blockIdx.x * 4 + wave;
-  const int len = min(max(p.seq_lens[b], 0), p.bound);
-  if (j >= len) return;
-  int begin, n;
-  packed_range(p.cu_q, b, p.T_q, begin, n);
-  const RowSource<D, kKvInt4> src = {p, b, h, 0, lane};
-  float k[E], total = 0.f;
-  src.load(false, j, k);
-  for (int i = max(0, j - (len - n)); i < n; ++i)
-    for (int g = 0; g < p.group; ++g) {
-      const float* const r = p.ws + ((int64_t)(begin + i) * p.n_q_heads + h * p.group + g) * (D + 2);
-      float t = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) t = fmaf(r[2 + lane + 64 * e], k[e], t);
-      t = add_xor32(add_xor16(row_allsum(t)));
-      if (r[1] != 0.f) total += fast_exp2(t - r[0]) / r[1];
-    }
-  const int64_t at = ((int64_t)b * p.n_kv_heads + h) * p.score_stride + j;
-  if (lane == 0) p.scores[at] = (p.prev ? p.prev[at] : 0.f) + total;
-}
-
 template <int D, int KV>
 static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream_t st) {
   const int64_t rows = p.T_q * p.n_q_heads;
@@ -471,19 +382,6 @@ int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;
 }
 
-int launch_weights(const PromptParams& p, int D, hipStream_t st) {
-  const int64_t rows = p.T_q * p.n_q_heads;
-  const dim3 grid((unsigned)((rows + 3) / 4)), block(256), wgrid((p.bound + 3) / 4, p.n_kv_heads, p.B);
-  if (D == 128) {
-    if (rows) row_stats_kernel<128><<<grid, block, 0, st>>>(p);
-    weights_kernel<128><<<wgrid, block, 0, st>>>(p);
-  } else {
-    if (rows) row_stats_kernel<64><<<grid, block, 0, st>>>(p);
-    weights_kernel<64><<<wgrid, block, 0, st>>>(p);
-  }
-  return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;
-}
-
 size_t prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len) {
   const PromptPlan plan = prompt_plan(Hq / Hkv, Hkv, T, B, max_k_len);
   return 16 + (plan.splits > 1 ? record_bytes(D, T * Hq, plan.splits) : 0);
@@ -493,6 +391,4 @@ size_t paged_prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_
   const int64_t rows = T * Hq;
   return 32 + record_bytes(D, rows, plan.splits) + (size_t)(rows + 3) / 4 * 16 + (size_t)rows * D * 2;
 }
-size_t weights_bytes(int D, int Hq, int, int64_t T, int, int64_t) { return 16 + (size_t)T * Hq * (D + 2) * 4; }
-
 }  // namespace saw

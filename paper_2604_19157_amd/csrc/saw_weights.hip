@@ -1,0 +1,309 @@
+// Accumulated attention weights: for every cached token the sum of its softmax weights over packed queries and the heads of a group.
+//
+//   x_ij = q~_i . s_j (c_j - z_j) = s_j (q~_i . (c_j - 8) - (z_j - 8) sum q~_i),   w_j = sum_i exp2(x_ij - m_i) / l_i
+//
+// Codes minus 8 are exact in fp16 and a rotated query is two fp16 limbs of its scaled self, so the matrix product is exact up to the sums:
+// the result is an fp32 record that grows over many steps.  Keys stand in the lanes and rows in the registers, so a key's scale and
+// zero-point are the lane's own, its sum over the rows needs no exchange but one at the end, and keys go from memory to operand registers
+// without shared memory: a lane holds a quarter of one key's codes, and the products run over the channels in the order in which
+// four instructions take the codes out of a word (0 4 1 5 2 6 3 7), which is how the query limbs are laid out.
+// Two passes over the keys: maximum and sum of every row (split over the keys, joined by a small pass), then the weights.
+#include "saw_prompt_tile.h"
+#include "saw_rotate_row.h"
+
+namespace saw {
+
+constexpr int kWeightRows = 16;                 // rows of a matrix tile
+constexpr int kWeightKeys = 64;                 // keys of a wavefront's step: four tiles of 16
+constexpr int kGroupTiles = 16;                 // row tiles that a block of the first pass takes
+
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// What the passes know of a row: the scale of its limbs, the sum of its channels; then its maximum and 1 / sum.
+struct RowInfo { float scale, sum_q, m, inv; };
+
+// The workspace: operand registers of every (row tile, head), row infos, and the first pass's partial (maximum, sum) pairs.
+template <int D>
+struct WeightSpace {
+  u32x4* limbs;             // [tile][head][limb][D / 32][64 lanes]
+  RowInfo* info;            // [tile][head][16]
+  float2* part;             // [chunk][tile][head][16]
+  int64_t tiles;
+  __host__ __device__ WeightSpace(float* ws, int64_t tiles, int heads) : tiles(tiles) {
+    limbs = (u32x4*)ws;
+    info = (RowInfo*)(limbs + tiles * heads * 2 * (D / 32) * 64);
+    part = (float2*)(info + tiles * heads * kWeightRows);
+  }
+};
+
+// Rotated queries of a row tile as operand registers: a wavefront per four rows.
+template <int D>
+__global__ __launch_bounds__(256) void weight_query_kernel(PromptParams p, int64_t tiles) {
+  constexpr int E = D / 64;
+  __shared__ __attribute__((aligned(16))) float rows[4][128];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y;
+  const WeightSpace<D> ws(p.ws, tiles, p.n_kv_heads);
+  RowTile rt;
+  if (!find_row_tile(p, blockIdx.x, kWeightRows, lane, rt)) return;
+  const int64_t at = (int64_t)blockIdx.x * p.n_kv_heads + h;
+  uint16_t* const limbs = (uint16_t*)(ws.limbs + at * 2 * (D / 32) * 64);
+  float* const x = rows[wave];
+  for (int k = 0; k < 4; ++k) {
+    const int r = 4 * wave + k, row = rt.row0 + min(r, rt.rows - 1);        // (rows behind the last: the last again, never looked at)
+    const int64_t src = (rt.begin + row / p.group) * p.q_stride + (int64_t)(h * p.group + row % p.group) * D;
+    if (E == 1) x[lane + 64] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[lane + 64 * e] = load_elem(p.q, p.dtype, src + lane + 64 * e);
+    wave_sync();
+    rotate_row(p, x, D, lane);
+    float top = 0.f, total = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[lane + 64 * e] * p.scale));
+    top = max_xor32(max_xor16(row_allmax_positive(top)));
+    const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14;
+    const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = lane + 64 * e, quarter = c / (D / 4), ks = c % (D / 4) / 8, i = 2 * (c % 4) + (c / 4) % 2;
+      const float v = x[c] * p.scale * down;
+      const uint16_t hi = f32_to_f16(v), lo = f32_to_f16(v - f16_to_f32(hi));
+      total += f16_to_f32(hi) + f16_to_f32(lo);
+      limbs[(ks * 64 + 16 * quarter + r) * 8 + i] = hi;
+      limbs[((D / 32 + ks) * 64 + 16 * quarter + r) * 8 + i] = lo;
+    }
+    total = add_xor32(add_xor16(row_allsum(total)));
+    if (lane == 0) ws.info[at * kWeightRows + r] = RowInfo{__uint_as_float((uint32_t)(127 + ex) << 23), total, 0.f, 0.f};
+    wave_sync();
+  }
+}
+
+// A wavefront's keys of one step as they come from memory: key 16 t + lane % 16, quarter lane / 16 of its codes.
+template <int D>
+struct KeyCodes {
+  uint32_t w[4][D / 32];
+  f32x2 pair[4];
+};
+template <int D>
+__device__ __forceinline__ void request_keys(const PromptParams& p, int b, int h, int key0, int len, int lane, KeyCodes<D>& k) {
+  const int32_t* const pages = p.page_table + (int64_t)b * p.max_pages;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    int page = pages[min((key0 >> 4) + t, (len - 1) >> 4)];
+    if (page < 0 || page >= p.num_pages) page = 0;
+    const int64_t vec = ((int64_t)page * p.n_kv_heads + h) * 16 + (lane & 15);
+    const uint8_t* const src = p.k_codes + vec * (D / 2) + (lane >> 4) * (D / 8);
+    if constexpr (D == 128) {
+      const u32x4 x = *(const u32x4*)src;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k.w[t][i] = x[i];
+    } else {
+      const u32x2 x = *(const u32x2*)src;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) k.w[t][i] = x[i];
+    }
+    k.pair[t] = ((const f32x2*)p.k_meta)[vec];
+  }
+}
+// codes - 8 of a word, in the order 0 4 1 5 2 6 3 7: 0x6400 + c is 1024 + c
+__device__ __forceinline__ u32x4 centred(uint32_t w) {
+  u32x4 r;
+  const f16x2 off = {(_Float16)1032.f, (_Float16)1032.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u) - off);
+  return r;
+}
+
+// Logits of 16 rows and 64 keys: x[t][r] of row 4 (lane / 16) + r and key 16 t + lane % 16, in log2 units; hidden ones -infinity.
+template <int D>
+__device__ __forceinline__ void step_logits(const u32x4* limbs, const u32x4 (&k)[4][D / 32], const f32x2 (&pair)[4], const RowInfo* info, int key0,
+                                            bool masked, int first_hidden, int shift, int row0, int lane, f32x4 (&x)[4]) {
+  u32x4 q[2][D / 32];
+#pragma unroll
+  for (int l = 0; l < 2; ++l)
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) q[l][ks] = limbs[(l * (D / 32) + ks) * 64 + lane];
+  float scale[4], sum_q[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const f32x2 v = *(const f32x2*)&info[4 * (lane >> 4) + r].scale;
+    scale[r] = v.x;
+    sum_q[r] = v.y;
+  }
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int l = 1; l >= 0; --l)
+#pragma unroll
+      for (int ks = 0; ks < D / 32; ++ks) s = mfma16(q[l][ks], k[t][ks], s);
+    const float z8 = pair[t].y - 8.f;
+    const int key = key0 + 16 * t + (lane & 15);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      x[t][r] = fmaf(-z8, sum_q[r], s[r]) * pair[t].x * scale[r];
+      // (row i sees the keys in front of first_hidden + its token)
+      if (masked && key >= first_hidden + ((row0 + 4 * (lane >> 4) + r) >> shift)) x[t][r] = -INFINITY;
+    }
+  }
+}
+
+// One pass over a chunk of the keys of a (sequence, kv head).  STATS: maximum and sum of each row of a group of row tiles over the
+// chunk; otherwise the weights of the chunk's keys over all rows.
+template <int D, bool STATS>
+__global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int64_t tiles, int chunk_keys) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.x % p.n_kv_heads, chunk = blockIdx.x / p.n_kv_heads, b = blockIdx.y;
+  const WeightSpace<D> ws(p.ws, tiles, p.n_kv_heads);
+  const int len = min(max(p.seq_lens[b], 0), p.bound);
+  int begin, n;
+  packed_range(p.cu_q, b, p.T_q, begin, n);
+  const int64_t first_tile = (int64_t)begin * p.group / kWeightRows + b;
+  const int shift = __builtin_ctz(p.group), first_hidden = len - n + 1;
+  const int64_t rows = (int64_t)n * p.group;
+  const int all = (int)((rows + kWeightRows - 1) / kWeightRows);
+  const int g0 = STATS ? (int)blockIdx.z * kGroupTiles : 0, g1 = STATS ? min(all, g0 + kGroupTiles) : all;
+  const int k0 = chunk * chunk_keys, k1 = min(len, k0 + chunk_keys);
+  if (STATS && g0 >= g1) return;
+  __shared__ float2 stats[4][STATS ? kGroupTiles * kWeightRows : 1];
+  if (STATS) {
+    for (int r = lane; r < (g1 - g0) * kWeightRows; r += 64) stats[wave][r] = make_float2(-INFINITY, 0.f);
+    wave_sync();
+  }
+  const int64_t record = ((int64_t)b * p.n_kv_heads + h) * p.score_stride;
+  KeyCodes<D> codes;
+  int key0 = k0 + kWeightKeys * wave;
+  if (key0 < k1) request_keys<D>(p, b, h, key0, len, lane, codes);
+  for (; key0 < k1; key0 += 4 * kWeightKeys) {
+    u32x4 k[4][D / 32];
+    f32x2 pair[4];
+    float total[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      pair[t] = codes.pair[t];
+      if (key0 + 16 * t + (lane & 15) >= len) pair[t] = f32x2{0.f, 0.f};       // (slots behind the end may hold anything)
+#pragma unroll
+      for (int ks = 0; ks < D / 32; ++ks) k[t][ks] = centred(codes.w[t][ks]);
+    }
+    if (key0 + 4 * kWeightKeys < k1) request_keys<D>(p, b, h, key0 + 4 * kWeightKeys, len, lane, codes);
+    // the first row that sees a key of the step: key0 < first_hidden + token
+    const int first_token = max(key0 - first_hidden + 1, 0);
+    for (int g = max(g0, (int)(((int64_t)first_token << shift) / kWeightRows)); g < g1; ++g) {
+      const int64_t at = (first_tile + g) * p.n_kv_heads + h;
+      const RowInfo* const info = ws.info + at * kWeightRows;
+      const int row0 = g * kWeightRows;
+      const bool masked = key0 + kWeightKeys > min(first_hidden + (row0 >> shift), len);
+      f32x4 x[4];
+      step_logits<D>(ws.limbs + at * 2 * (D / 32) * 64, k, pair, info, key0, masked, first_hidden, shift, row0, lane, x);
+      if (masked) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (key0 + 16 * t + (lane & 15) >= len) x[t] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      }
+      if constexpr (STATS) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float top = row_allmax(fmaxf(fmaxf(x[0][r], x[1][r]), fmaxf(x[2][r], x[3][r])));
+          float2* const mine = &stats[wave][(g - g0) * kWeightRows + 4 * (lane >> 4) + r];
+          const float2 old = *mine;
+          const float m = fmaxf(old.x, top), ref = m == -INFINITY ? 0.f : m;
+          const float part = row_allsum((fast_exp2(x[0][r] - ref) + fast_exp2(x[1][r] - ref)) + (fast_exp2(x[2][r] - ref) + fast_exp2(x[3][r] - ref)));
+          const float sum = fmaf(old.y, fast_exp2(old.x - ref), part);
+          wave_sync();
+          if ((lane & 15) == 0) *mine = make_float2(m, sum);
+        }
+        wave_sync();
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x2 mi = *(const f32x2*)&info[4 * (lane >> 4) + r].m;
+          const bool there = row0 + 4 * (lane >> 4) + r < rows;
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const float w = fast_exp2(x[t][r] - mi.x) * mi.y;
+            if (there) total[t] += w;
+          }
+        }
+      }
+    }
+    if constexpr (!STATS) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float w = add_xor32(add_xor16(total[t]));
+        const int key = key0 + 16 * t + lane;
+        if (lane < 16 && key < len) p.scores[record + key] = (p.prev ? p.prev[record + key] : 0.f) + w;
+      }
+    }
+  }
+  if constexpr (STATS) {
+    __syncthreads();
+    for (int r = threadIdx.x; r < (g1 - g0) * kWeightRows; r += 256) {
+      const float2 a = stats[0][r], c = stats[1][r], d = stats[2][r], e = stats[3][r];
+      const float m = fmaxf(fmaxf(a.x, c.x), fmaxf(d.x, e.x)), ref = m == -INFINITY ? 0.f : m;
+      const float sum = (a.y * fast_exp2(a.x - ref) + c.y * fast_exp2(c.x - ref)) + (d.y * fast_exp2(d.x - ref) + e.y * fast_exp2(e.x - ref));
+      const int64_t at = (first_tile + g0 + r / kWeightRows) * p.n_kv_heads + h;
+      ws.part[((int64_t)chunk * tiles * p.n_kv_heads + at) * kWeightRows + r % kWeightRows] = make_float2(m, sum);
+    }
+  }
+}
+
+// Joins the partial (maximum, sum) pairs of a row tile and head.
+template <int D>
+__global__ __launch_bounds__(64) void weight_join_kernel(PromptParams p, int64_t tiles, int chunks) {
+  const WeightSpace<D> ws(p.ws, tiles, p.n_kv_heads);
+  const int lane = threadIdx.x, r = lane & 15;
+  RowTile rt;
+  if (!find_row_tile(p, blockIdx.x, kWeightRows, lane, rt)) return;
+  const int64_t at = ((int64_t)blockIdx.x * p.n_kv_heads + blockIdx.y) * kWeightRows + r, step = tiles * p.n_kv_heads * kWeightRows;
+  float m = -INFINITY, sum = 0.f;
+  for (int c = lane >> 4; c < chunks; c += 4) {
+    const float2 v = ws.part[c * step + at];
+    const float top = fmaxf(m, v.x), ref = top == -INFINITY ? 0.f : top;
+    sum = sum * fast_exp2(m - ref) + v.y * fast_exp2(v.x - ref);
+    m = top;
+  }
+  const float top = max_xor32(max_xor16(m)), ref = top == -INFINITY ? 0.f : top;
+  sum = add_xor32(add_xor16(sum * fast_exp2(m - ref)));
+  if (lane < 16) {
+    ws.info[at].m = ref;
+    ws.info[at].inv = sum == 0.f ? 0.f : 1.f / sum;
+  }
+}
+
+static int weight_chunks(int Hkv, int B, int64_t bound) {
+  const int64_t items = (int64_t)B * Hkv;
+  int64_t s = 1024 / items;
+  const int64_t most = (bound + 4 * kWeightKeys - 1) / (4 * kWeightKeys);
+  if (s > most) s = most;
+  return s < 1 ? 1 : s > 256 ? 256 : (int)s;
+}
+
+size_t weights_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t bound) {
+  const int64_t tiles = row_tiles(T, Hq / Hkv, kWeightRows, B);
+  return 16 + (size_t)tiles * Hkv * (2 * (D / 32) * 64 * 16 + kWeightRows * (sizeof(RowInfo) + (size_t)weight_chunks(Hkv, B, bound) * 8));
+}
+
+template <int D>
+static void launch_passes(const PromptParams& p, int64_t tiles, int chunks, int chunk_keys, hipStream_t st) {
+  const int groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles);
+  if (p.T_q) {
+    weight_query_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(256), 0, st>>>(p, tiles);
+    weight_pass_kernel<D, true><<<dim3(p.n_kv_heads * chunks, p.B, groups), dim3(256), 0, st>>>(p, tiles, chunk_keys);
+    weight_join_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(64), 0, st>>>(p, tiles, chunks);
+  }
+  weight_pass_kernel<D, false><<<dim3(p.n_kv_heads * chunks, p.B), dim3(256), 0, st>>>(p, tiles, chunk_keys);
+}
+
+int launch_weights(const PromptParams& p, int D, hipStream_t st) {
+  const int64_t tiles = row_tiles(p.T_q, p.group, kWeightRows, p.B);
+  const int chunks = weight_chunks(p.n_kv_heads, p.B, p.bound), unit = 4 * kWeightKeys;
+  const int chunk_keys = (int)(((int64_t)(p.bound + chunks - 1) / chunks + unit - 1) / unit * unit);
+  if (tiles > 0x7fffffffLL || (int64_t)p.n_kv_heads * chunks > 0x7fffffffLL || (tiles + kGroupTiles - 1) / kGroupTiles > 65535) return SAW_EINVAL;
+  if (D == 128) launch_passes<128>(p, tiles, chunks, chunk_keys, st);
+  else launch_passes<64>(p, tiles, chunks, chunk_keys, st);
+  return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;
+}
+
+}  // namespace saw
