@@ -5,16 +5,78 @@ namespace saw {
 
 // Order of the scores as unsigned numbers: larger score, larger key; -0 = +0; NaN below everything.
 __device__ __forceinline__ uint32_t score_key(float f) {
-  const uint32_t u = __float_as_uint(f);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
-  if ((u & 0x7fffffffu) == 0u) return 0x80000000u;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = __float_as_uint(f + 0.f);                           // (-0 + 0 = +0)
+  const uint32_t key = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return f == f ? key : 0u;
+}
+__device__ __forceinline__ float score_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+
+constexpr int kBins = 2048, kCopies = 4, kListed = 16384, kAtOnce = 16;
+
+// The largest bin d such that the bins above it hold fewer than `want` entries, and how many are still wanted of it: by the first
+// wavefront, 32 bins a lane.  (A single thread that walked the bins took 8 us a digit.)
+__device__ __forceinline__ int bin_of(const int* hist, int d) {
+  int n = 0;
+#pragma unroll
+  for (int c = 0; c < kCopies; ++c) n += hist[d * kCopies + c];
+  return n;
+}
+__device__ __forceinline__ void pick_bin(const int* hist, int want, int lane, int (&pick)[3]) {
+  constexpr int kMine = kBins / 64;
+  int mine = 0;
+#pragma unroll 8
+  for (int i = 0; i < kMine; ++i) mine += bin_of(hist, lane * kMine + (i + lane) % kMine);
+  int upto = mine;                               // entries of this lane's bins and of all lanes' above
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_down(upto, d);
+    if (lane + d < 64) upto += v;
+  }
+  const uint64_t enough = __ballot(upto >= want);          // lanes 0 .. k
+  const int k = enough ? 63 - __builtin_clzll(enough) : 0;
+  // lane k's bins, one a lane, the highest first
+  int left = want - __shfl(upto - mine, k);
+  const int d = k * kMine + kMine - 1 - lane;
+  const int of = lane < kMine ? bin_of(hist, d) : 0;
+  int before = of;                               // of the bins down to this one
+#pragma unroll
+  for (int i = 1; i < kMine; i <<= 1) {
+    const int v = __shfl_up(before, i);
+    if (lane >= i) before += v;
+  }
+  const uint64_t reached = __ballot(lane < kMine && before >= left) | 1ull << (kMine - 1);
+  if (lane == __builtin_ctzll(reached)) {
+    pick[0] = d;
+    pick[1] = left - (before - of);
+    pick[2] = of;
+  }
 }
 
-// Kept positions of one (sequence, kv head), in ascending order: a block finds the key of the last score that is kept, 8 bits of it a
-// pass, and then hands out the places in one scan over the positions; of equal keys the lowest positions are kept.
+// f(position, score) for the positions of [j0, j1) that a thread of `threads` is given, kAtOnce loads in flight while there are as many
+template <int N, typename F>
+__device__ __forceinline__ int batch_scores(const float* s, int j, int j1, int thread, int threads, F f) {
+  for (; j + (N - 1) * threads < j1; j += N * threads) {
+    float x[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) x[u] = s[min(j + u * threads + thread, j1 - 1)];
+#pragma unroll
+    for (int u = 0; u < N; ++u) f(j + u * threads + thread, x[u]);
+  }
+  return j;
+}
+template <typename F>
+__device__ __forceinline__ void for_scores(const float* s, int j0, int j1, int thread, int threads, F f) {
+  const int j = batch_scores<kAtOnce>(s, j0, j1, thread, threads, f);
+  batch_scores<1>(s, batch_scores<4>(s, j, j1, thread, threads, f), j1, thread, threads, f);
+}
+
+// Kept positions of one (sequence, kv head), in ascending order, by one block.  The key of the last score that is kept is found 11, 11 and
+// 10 bits at a time; scores that share its first digit are listed in shared memory on the way, so that they alone are looked at for the
+// others (where more than 16384 do, all scores are read again).  Then each wavefront counts what it keeps of its share of the positions
+// and writes it behind the wavefronts in front of it; of equal keys the lowest positions are kept.
+// Bound by the latency of a single block's four readings of the scores, which stay in L2: 131072 tokens, 8 blocks on the chip.
 __global__ __launch_bounds__(1024) void evict_select_kernel(EvictParams p) {
-  const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = min(max(p.seq_lens[b], 0), p.bound);
   const int64_t row = (int64_t)b * p.n_kv_heads + h;
   const float* const s = p.scores + row * p.score_stride;
@@ -22,70 +84,101 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictParams p) {
   float* const out = p.scores_out ? p.scores_out + row * p.score_out_stride : nullptr;
   const int n = min(len, p.budget), old = max(len - p.recent, 0);
   if (h == 0 && tid == 0) p.new_lens[b] = n;
-  __shared__ int hist[256];
-  __shared__ int pick[2];                       // digit, how many of it are still wanted
-  __shared__ int sums[16][2];
-  uint32_t prefix = 0;
-  int want = n - (len - old);                   // of the old tokens
-  const bool all = len <= p.budget;
-  if (!all) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int j = tid; j < old; j += 1024) {
-        const uint32_t key = score_key(s[j]);
-        if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255], 1);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        int left = want, d = 255;
-        while (d > 0 && hist[d] < left) left -= hist[d--];
-        pick[0] = d;
-        pick[1] = left;
-      }
-      __syncthreads();
-      prefix |= (uint32_t)pick[0] << shift;
-      want = pick[1];
-      __syncthreads();
-    }
-  }
-  // `want` of the tokens whose key is `prefix` are kept, the lowest positions first
-  int done = 0, ties = 0;
-  for (int j0 = 0; j0 < len; j0 += 1024) {
-    const int j = j0 + tid;
-    bool above = false, tie = false;
-    if (j < len) {
-      if (all || j >= old) above = true;
-      else {
-        const uint32_t key = score_key(s[j]);
-        above = n > len - old && key > prefix;
-        tie = n > len - old && key == prefix;
-      }
-    }
-    const uint64_t am = __ballot(above), tm = __ballot(tie), below = (1ull << lane) - 1;
-    if (lane == 0) { sums[wave][0] = __popcll(am); sums[wave][1] = __popcll(tm); }
-    __syncthreads();
-    int t0 = ties, a0 = done, at, tt = ties;
-    for (int w = 0; w < 16; ++w) {
-      if (w < wave) { t0 += sums[w][1]; a0 += sums[w][0]; }
-      done += sums[w][0];
-      tt += sums[w][1];
-    }
-    t0 += __popcll(tm & below);
-    a0 += __popcll(am & below);
-    at = a0 + min(t0, want) - 0;
-    // (`done` counts what is above; kept ties are counted apart)
-    if (above || (tie && t0 < want)) {
-      kept[at] = j;
-      if (out) out[at] = s[j];
-    }
-    ties = tt;
-    __syncthreads();
-  }
   for (int i = n + tid; i < p.budget; i += 1024) {
     kept[i] = -1;
     if (out) out[i] = 0.f;
   }
+  if (len <= p.budget) {
+    for (int i = tid; i < len; i += 1024) {
+      kept[i] = i;
+      if (out) out[i] = s[i];
+    }
+    return;
+  }
+  __shared__ int hist[kBins * kCopies];          // (four copies, by lane: scores of like size meet in few bins)
+  __shared__ int pick[3];                       // digit, how many of it are still wanted, how many there are
+  __shared__ uint32_t listed[kListed];
+  __shared__ int count;
+  __shared__ int2 sums[16];
+  const uint64_t below = (1ull << lane) - 1;
+  uint32_t prefix = 0;
+  int want = p.budget - p.recent;               // of the tokens in front of `old`
+  int candidates = -1;                          // listed keys; -1: not listed
+  for (int digit = 0; digit < 3; ++digit) {
+    const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : kBins;
+    for (int i = tid; i < kBins * kCopies; i += 1024) hist[i] = 0;
+    if (tid == 0) count = 0;
+    __syncthreads();
+    if (digit == 0 || candidates < 0) {
+      const int above = digit == 0 ? 31 : digit == 1 ? 21 : 10;                // (bits in front of the digit; none of the first)
+      for_scores(s, 0, old, tid, 1024, [&](int j, float f) {
+        const uint32_t key = score_key(f);
+        if (j < old && (digit == 0 || key >> above == prefix >> above)) atomicAdd(&hist[((key >> shift) & (bins - 1)) * kCopies + lane % kCopies], 1);
+      });
+    } else {
+      for (int j = tid; j < candidates; j += 1024) {
+        const uint32_t key = listed[j];
+        if (digit == 1 || (key >> 10) == (prefix >> 10)) atomicAdd(&hist[((key >> shift) & (bins - 1)) * kCopies + lane % kCopies], 1);
+      }
+    }
+    __syncthreads();
+    if (wave == 0) pick_bin(hist, want, lane, pick);
+    __syncthreads();
+    prefix |= (uint32_t)pick[0] << shift;
+    want = pick[1];
+    if (digit == 0) {
+      candidates = pick[2] <= kListed ? 0 : -1;
+      if (candidates == 0) {
+        for_scores(s, 0, old, tid, 1024, [&](int j, float f) {
+          const uint32_t key = score_key(f);
+          const bool take = j < old && key >> 21 == prefix >> 21;
+          const uint64_t m = __ballot(take);
+          if (m) {                                // (one addition a wavefront)
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&count, __popcll(m));
+            at = __builtin_amdgcn_readfirstlane(at) + __popcll(m & below);
+            if (take) listed[at] = key;
+          }
+        });
+        __syncthreads();
+        candidates = count;
+      }
+    }
+    __syncthreads();
+  }
+  // `want` of the tokens whose key is `prefix` are kept, the lowest positions first.  (Compared as floats, which agrees with the keys
+  // but for NaN: if that is the last that is kept, every number is above it.)
+  const float last = score_of(prefix);
+  const bool nan = prefix == 0;
+  const int share = (len + 1023) / 1024 * 64, j0 = wave * share, j1 = min(len, j0 + share);
+  int above = 0, ties = 0;
+  for_scores(s, j0, j1, lane, 64, [&](int at, float f) {
+    above += __popcll(__ballot(at < j1 && (at >= old || (nan ? f == f : f > last))));
+    ties += __popcll(__ballot(at < j1 && at < old && (nan ? f != f : f == last)));
+  });
+  if (lane == 0) sums[wave] = make_int2(above, ties);
+  __syncthreads();
+  int done = 0, tied = 0;                        // of the wavefronts in front: kept for their key, ties
+  for (int w = 0; w < wave; ++w) { done += sums[w].x; tied += sums[w].y; }
+  for_scores(s, j0, j1, lane, 64, [&](int at, float f) {
+    const bool over = at < j1 && (at >= old || (nan ? f == f : f > last)), tie = at < j1 && at < old && (nan ? f != f : f == last);
+    const uint64_t om = __ballot(over), tm = __ballot(tie);
+    if (om | tm) {
+      int to = done + min(tied, want) + __builtin_amdgcn_mbcnt_hi((uint32_t)(om >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)om, 0));
+      bool keep = over;
+      if (tm) {
+        const int t = tied + __builtin_amdgcn_mbcnt_hi((uint32_t)(tm >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)tm, 0));
+        to += min(t, want) - min(tied, want);
+        keep = over || (tie && t < want);
+      }
+      if (keep) {
+        kept[to] = at;
+        if (out) out[to] = f;
+      }
+      done += __popcll(om);
+      tied += __popcll(tm);
+    }
+  });
 }
 
 template <int D>
