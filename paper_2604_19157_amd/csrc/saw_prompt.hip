@@ -2,6 +2,7 @@
 #include <type_traits>
 
 #include "saw_prompt_tile.h"
+#include "saw_rotate_regs.h"
 #include "saw_rotate_row.h"
 
 namespace saw {
@@ -34,8 +35,11 @@ struct RowSource {
 };
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Rotated queries for the INT4 pages: one wavefront a row of 128 channels or two heads of 64.  A row leaves as fp16 times 2^-e, its
-// largest channel in [2^14, 2^15): relative rounding 2^-11 whatever the row's size, down to 2^-39 of the largest.
+// A rotated query becomes fp16 times 2^-e with the row's largest channel in [2^14, 2^15): relative rounding 2^-11 whatever the row's
+// size, down to 2^-39 of the largest.
+__device__ __forceinline__ int query_exponent(float top) { return min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14; }
+
+// Queries under a learned rotation, whose 64 KiB a block of rows would read again: one wavefront a row.
 //   ws: [rows][D] fp16 | [rows] float 2^e
 template <int D>
 __global__ __launch_bounds__(256) void prompt_query_kernel(PromptParams p) {
@@ -55,7 +59,7 @@ __global__ __launch_bounds__(256) void prompt_query_kernel(PromptParams p) {
 #pragma unroll
   for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[lane + 64 * e]));
   top = max_xor32(max_xor16(row_allmax_positive(top)));
-  const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14;
+  const int ex = query_exponent(top);
   const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
   uint16_t* const q = p.query + row * D;
 #pragma unroll
@@ -87,6 +91,162 @@ __device__ __forceinline__ void put_piece(char* tile, int row, int piece, u32x4 
     x.w = M::pack(fmaf((float)(even >> 24), s, -sz), fmaf((float)(odd >> 24), s, -sz));
     const int chunk = 4 * piece + i;
     *(u32x4*)(tile + row * (2 * D) + 16 * (VALUE ? v_place(row, chunk) : k_place(row, chunk))) = x;
+  }
+}
+
+// The queries of a lane column as B operand: channels of k-step ks, half h and place i have bits (ks, h, i), h at bit HALF_BIT.  Those for
+// the INT4 pages are rotated here, in registers, and become fp16 times 2^-e (prompt_query_kernel does the same for a learned rotation);
+// returns what turns a logit into log2 units.
+template <int D, int KV, int HALF_BIT>
+__device__ __forceinline__ float row_query(const PromptParams& p, int64_t token, int head, int lane, u32x4 (&qf)[D / 16]) {
+  const int half = lane >> 5;
+  const bool ready = KV == kKvInt4 && p.dense_k;
+  const int64_t at = token * p.n_q_heads + head;
+  const uint16_t* const src = ready ? p.query + at * D : (const uint16_t*)p.q + token * p.q_stride + (int64_t)head * D;
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const u32x4*)(src + (spread_channel<HALF_BIT>(8 * ks) | half << HALF_BIT));
+  if constexpr (KV == kKvInt4) {
+    if (ready) return p.scale * p.query_scale[at];
+    float x[D / 2];
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (p.dtype == SAW_BF16) widen2<SAW_BF16>(qf[ks][i], x[8 * ks + 2 * i], x[8 * ks + 2 * i + 1]);
+        else widen2<SAW_F16>(qf[ks][i], x[8 * ks + 2 * i], x[8 * ks + 2 * i + 1]);
+      }
+    float top = 0.f;
+    if (p.rot_k) {
+      if (p.has_signs) sign_rows<D, HALF_BIT>(x, p.signs, lane);
+      fwht_rows<D, HALF_BIT>(x, p.had_block, lane);
+    }
+    const float norm = p.rot_k ? had_norm(p.had_block) : 1.f;
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) {
+      x[i] *= norm;
+      top = fmaxf(top, fabsf(x[i]));
+    }
+    const int ex = query_exponent(max_xor32(top));
+    const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) qf[ks][i] = MathF16::pack(x[8 * ks + 2 * i] * down, x[8 * ks + 2 * i + 1] * down);
+    return p.scale * __uint_as_float((uint32_t)(127 + ex) << 23);
+  }
+  return p.scale;
+}
+
+// The end of a wavefront's 32 rows: outputs, or partial records [split][row][D] and [split][row] (maximum, sum) where the keys are split
+// or a learned rotation has to be undone.
+template <int D, int KV, int HALF_BIT>
+__device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile& rt, int w0, int last, int row, int h, int64_t token, int head,
+                                            int k0, int len, int t0, int t1, const u32x4 (&qf)[D / 16], float scale, RowState<D>& st, int lane) {
+  constexpr bool kInt4 = KV == kKvInt4;
+  const int shift = __builtin_ctz(p.group);
+  const float sum = add_xor32(st.sum);
+  const int64_t at = token * p.n_q_heads + head;
+  // Values that are no numbers: a masked key's weight is zero, but zero times infinity is not.  Rows of a wavefront that ended with one
+  // are taken again, key by key, over the keys that each sees.
+  float odd = 0.f;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) odd = fmaf(st.o[t][r], 0.f, odd);
+  const bool split = gridDim.y > 1 || (kInt4 && p.dense_v);
+  const int64_t rows = p.T_q * p.n_q_heads;
+  float* const records = p.ws + (int64_t)blockIdx.y * rows * D;
+  float2* const ml = (float2*)(p.ws + (int64_t)gridDim.y * rows * D) + (int64_t)blockIdx.y * rows;
+  if (__any(odd != odd)) {
+    constexpr int E = D / 64;
+    const RowSource<D, KV> src = {p, rt.b, h, k0, lane};
+    for (int i = 0; i < 32 && w0 + i <= last; ++i) {
+      const int tok_i = (w0 + i) >> shift;
+      const int64_t mine = (int64_t)(rt.begin + tok_i) * p.n_q_heads + h * p.group + ((w0 + i) & (p.group - 1));
+      const int sees = p.causal ? max(min(len, len - rt.n + tok_i + 1), 0) : len;
+      const int end = min(sees, t1 * kTileKeys);
+      const float unit = __shfl(scale, i);
+      float q[E], acc[E], m = -INFINITY, den = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) { q[e] = 0.f; acc[e] = 0.f; }
+      // (channel c of row i is in register c's place of lane i or i + 32)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int c = lane + 64 * e, half = (c >> HALF_BIT) & 1, v = (c & ((1 << HALF_BIT) - 1)) | c >> (HALF_BIT + 1) << HALF_BIT;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const uint32_t w = __shfl((int)qf[ks][d], i + 32 * half), x = v & 1 ? w >> 16 : w & 0xffffu;
+            if (v >> 1 == 4 * ks + d) q[e] = (KV == kKvBf16 ? bf16_to_f32(x) : f16_to_f32(x)) * unit;
+          }
+      }
+      for (int j = t0 * kTileKeys; j < end; ++j) {
+        float k[E], v[E], x = 0.f;
+        src.load(false, j, k);
+        src.load(true, j, v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
+        x = add_xor32(add_xor16(row_allsum(x)));
+        const float top = fmaxf(m, x), ref = top == -INFINITY ? 0.f : top;
+        const float alpha = fast_exp2(m - ref), w = fast_exp2(x - ref);
+        m = top;
+        den = fmaf(den, alpha, w);
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(acc[e], alpha, w * v[e]);
+      }
+      if (split) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) records[mine * D + lane + 64 * e] = acc[e];
+        if (lane == 0) ml[mine] = make_float2(m, den);
+      } else {
+        float x[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = den == 0.f ? 0.f : acc[e] / den;
+        if (kInt4 && p.rot_v) {                                          // (lane + 64 e: bits 0 to 5 across the lanes, the last in the lane)
+          for (int st = 1; st < p.had_block && st < 64; st <<= 1)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              const float other = __shfl_xor(x[e], st);
+              x[e] = lane & st ? other - x[e] : x[e] + other;
+            }
+          if (E == 2 && p.had_block == 128) { const float a = x[0], b = x[E - 1]; x[0] = a + b; x[E - 1] = a - b; }
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = apply_sign(p.signs, lane + 64 * e, x[e] * had_norm(p.had_block));
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) store_elem(p.out, p.dtype, mine * D + lane + 64 * e, x[e]);
+      }
+    }
+    return;
+  }
+  if (split) {
+    if (row > last) return;
+    if (lane < 32) ml[at] = make_float2(st.m, sum);
+    if (sum != 0.f)
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *(f32x4*)(records + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) = f32x4{st.o[t][r], st.o[t][r + 1], st.o[t][r + 2], st.o[t][r + 3]};
+    return;
+  }
+  float inv = sum == 0.f ? 0.f : 1.f / sum;
+  float x[D / 2];
+#pragma unroll
+  for (int i = 0; i < D / 2; ++i) x[i] = st.o[i / 16][i % 16];
+  if (kInt4 && p.rot_v) {
+    fwht_rows<D, 2>(x, p.had_block, lane);                               // (accumulators: the half is bit 2 of the channel)
+    if (p.has_signs) sign_rows<D, 2>(x, p.signs, lane);
+    inv *= had_norm(p.had_block);
+  }
+  if (row > last) return;
+#pragma unroll
+  for (int i = 0; i < D / 2; i += 4) {
+    const bool bf16 = kInt4 ? p.dtype == SAW_BF16 : KV == kKvBf16;
+    *(u32x2*)((uint16_t*)p.out + at * D + spread_channel<2>(i) + 4 * (lane >> 5)) =
+        bf16 ? u32x2{MathBf16::pack(x[i] * inv, x[i + 1] * inv), MathBf16::pack(x[i + 2] * inv, x[i + 3] * inv)}
+             : u32x2{MathF16::pack(x[i] * inv, x[i + 1] * inv), MathF16::pack(x[i + 2] * inv, x[i + 3] * inv)};
   }
 }
 
@@ -124,15 +284,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
 
   const int64_t token = rt.begin + (min(row, last) >> shift);
   const int head = h * p.group + (row & (p.group - 1));
-  const int64_t at = token * p.n_q_heads + head;
   u32x4 qf[D / 16];
-  float scale = p.scale;
-  {
-    const uint16_t* const src = kInt4 ? p.query + at * D : (const uint16_t*)p.q + token * p.q_stride + (int64_t)head * D;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const u32x4*)(src + 16 * ks + 8 * (lane >> 5));
-    if (kInt4) scale *= p.query_scale[at];
-  }
+  const float scale = row_query<D, KV, 3>(p, token, head, lane, qf);
   RowState<D> st;
   st.m = -INFINITY; st.ref = 0.f; st.sum = 0.f;
 #pragma unroll
@@ -228,74 +381,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
       if (t + 1 < t1) tile_scale = put(buf ^ 1, c);
     }
   }
-  const float sum = add_xor32(st.sum);
-  // Values that are no numbers: a masked key's weight is zero, but zero times infinity is not.  Rows of a wavefront that ended with one
-  // are taken again, key by key, over the keys that each sees.
-  float odd = 0.f;
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) odd = fmaf(st.o[t][r], 0.f, odd);
-  const bool split = kInt4 || gridDim.y > 1;
-  const int64_t rows = p.T_q * p.n_q_heads;
-  float* const records = p.ws + (int64_t)blockIdx.y * rows * D;
-  float2* const ml = (float2*)(p.ws + (int64_t)gridDim.y * rows * D) + (int64_t)blockIdx.y * rows;
-  if (__any(odd != odd)) {
-    constexpr int E = D / 64;
-    const RowSource<D, KV> src = {p, rt.b, h, k0, lane};
-    for (int i = 0; i < 32 && w0 + i <= last; ++i) {
-      const int64_t tok = rt.begin + ((w0 + i) >> shift);
-      const int hd = h * p.group + ((w0 + i) & (p.group - 1));
-      const int64_t mine = tok * p.n_q_heads + hd;
-      const int end = min(sees_of(w0 + i), t1 * kTileKeys);
-      float q[E], acc[E], m = -INFINITY, den = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if constexpr (kInt4) q[e] = f16_to_f32(p.query[mine * D + lane + 64 * e]) * p.query_scale[mine] * p.scale;
-        else q[e] = load_elem(p.q, p.dtype, tok * p.q_stride + (int64_t)hd * D + lane + 64 * e) * p.scale;
-        acc[e] = 0.f;
-      }
-      for (int j = t0 * kTileKeys; j < end; ++j) {
-        float k[E], v[E], x = 0.f;
-        src.load(false, j, k);
-        src.load(true, j, v);
-#pragma unroll
-        for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
-        x = add_xor32(add_xor16(row_allsum(x)));
-        const float top = fmaxf(m, x), ref = top == -INFINITY ? 0.f : top;
-        const float alpha = fast_exp2(m - ref), w = fast_exp2(x - ref);
-        m = top;
-        den = fmaf(den, alpha, w);
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(acc[e], alpha, w * v[e]);
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (split) records[mine * D + lane + 64 * e] = acc[e];
-        else store_elem(p.out, p.dtype, mine * D + lane + 64 * e, den == 0.f ? 0.f : acc[e] / den);
-      }
-      if (split && lane == 0) ml[mine] = make_float2(m, den);
-    }
-    return;
-  }
-  if (row > last) return;
-  if (split) {
-    if (lane < 32) ml[at] = make_float2(st.m, sum);
-    if (sum != 0.f)
-#pragma unroll
-      for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *(f32x4*)(records + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) = f32x4{st.o[t][r], st.o[t][r + 1], st.o[t][r + 2], st.o[t][r + 3]};
-    return;
-  }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int r = 0; r < 16; r += 4)
-      *(u32x2*)((uint16_t*)p.out + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) =
-          u32x2{M2::pack(st.o[t][r] * inv, st.o[t][r + 1] * inv), M2::pack(st.o[t][r + 2] * inv, st.o[t][r + 3] * inv)};
+  finish_rows<D, KV, 3>(p, rt, w0, last, row, h, token, head, k0, len, t0, t1, qf, scale, st, lane);
 }
 
 // Joins the partial records of a row: one wavefront a row.
@@ -357,9 +443,9 @@ template <int D, int KV>
 static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream_t st) {
   const int64_t rows = p.T_q * p.n_q_heads;
   const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, 32 * plan.waves, p.B) * p.n_kv_heads), plan.splits), by_row((unsigned)((rows + 3) / 4)), block(256);
-  if (KV == kKvInt4) prompt_query_kernel<D><<<by_row, block, 0, st>>>(p);
+  if (KV == kKvInt4 && D == kDenseD && p.dense_k) prompt_query_kernel<D><<<by_row, block, 0, st>>>(p);
   prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
-  if (KV == kKvInt4 || plan.splits > 1) prompt_merge_kernel<D, KV == kKvInt4><<<by_row, block, 0, st>>>(p, plan.splits);
+  if (plan.splits > 1 || (KV == kKvInt4 && p.dense_v)) prompt_merge_kernel<D, KV == kKvInt4><<<by_row, block, 0, st>>>(p, plan.splits);
 }
 
 int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
