@@ -90,7 +90,7 @@ __device__ __forceinline__ void put_piece(char* tile, int row, int piece, u32x4 
     x.z = M::pack(fmaf((float)((even >> 16) & 0xff), s, -sz), fmaf((float)((odd >> 16) & 0xff), s, -sz));
     x.w = M::pack(fmaf((float)(even >> 24), s, -sz), fmaf((float)(odd >> 24), s, -sz));
     const int chunk = 4 * piece + i;
-    *(u32x4*)(tile + row * (2 * D) + 16 * (VALUE ? v_place(row, chunk) : k_place(row, chunk))) = x;
+    *(u32x4*)(tile + row * (2 * D) + 16 * (VALUE ? v_place<D>(row, chunk) : k_place<D>(row, chunk))) = x;
   }
 }
 
@@ -312,8 +312,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
         const int in = wave * (kInstr / NW) + j;                             // 1024 bytes: kRpi rows
         const int r = in * kRpi + lane / (D / 8), place = lane % (D / 8);
         const int64_t key = min(t * kTileKeys + r, len - 1);                 // (behind the end: the last key again, masked)
-        __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)(kp + key * p.k_stride + 8 * k_place(r, place)), (LDS_AS void*)(lds[buf][0] + in * 1024), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)(vp + key * p.v_stride + 8 * v_place(r, place)), (LDS_AS void*)(lds[buf][1] + in * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)(kp + key * p.k_stride + 8 * k_place<D>(r, place)), (LDS_AS void*)(lds[buf][0] + in * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const GLOBAL_AS void*)(vp + key * p.v_stride + 8 * v_place<D>(r, place)), (LDS_AS void*)(lds[buf][1] + in * 1024), 16, 0, 0);
       }
     };
     if (t0 < t1) load(0, t0);

@@ -72,11 +72,16 @@ struct MathF16 {
 
 constexpr int kTileKeys = 64;
 
-// A tile of 64 keys in shared memory: rows of D 16-bit values in 16-byte chunks, chunk c of row r at place c ^ (r & 7) for K, whose
-// operand reads take one chunk of 32 rows, and c ^ 2 (r & 3) for V, whose transposing reads take 32 bytes of four rows: without
-// either, all rows of a read would start on the same banks.
-__device__ __forceinline__ int k_place(int row, int chunk) { return chunk ^ (row & 7); }
-__device__ __forceinline__ int v_place(int row, int chunk) { return chunk ^ (2 * (row & 3)); }
+// A tile of 64 keys in shared memory: rows of D 16-bit values in 16-byte chunks, the chunks of a row exchanged so that whatever a
+// read takes at once (256 bytes a clock) lies on different banks.  K: operand reads take one chunk of 16 rows.  V: transposing reads take 32
+// bytes of four rows for each 16 lanes.  Rows of 64 channels stand two to 256 bytes.  (Exchanges that keep only 128 bytes a clock apart:
+// half of the cycles of all LDS reads were conflicts, 8192 causal tokens 550 us.)
+template <int D>
+__device__ __forceinline__ int k_place(int row, int chunk) { return chunk ^ (D == 128 ? row & 15 : (row >> 1) & 7); }
+template <int D>
+__device__ __forceinline__ int v_place(int row, int chunk) {
+  return chunk ^ (D == 128 ? 4 * (row & 3) + 2 * ((row >> 2) & 1) : 4 * ((row >> 1) & 1) + 2 * ((row >> 2) & 1));
+}
 
 // What a wavefront keeps of its 32 rows while it goes over the keys.  Products are taken transposed: S^T = K Q^T has a query per
 // lane column and 16 of 32 keys in the lane's registers, so that maximum and sum of a row are lane-local up to the other half of the
@@ -99,7 +104,7 @@ __device__ __forceinline__ void tile_logits(const char* k, const u32x4 (&qf)[D /
     const char* const at = k + row * (2 * D);
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
-      const u32x4 a = *(const u32x4*)(at + 16 * k_place(row, 2 * ks + (lane >> 5)));
+      const u32x4 a = *(const u32x4*)(at + 16 * k_place<D>(row, 2 * ks + (lane >> 5)));
       s[kb] = M1::mfma(a, qf[ks], s[kb]);
     }
   }
@@ -159,7 +164,7 @@ __device__ __forceinline__ void tile_values(const char* v, const u32x4 (&pf)[4],
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) {
       const int chunk = 4 * t + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-      const char* const at = v + (16 * ks + key) * (2 * D) + 16 * v_place(key, chunk) + 8 * (i & 1);
+      const char* const at = v + (16 * ks + key) * (2 * D) + 16 * v_place<D>(key, chunk) + 8 * (i & 1);
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(at));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(at + 8 * (2 * D)));
       const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
