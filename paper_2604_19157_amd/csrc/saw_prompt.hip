@@ -78,21 +78,29 @@ struct CodePieces {
   f32x2 key_pair;           // of key `lane` of the tile, for the tile's exponent
 };
 
-// x s - s z of 32 codes, as 16-bit values in channel order, to four places of a row
+// c s - s z of the eight codes of a word, as 16-bit values in channel order
+template <typename M>
+__device__ __forceinline__ u32x4 widen_codes(uint32_t w, float s, float sz) {
+  const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
+  u32x4 x;
+  x.x = M::pack(fmaf((float)(even & 0xff), s, -sz), fmaf((float)(odd & 0xff), s, -sz));
+  x.y = M::pack(fmaf((float)((even >> 8) & 0xff), s, -sz), fmaf((float)((odd >> 8) & 0xff), s, -sz));
+  x.z = M::pack(fmaf((float)((even >> 16) & 0xff), s, -sz), fmaf((float)((odd >> 16) & 0xff), s, -sz));
+  x.w = M::pack(fmaf((float)(even >> 24), s, -sz), fmaf((float)(odd >> 24), s, -sz));
+  return x;
+}
+// ... of 32 codes to four places of a row
 template <typename M, int D, bool VALUE>
 __device__ __forceinline__ void put_piece(char* tile, int row, int piece, u32x4 w, float s, float sz) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t even = w[i] & 0x0f0f0f0fu, odd = (w[i] >> 4) & 0x0f0f0f0fu;
-    u32x4 x;
-    x.x = M::pack(fmaf((float)(even & 0xff), s, -sz), fmaf((float)(odd & 0xff), s, -sz));
-    x.y = M::pack(fmaf((float)((even >> 8) & 0xff), s, -sz), fmaf((float)((odd >> 8) & 0xff), s, -sz));
-    x.z = M::pack(fmaf((float)((even >> 16) & 0xff), s, -sz), fmaf((float)((odd >> 16) & 0xff), s, -sz));
-    x.w = M::pack(fmaf((float)(even >> 24), s, -sz), fmaf((float)(odd >> 24), s, -sz));
     const int chunk = 4 * piece + i;
-    *(u32x4*)(tile + row * (2 * D) + 16 * (VALUE ? v_place<D>(row, chunk) : k_place<D>(row, chunk))) = x;
+    *(u32x4*)(tile + row * (2 * D) + 16 * (VALUE ? v_place<D>(row, chunk) : k_place<D>(row, chunk))) = widen_codes<M>(w[i], s, sz);
   }
 }
+
+// The power of two that a tile's keys are divided by: the largest lands just below 2^15.
+__device__ __forceinline__ int key_exponent(float top) { return max((int)(__float_as_uint(top) >> 23) - 127, -100) - 14; }
 
 // The queries of a lane column as B operand: channels of k-step ks, half h and place i have bits (ks, h, i), h at bit HALF_BIT.  Those for
 // the INT4 pages are rotated here, in registers, and become fp16 times 2^-e (prompt_query_kernel does the same for a learned rotation);
@@ -223,12 +231,11 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
   if (split) {
     if (row > last) return;
     if (lane < 32) ml[at] = make_float2(st.m, sum);
-    if (sum != 0.f)
 #pragma unroll
-      for (int t = 0; t < D / 32; ++t)
+    for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *(f32x4*)(records + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) = f32x4{st.o[t][r], st.o[t][r + 1], st.o[t][r + 2], st.o[t][r + 3]};
+      for (int r = 0; r < 16; r += 4)
+        *(f32x4*)(records + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) = f32x4{st.o[t][r], st.o[t][r + 1], st.o[t][r + 2], st.o[t][r + 3]};
     return;
   }
   float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -328,35 +335,26 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
     using Pieces = CodePieces<D, NW>;
     const int32_t* const pages = p.page_table + (int64_t)rt.b * p.max_pages;
     const int threads = 64 * NW;
-    // (a tile is four pages; ids of pages behind the sequence's last are not looked at)
-    auto vector_of = [&](const int (&page)[4], int key) {                    // of a key of the tile
-      const int i = key >> 4, id = i == 0 ? page[0] : i == 1 ? page[1] : i == 2 ? page[2] : page[3];
-      return ((int64_t)id * p.n_kv_heads + h) * 16 + (key & 15);
-    };
+    TilePages ids;
     auto request = [&](int t, Pieces& c) {
-      int page[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        page[i] = pages[min(4 * t + i, (len - 1) >> 4)];
-        if (page[i] < 0 || page[i] >= p.num_pages) page[i] = 0;
-      }
+      ids.ready(p);
 #pragma unroll
       for (int j = 0; j < Pieces::kEach; ++j) {
         const int piece = j * threads + threadIdx.x, value = piece >= Pieces::kPieces / 2, i = value ? piece - Pieces::kPieces / 2 : piece;
         const int key = i / (D / 32);
-        const int64_t vec = vector_of(page, key);
+        const int64_t vec = ids.vector_of(p, h, key);
         c.codes[j] = ((const u32x4*)((value ? p.v_codes : p.k_codes) + vec * (D / 2)))[i % (D / 32)];
         c.pair[j] = ((const f32x2*)(value ? p.v_meta : p.k_meta))[vec];
         if (t * kTileKeys + key >= len) c.pair[j] = f32x2{0.f, 0.f};         // (slots behind the end may hold anything)
       }
-      c.key_pair = ((const f32x2*)p.k_meta)[vector_of(page, lane)];
+      c.key_pair = ((const f32x2*)p.k_meta)[ids.vector_of(p, h, lane)];
       if (t * kTileKeys + lane >= len) c.key_pair = f32x2{0.f, 0.f};
     };
     auto put = [&](int buf, const Pieces& c) {                               // returns the tile's power of two
       float top = fmaxf(fabsf(c.key_pair.x * c.key_pair.y), fabsf(c.key_pair.x * (15.f - c.key_pair.y)));
       if (!(top < INFINITY)) top = 0.f;
       top = max_xor32(max_xor16(row_allmax_positive(top)));
-      const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -100) - 14;
+      const int ex = key_exponent(top);
       const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
 #pragma unroll
       for (int j = 0; j < Pieces::kEach; ++j) {
@@ -370,19 +368,157 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
     Pieces c;
     float tile_scale = 1.f;
     if (t0 < t1) {
+      ids.fetch(pages, t0, len);
       request(t0, c);
+      ids.fetch(pages, t0 + 1, len);
       tile_scale = put(0, c);
     }
     for (int t = t0; t < t1; ++t) {
       const int buf = (t - t0) & 1;
       lds_barrier();
-      if (t + 1 < t1) request(t + 1, c);
+      if (t + 1 < t1) {
+        request(t + 1, c);
+        ids.fetch(pages, t + 2, len);
+      }
       products(buf, t, scale * tile_scale);
       if (t + 1 < t1) tile_scale = put(buf ^ 1, c);
     }
   }
   finish_rows<D, KV, 3>(p, rt, w0, last, row, h, token, head, k0, len, t0, t1, qf, scale, st, lane);
 }
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// Few rows over the INT4 pages (draft tokens to verify, a decode step's queries): a block takes 32 rows, and its wavefronts share out the
+// keys, every fourth tile each, so that none waits for another until they join their states at the end.  Keys go from memory to operand
+// registers - a lane holds one half of one key's channels, which the queries' k-steps follow -, values through 64 rows of shared
+// memory of the wavefront's own for the transposing reads.
+template <int D>
+__global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
+  constexpr int NW = 4, kRow = 2 * D, kTile = kTileKeys * kRow, kHalfBit = D == 128 ? 6 : 5, kWords = D / 16, kPieces = D / 32;
+  static_assert(kTile == 64 * (D / 2) * 4, "a state fits the wavefront's tile");
+  __shared__ __attribute__((aligned(1024))) char lds[NW][kTile];
+  __shared__ float2 join[NW][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.x % p.n_kv_heads;
+  RowTile rt;
+  if (!find_row_tile(p, blockIdx.x / p.n_kv_heads, 32, lane, rt)) return;
+  const int len = min(max(p.seq_lens[rt.b], 0), p.bound);
+  const int shift = __builtin_ctz(p.group);
+  const int last = rt.row0 + rt.rows - 1, row = rt.row0 + (lane & 31);
+  auto sees_of = [&](int r) { return max(min(len, len - rt.n + (r >> shift) + 1), 0); };
+  const int sees = row <= last ? sees_of(row) : 0, kend = sees_of(last), kfull = rt.rows == 32 ? sees_of(rt.row0) : 0;
+  const int nt = (kend + kTileKeys - 1) / kTileKeys, per = (nt + (int)gridDim.y - 1) / (int)gridDim.y;
+  const int t0 = (int)blockIdx.y * per, t1 = min(nt, t0 + per);
+  const int64_t token = rt.begin + (min(row, last) >> shift);
+  const int head = h * p.group + (row & (p.group - 1));
+  const int32_t* const pages = p.page_table + (int64_t)rt.b * p.max_pages;
+  char* const mine = lds[wave];
+
+  u32x4 kc[2][kWords / 4], vc[kPieces];
+  f32x2 kpair[2], vpair[kPieces];
+  TilePages ids;
+  auto request = [&] {
+    ids.ready(p);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int64_t vec = ids.vector_of(p, h, 32 * kb + (lane & 31));
+      const u32x4* const src = (const u32x4*)(p.k_codes + vec * (D / 2) + (lane >> 5) * (D / 4));
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i) kc[kb][i] = src[i];
+      kpair[kb] = ((const f32x2*)p.k_meta)[vec];
+    }
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int piece = 64 * j + lane;
+      const int64_t vec = ids.vector_of(p, h, piece / kPieces);
+      vc[j] = ((const u32x4*)(p.v_codes + vec * (D / 2)))[piece % kPieces];
+      vpair[j] = ((const f32x2*)p.v_meta)[vec];
+    }
+  };
+  if (t0 + wave < t1) {
+    ids.fetch(pages, t0 + wave, len);
+    request();
+    ids.fetch(pages, t0 + wave + NW, len);
+  }
+  u32x4 qf[D / 16];
+  const float scale = row_query<D, kKvInt4, kHalfBit>(p, token, head, lane, qf);
+  RowState<D> st;
+  st.m = -INFINITY; st.ref = 0.f; st.sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st.o[t][r] = 0.f;
+
+  for (int t = t0 + wave; t < t1; t += NW) {
+    // (slots behind the end may hold anything)
+    float top = 0.f, s[2], sz[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const bool there = t * kTileKeys + 32 * kb + (lane & 31) < len;
+      s[kb] = there ? kpair[kb].x : 0.f;
+      sz[kb] = there ? kpair[kb].x * kpair[kb].y : 0.f;
+      const float most = fmaxf(fabsf(sz[kb]), fabsf(fmaf(15.f, s[kb], -sz[kb])));
+      if (most < INFINITY) top = fmaxf(top, most);
+    }
+    const int ex = key_exponent(max_xor16(row_allmax_positive(top)));
+    const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+    f32x16 x[2];
+    u32x4 pf[4];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[kb][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) x[kb] = MathF16::mfma(widen_codes<MathF16>(kc[kb][ks / 4][ks % 4], s[kb] * down, sz[kb] * down), qf[ks], x[kb]);
+    }
+    wave_sync();
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int key = (64 * j + lane) / kPieces;
+      const bool there = t * kTileKeys + key < len;
+      put_piece<MathBf16, D, true>(mine, key, lane % kPieces, vc[j], there ? vpair[j].x : 0.f, there ? vpair[j].x * vpair[j].y : 0.f);
+    }
+    wave_sync();
+    if (t + NW < t1) {
+      request();
+      ids.fetch(pages, t + 2 * NW, len);
+    }
+    if ((t + 1) * kTileKeys > kfull) tile_mask(x, sees - t * kTileKeys, lane);
+    tile_weights<D, MathBf16>(x, scale * __uint_as_float((uint32_t)(127 + ex) << 23), st, pf);
+    tile_values<D, MathBf16>(mine, pf, st, lane);
+  }
+  // the other wavefronts' states join the first's
+  wave_sync();
+  if (wave > 0) {
+#pragma unroll
+    for (int i = 0; i < D / 2; i += 4) *(f32x4*)(mine + i * 256 + 16 * lane) = f32x4{st.o[i / 16][i % 16], st.o[i / 16][i % 16 + 1], st.o[i / 16][i % 16 + 2], st.o[i / 16][i % 16 + 3]};
+    join[wave][lane] = make_float2(st.m, st.sum);
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  float m = st.m;
+#pragma unroll
+  for (int w = 1; w < NW; ++w) m = fmaxf(m, join[w][lane].x);
+  const float ref = m == -INFINITY ? 0.f : m;
+  const float alpha = fast_exp2(st.m - ref);
+  st.sum *= alpha;
+#pragma unroll
+  for (int i = 0; i < D / 2; ++i) st.o[i / 16][i % 16] *= alpha;
+  for (int w = 1; w < NW; ++w) {
+    const float a = fast_exp2(join[w][lane].x - ref);
+    st.sum = fmaf(a, join[w][lane].y, st.sum);
+#pragma unroll
+    for (int i = 0; i < D / 2; i += 4) {
+      const f32x4 o = *(const f32x4*)(lds[w] + i * 256 + 16 * lane);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) st.o[i / 16][i % 16 + k] = fmaf(a, o[k], st.o[i / 16][i % 16 + k]);
+    }
+  }
+  st.m = m;
+  finish_rows<D, kKvInt4, kHalfBit>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, qf, scale, st, lane);
+}
+
+constexpr int kMaxKeySplits = 64;
 
 // Joins the partial records of a row: one wavefront a row.
 template <int D, bool INT4>
@@ -396,20 +532,28 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int s
   const int b = last_not_above(p.B, token, lane, [&](int i) { return clamped_offset(p.cu_q, i, p.T_q); });
   if (b < 0 || token >= clamped_offset(p.cu_q, b + 1, p.T_q)) return;
   const float2* const ml = (const float2*)(p.ws + (int64_t)splits * rows * D);
-  float m = -INFINITY;
-  for (int s = lane; s < splits; s += 64) m = fmaxf(m, ml[s * rows + row].x);
-  m = max_xor32(max_xor16(row_allmax(m)));
-  const float ref = m == -INFINITY ? 0.f : m;
-  float den = 0.f, o[E];
+  float2 mine = make_float2(-INFINITY, 0.f);                              // (a split a lane: kMaxKeySplits of them)
+  if (lane < splits) mine = ml[lane * rows + row];
+  const float m = max_xor32(max_xor16(row_allmax(mine.x)));
+  const float weight = fast_exp2(mine.x - (m == -INFINITY ? 0.f : m));
+  const float den = add_xor32(add_xor16(row_allsum(weight * mine.y)));
+  float o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int s = 0; s < splits; ++s) {
-    const float2 r = ml[s * rows + row];
-    if (r.y == 0.f) continue;                                             // (nothing seen there: no values were written)
-    const float w = fast_exp2(r.x - ref);
-    den = fmaf(w, r.y, den);
+  constexpr int kAhead = 8;                                               // records on their way at once
+  for (int s0 = 0; s0 < splits; s0 += kAhead) {
+    float v[kAhead][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(w, p.ws[(s * rows + row) * D + E * lane + e], o[e]);
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = p.ws[(min(s0 + k, splits - 1) * rows + row) * D + E * lane + e];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), min(s0 + k, splits - 1)));
+      if (s0 + k < splits)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(w, v[k][e], o[e]);
+    }
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = den == 0.f ? 0.f : o[e] / den;
@@ -427,14 +571,16 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int s
   for (int e = 0; e < E; ++e) store_elem(p.out, p.dtype, row * D + E * lane + e, o[e]);
 }
 
-// How a call is handed out: wavefronts of a block and splits of the keys.
-struct PromptPlan { int waves, splits; };
-static PromptPlan prompt_plan(int G, int Hkv, int64_t T, int B, int64_t max_k_len) {
-  PromptPlan r = {4, 1};
-  const int64_t blocks = row_tiles(T, G, 32 * r.waves, B) * Hkv;
-  int64_t s = 512 / blocks, most = (max_k_len + 255) / 256;
+// How a call is handed out: rows of a block, wavefronts of it, splits of the keys.
+struct PromptPlan { int rows, waves, splits; };
+static PromptPlan prompt_plan(bool int4, int G, int Hkv, int64_t T, int B, int64_t max_k_len) {
+  PromptPlan r = {128, 4, 1};
+  int64_t want = 512;
+  if (int4 && T * G <= 64 * (int64_t)B) { r.rows = 32; want = 1280; }
+  const int64_t blocks = row_tiles(T, G, r.rows, B) * Hkv;
+  int64_t s = want / blocks, most = (max_k_len + 255) / 256;
   if (s > most) s = most;
-  r.splits = s < 1 ? 1 : s > 64 ? 64 : (int)s;
+  r.splits = s < 1 ? 1 : s > kMaxKeySplits ? kMaxKeySplits : (int)s;
   return r;
 }
 static size_t record_bytes(int D, int64_t rows, int splits) { return (size_t)rows * splits * (D + 2) * 4; }
@@ -442,16 +588,17 @@ static size_t record_bytes(int D, int64_t rows, int splits) { return (size_t)row
 template <int D, int KV>
 static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream_t st) {
   const int64_t rows = p.T_q * p.n_q_heads;
-  const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, 32 * plan.waves, p.B) * p.n_kv_heads), plan.splits), by_row((unsigned)((rows + 3) / 4)), block(256);
+  const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads), plan.splits), by_row((unsigned)((rows + 3) / 4)), block(256);
   if (KV == kKvInt4 && D == kDenseD && p.dense_k) prompt_query_kernel<D><<<by_row, block, 0, st>>>(p);
-  prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
+  if (plan.rows == 32) few_rows_kernel<D><<<grid, block, 0, st>>>(p);
+  else prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
   if (plan.splits > 1 || (KV == kKvInt4 && p.dense_v)) prompt_merge_kernel<D, KV == kKvInt4><<<by_row, block, 0, st>>>(p, plan.splits);
 }
 
 int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
   const int64_t rows = p.T_q * p.n_q_heads;
-  const PromptPlan plan = prompt_plan(p.group, p.n_kv_heads, p.T_q, p.B, p.bound);
-  if (row_tiles(p.T_q, p.group, 32 * plan.waves, p.B) * p.n_kv_heads > 0x7fffffffLL || rows / 4 >= 0x7fffffffLL) return SAW_EINVAL;
+  const PromptPlan plan = prompt_plan(int4, p.group, p.n_kv_heads, p.T_q, p.B, p.bound);
+  if (row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads > 0x7fffffffLL || rows / 4 >= 0x7fffffffLL) return SAW_EINVAL;
   if (int4) {
     // (behind the records: rows of D + 2 floats)
     p.query_scale = p.ws + ((D + 2) * rows * plan.splits + 3) / 4 * 4;
@@ -469,12 +616,13 @@ int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
 }
 
 size_t prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len) {
-  const PromptPlan plan = prompt_plan(Hq / Hkv, Hkv, T, B, max_k_len);
+  const PromptPlan plan = prompt_plan(false, Hq / Hkv, Hkv, T, B, max_k_len);
   return 16 + (plan.splits > 1 ? record_bytes(D, T * Hq, plan.splits) : 0);
 }
 size_t paged_prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len) {
-  const PromptPlan plan = prompt_plan(Hq / Hkv, Hkv, T, B, max_k_len);
+  const PromptPlan plan = prompt_plan(true, Hq / Hkv, Hkv, T, B, max_k_len);
   const int64_t rows = T * Hq;
   return 32 + record_bytes(D, rows, plan.splits) + (size_t)(rows + 3) / 4 * 16 + (size_t)rows * D * 2;
 }
+
 }  // namespace saw

@@ -72,6 +72,28 @@ struct MathF16 {
 
 constexpr int kTileKeys = 64;
 
+// Ids of the four pages of a tile of 64 keys, fetched a tile ahead of the keys, which cannot be requested without them.  Pages behind the
+// sequence's last are not looked at (the last again); ids out of range are page 0.  (A vector load whose lanes are read out at the use:
+// scalar loads on their way make every wait for shared memory a wait for them as well, few rows 58 -> 70 us.)
+struct TilePages {
+  int ahead;
+  __device__ __forceinline__ void fetch(const int32_t* pages, int tile, int len) { ahead = pages[min(4 * tile + (int)(threadIdx.x & 3), (len - 1) >> 4)]; }
+  __device__ __forceinline__ void ready(const PromptParams& p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      id[i] = __builtin_amdgcn_readlane(ahead, i);
+      if (id[i] < 0 || id[i] >= p.num_pages) id[i] = 0;
+    }
+  }
+  int id[4];
+  // vector of key `key` of the tile in the pools of kv head h
+  __device__ __forceinline__ int64_t vector_of(const PromptParams& p, int h, int key) const {
+    const int i = key >> 4;
+    const int page = i == 0 ? id[0] : i == 1 ? id[1] : i == 2 ? id[2] : id[3];
+    return ((int64_t)page * p.n_kv_heads + h) * 16 + (key & 15);
+  }
+};
+
 // A tile of 64 keys in shared memory: rows of D 16-bit values in 16-byte chunks, the chunks of a row exchanged so that whatever a
 // read takes at once (256 bytes a clock) lies on different banks.  K: operand reads take one chunk of 16 rows.  V: transposing reads take 32
 // bytes of four rows for each 16 lanes.  Rows of 64 channels stand two to 256 bytes.  (Exchanges that keep only 128 bytes a clock apart:

@@ -38,45 +38,49 @@ struct WeightSpace {
   }
 };
 
-// Rotated queries of a row tile as operand registers: a wavefront per four rows.
+// One row of a tile: rotated, scaled to its largest channel in [2^14, 2^15), split into two fp16 limbs at its place among the operand
+// registers; returns (2^e, sum of its channels as the limbs hold them).  By one wavefront; x: 128 floats of its own.
 template <int D>
-__global__ __launch_bounds__(256) void weight_query_kernel(PromptParams p, int64_t tiles) {
+__device__ __forceinline__ f32x2 put_query_row(const PromptParams& p, int64_t token, int head, float* x, uint16_t* limbs, int r, int lane) {
   constexpr int E = D / 64;
-  __shared__ __attribute__((aligned(16))) float rows[4][128];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y;
+  const int64_t src = token * p.q_stride + (int64_t)head * D;
+  if (E == 1) x[lane + 64] = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[lane + 64 * e] = load_elem(p.q, p.dtype, src + lane + 64 * e);
+  wave_sync();
+  rotate_row(p, x, D, lane);
+  float top = 0.f, total = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[lane + 64 * e] * p.scale));
+  top = max_xor32(max_xor16(row_allmax_positive(top)));
+  const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14;
+  const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int c = lane + 64 * e, quarter = c / (D / 4), ks = c % (D / 4) / 8, i = 2 * (c % 4) + (c / 4) % 2;
+    const float v = x[c] * p.scale * down;
+    const uint16_t hi = f32_to_f16(v), lo = f32_to_f16(v - f16_to_f32(hi));
+    total += f16_to_f32(hi) + f16_to_f32(lo);
+    limbs[(ks * 64 + 16 * quarter + r) * 8 + i] = hi;
+    limbs[((D / 32 + ks) * 64 + 16 * quarter + r) * 8 + i] = lo;
+  }
+  total = add_xor32(add_xor16(row_allsum(total)));
+  wave_sync();
+  return f32x2{__uint_as_float((uint32_t)(127 + ex) << 23), total};
+}
+
+// Rotated queries of a row tile as operand registers: a wavefront a row.
+template <int D>
+__global__ __launch_bounds__(1024) void weight_query_kernel(PromptParams p, int64_t tiles) {
+  __shared__ __attribute__((aligned(16))) float rows[kWeightRows][128];
+  const int lane = threadIdx.x & 63, r = threadIdx.x >> 6, h = blockIdx.y;
   const WeightSpace<D> ws(p.ws, tiles, p.n_kv_heads);
   RowTile rt;
   if (!find_row_tile(p, blockIdx.x, kWeightRows, lane, rt)) return;
   const int64_t at = (int64_t)blockIdx.x * p.n_kv_heads + h;
-  uint16_t* const limbs = (uint16_t*)(ws.limbs + at * 2 * (D / 32) * 64);
-  float* const x = rows[wave];
-  for (int k = 0; k < 4; ++k) {
-    const int r = 4 * wave + k, row = rt.row0 + min(r, rt.rows - 1);        // (rows behind the last: the last again, never looked at)
-    const int64_t src = (rt.begin + row / p.group) * p.q_stride + (int64_t)(h * p.group + row % p.group) * D;
-    if (E == 1) x[lane + 64] = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[lane + 64 * e] = load_elem(p.q, p.dtype, src + lane + 64 * e);
-    wave_sync();
-    rotate_row(p, x, D, lane);
-    float top = 0.f, total = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[lane + 64 * e] * p.scale));
-    top = max_xor32(max_xor16(row_allmax_positive(top)));
-    const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14;
-    const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = lane + 64 * e, quarter = c / (D / 4), ks = c % (D / 4) / 8, i = 2 * (c % 4) + (c / 4) % 2;
-      const float v = x[c] * p.scale * down;
-      const uint16_t hi = f32_to_f16(v), lo = f32_to_f16(v - f16_to_f32(hi));
-      total += f16_to_f32(hi) + f16_to_f32(lo);
-      limbs[(ks * 64 + 16 * quarter + r) * 8 + i] = hi;
-      limbs[((D / 32 + ks) * 64 + 16 * quarter + r) * 8 + i] = lo;
-    }
-    total = add_xor32(add_xor16(row_allsum(total)));
-    if (lane == 0) ws.info[at * kWeightRows + r] = RowInfo{__uint_as_float((uint32_t)(127 + ex) << 23), total, 0.f, 0.f};
-    wave_sync();
-  }
+  const int row = rt.row0 + min(r, rt.rows - 1);                          // (rows behind the last: the last again, never looked at)
+  const f32x2 v = put_query_row<D>(p, rt.begin + row / p.group, h * p.group + row % p.group, rows[r], (uint16_t*)(ws.limbs + at * 2 * (D / 32) * 64), r, lane);
+  if (lane == 0) ws.info[at * kWeightRows + r] = RowInfo{v.x, v.y, 0.f, 0.f};
 }
 
 // A wavefront's keys of one step as they come from memory: key 16 t + lane % 16, quarter lane / 16 of its codes.
@@ -86,13 +90,11 @@ struct KeyCodes {
   f32x2 pair[4];
 };
 template <int D>
-__device__ __forceinline__ void request_keys(const PromptParams& p, int b, int h, int key0, int len, int lane, KeyCodes<D>& k) {
-  const int32_t* const pages = p.page_table + (int64_t)b * p.max_pages;
+__device__ __forceinline__ void request_keys(const PromptParams& p, TilePages& ids, int h, int lane, KeyCodes<D>& k) {
+  ids.ready(p);
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    int page = pages[min((key0 >> 4) + t, (len - 1) >> 4)];
-    if (page < 0 || page >= p.num_pages) page = 0;
-    const int64_t vec = ((int64_t)page * p.n_kv_heads + h) * 16 + (lane & 15);
+    const int64_t vec = ids.vector_of(p, h, 16 * t + (lane & 15));
     const uint8_t* const src = p.k_codes + vec * (D / 2) + (lane >> 4) * (D / 8);
     if constexpr (D == 128) {
       const u32x4 x = *(const u32x4*)src;
@@ -106,6 +108,39 @@ __device__ __forceinline__ void request_keys(const PromptParams& p, int b, int h
     k.pair[t] = ((const f32x2*)p.k_meta)[vec];
   }
 }
+// A wavefront's steps, every `stride` keys: two of them on their way while a third is worked on, page ids one further ahead.
+template <int D>
+struct KeyStream {
+  KeyCodes<D> codes[2];
+  TilePages ids;
+  const int32_t* pages;
+  int end, stride, len;
+  __device__ __forceinline__ void start(const PromptParams& p, int h, int key0, int lane) {
+    if (key0 >= end) return;
+    ids.fetch(pages, key0 / kWeightKeys, len);
+    request_keys<D>(p, ids, h, lane, codes[0]);
+    ids.fetch(pages, (key0 + stride) / kWeightKeys, len);
+    if (key0 + stride < end) request_keys<D>(p, ids, h, lane, codes[1]);
+    ids.fetch(pages, (key0 + 2 * stride) / kWeightKeys, len);
+  }
+  // behind the use of a slot at key0: what comes two steps later
+  __device__ __forceinline__ void next(const PromptParams& p, int h, int key0, int lane, KeyCodes<D>& slot) {
+    if (key0 + 2 * stride >= end) return;
+    request_keys<D>(p, ids, h, lane, slot);
+    ids.fetch(pages, (key0 + 3 * stride) / kWeightKeys, len);
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(int key0, F step) {
+    while (key0 < end) {
+      step(key0, codes[0]);
+      key0 += stride;
+      if (key0 >= end) break;
+      step(key0, codes[1]);
+      key0 += stride;
+    }
+  }
+};
+
 // codes - 8 of a word, in the order 0 4 1 5 2 6 3 7: 0x6400 + c is 1024 + c
 __device__ __forceinline__ u32x4 centred(uint32_t w) {
   u32x4 r;
@@ -116,37 +151,57 @@ __device__ __forceinline__ u32x4 centred(uint32_t w) {
   return r;
 }
 
-// Logits of 16 rows and 64 keys: x[t][r] of row 4 (lane / 16) + r and key 16 t + lane % 16, in log2 units; hidden ones -infinity.
+// A row tile in a wavefront's registers.
 template <int D>
-__device__ __forceinline__ void step_logits(const u32x4* limbs, const u32x4 (&k)[4][D / 32], const f32x2 (&pair)[4], const RowInfo* info, int key0,
-                                            bool masked, int first_hidden, int shift, int row0, int lane, f32x4 (&x)[4]) {
+struct TileQueries {
   u32x4 q[2][D / 32];
+  float scale[4], sum_q[4];       // of rows 4 (lane / 16) + 0..3
+  __device__ __forceinline__ void load(const u32x4* limbs, const RowInfo* info, int lane) {
 #pragma unroll
-  for (int l = 0; l < 2; ++l)
+    for (int l = 0; l < 2; ++l)
 #pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) q[l][ks] = limbs[(l * (D / 32) + ks) * 64 + lane];
-  float scale[4], sum_q[4];
+      for (int ks = 0; ks < D / 32; ++ks) q[l][ks] = limbs[(l * (D / 32) + ks) * 64 + lane];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const f32x2 v = *(const f32x2*)&info[4 * (lane >> 4) + r].scale;
-    scale[r] = v.x;
-    sum_q[r] = v.y;
+    for (int r = 0; r < 4; ++r) {
+      const f32x2 v = *(const f32x2*)&info[4 * (lane >> 4) + r].scale;
+      scale[r] = v.x;
+      sum_q[r] = v.y;
+    }
   }
+};
+
+// Logits of 16 rows and 64 keys: x[t][r] of row 4 (lane / 16) + r and key 16 t + lane % 16, in log2 units; hidden ones and those behind the
+// sequence's end -infinity.
+template <int D>
+__device__ __forceinline__ void step_logits(const TileQueries<D>& tq, const u32x4 (&k)[4][D / 32], const f32x2 (&pair)[4], int key0, int len,
+                                            bool masked, int first_hidden, int shift, int row0, int lane, f32x4 (&x)[4]) {
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int l = 1; l >= 0; --l)
 #pragma unroll
-      for (int ks = 0; ks < D / 32; ++ks) s = mfma16(q[l][ks], k[t][ks], s);
+      for (int ks = 0; ks < D / 32; ++ks) s = mfma16(tq.q[l][ks], k[t][ks], s);
     const float z8 = pair[t].y - 8.f;
     const int key = key0 + 16 * t + (lane & 15);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      x[t][r] = fmaf(-z8, sum_q[r], s[r]) * pair[t].x * scale[r];
+      x[t][r] = fmaf(-z8, tq.sum_q[r], s[r]) * pair[t].x * tq.scale[r];
       // (row i sees the keys in front of first_hidden + its token)
-      if (masked && key >= first_hidden + ((row0 + 4 * (lane >> 4) + r) >> shift)) x[t][r] = -INFINITY;
+      if (masked && (key >= len || key >= first_hidden + ((row0 + 4 * (lane >> 4) + r) >> shift))) x[t][r] = -INFINITY;
     }
+  }
+}
+
+// A step's codes as operand registers; pairs of slots behind the end, which may hold anything, become zero.
+template <int D>
+__device__ __forceinline__ void take_keys(const KeyCodes<D>& codes, int key0, int len, int lane, u32x4 (&k)[4][D / 32], f32x2 (&pair)[4]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    pair[t] = codes.pair[t];
+    if (key0 + 16 * t + (lane & 15) >= len) pair[t] = f32x2{0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) k[t][ks] = centred(codes.w[t][ks]);
   }
 }
 
@@ -173,21 +228,18 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
     wave_sync();
   }
   const int64_t record = ((int64_t)b * p.n_kv_heads + h) * p.score_stride;
-  KeyCodes<D> codes;
-  int key0 = k0 + kWeightKeys * wave;
-  if (key0 < k1) request_keys<D>(p, b, h, key0, len, lane, codes);
-  for (; key0 < k1; key0 += 4 * kWeightKeys) {
+  TileQueries<D> tq;
+  int held = -1;                // the row tile in tq: a single one is loaded once
+  KeyStream<D> keys;
+  keys.pages = p.page_table + (int64_t)b * p.max_pages;
+  keys.end = k1; keys.stride = 4 * kWeightKeys; keys.len = len;
+  keys.start(p, h, k0 + kWeightKeys * wave, lane);
+  keys.each(k0 + kWeightKeys * wave, [&](int key0, KeyCodes<D>& codes) {
     u32x4 k[4][D / 32];
     f32x2 pair[4];
     float total[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      pair[t] = codes.pair[t];
-      if (key0 + 16 * t + (lane & 15) >= len) pair[t] = f32x2{0.f, 0.f};       // (slots behind the end may hold anything)
-#pragma unroll
-      for (int ks = 0; ks < D / 32; ++ks) k[t][ks] = centred(codes.w[t][ks]);
-    }
-    if (key0 + 4 * kWeightKeys < k1) request_keys<D>(p, b, h, key0 + 4 * kWeightKeys, len, lane, codes);
+    take_keys<D>(codes, key0, len, lane, k, pair);
+    keys.next(p, h, key0, lane, codes);
     // the first row that sees a key of the step: key0 < first_hidden + token
     const int first_token = max(key0 - first_hidden + 1, 0);
     for (int g = max(g0, (int)(((int64_t)first_token << shift) / kWeightRows)); g < g1; ++g) {
@@ -196,12 +248,9 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
       const int row0 = g * kWeightRows;
       const bool masked = key0 + kWeightKeys > min(first_hidden + (row0 >> shift), len);
       f32x4 x[4];
-      step_logits<D>(ws.limbs + at * 2 * (D / 32) * 64, k, pair, info, key0, masked, first_hidden, shift, row0, lane, x);
-      if (masked) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (key0 + 16 * t + (lane & 15) >= len) x[t] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      }
+      if (g != held) tq.load(ws.limbs + at * 2 * (D / 32) * 64, info, lane);
+      held = g;
+      step_logits<D>(tq, k, pair, key0, len, masked, first_hidden, shift, row0, lane, x);
       if constexpr (STATS) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -236,7 +285,7 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
         if (lane < 16 && key < len) p.scores[record + key] = (p.prev ? p.prev[record + key] : 0.f) + w;
       }
     }
-  }
+  });
   if constexpr (STATS) {
     __syncthreads();
     for (int r = threadIdx.x; r < (g1 - g0) * kWeightRows; r += 256) {
@@ -272,9 +321,136 @@ __global__ __launch_bounds__(64) void weight_join_kernel(PromptParams p, int64_t
   }
 }
 
+// Statistics and weights in one launch, for batches of few rows a sequence that fill the chip by themselves (a decode step): a block takes
+// a (sequence, kv head), reads its keys once and keeps the logits in shared memory while they fit; longer ones are worked out again.
+// Sequences of more rows take a row tile after the other, the later ones on top of what the earlier wrote.
+constexpr int kKeptLogits = 16384;
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void weight_step_kernel(PromptParams p) {
+  __shared__ __attribute__((aligned(16))) float kept[kKeptLogits];
+  __shared__ u32x4 limbs[2 * (D / 32) * 64];
+  __shared__ RowInfo info[kWeightRows];
+  __shared__ float2 stats[4][kWeightRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.x, b = blockIdx.y;
+  const int len = min(max(p.seq_lens[b], 0), p.bound);
+  int begin, n;
+  packed_range(p.cu_q, b, p.T_q, begin, n);
+  const int shift = __builtin_ctz(p.group), first_hidden = len - n + 1;
+  const int64_t rows = (int64_t)n * p.group, record = ((int64_t)b * p.n_kv_heads + h) * p.score_stride;
+  const float* prev = p.prev;
+  if (rows == 0)
+    for (int j = threadIdx.x; j < len; j += 256) p.scores[record + j] = prev ? prev[record + j] : 0.f;
+  if (len == 0) return;
+  for (int64_t row0 = 0; row0 < rows; row0 += kWeightRows) {
+    const int here = (int)min((int64_t)kWeightRows, rows - row0);
+    const int start = kWeightKeys * wave;
+    KeyStream<D> keys;
+    keys.pages = p.page_table + (int64_t)b * p.max_pages;
+    keys.end = keys.len = len;
+    keys.stride = 4 * kWeightKeys;
+    keys.start(p, h, start, lane);
+    for (int r = wave; r < kWeightRows; r += 4) {
+      const int64_t row = row0 + min(r, here - 1);
+      // (a wavefront's row is turned over in its part of the logits' memory)
+      const f32x2 v = put_query_row<D>(p, begin + (row >> shift), h * p.group + (int)(row & (p.group - 1)), kept + 128 * wave, (uint16_t*)limbs, r, lane);
+      if (lane == 0) info[r] = RowInfo{v.x, v.y, 0.f, 0.f};
+      if (r + 4 >= here && r + 4 < kWeightRows) {                          // (the same row for the places that are left)
+        for (int s = r + 4; s < kWeightRows; s += 4) {
+#pragma unroll
+          for (int l = 0; l < 2; ++l)
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks)
+              if (lane < 4) limbs[(l * (D / 32) + ks) * 64 + 16 * lane + s] = u32x4{0, 0, 0, 0};
+          if (lane == 0) info[s] = RowInfo{0.f, 0.f, 0.f, 0.f};
+        }
+        break;
+      }
+    }
+    __syncthreads();
+    TileQueries<D> tq;
+    tq.load(limbs, info, lane);
+    const bool keep = (int64_t)here * len <= kKeptLogits;
+    float m[4], sum[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) { m[r] = -INFINITY; sum[r] = 0.f; }
+    for (int pass = 0; pass < 2; ++pass) {
+      if (pass == 1) {
+        // rows' maxima and sums over all lanes and wavefronts
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float top = row_allmax(m[r]), part = row_allsum(sum[r] * fast_exp2(m[r] - (top == -INFINITY ? 0.f : top)));
+          if ((lane & 15) == 0) stats[wave][4 * (lane >> 4) + r] = make_float2(top, part);
+        }
+        __syncthreads();
+        if (threadIdx.x < kWeightRows) {
+          const int r = threadIdx.x;
+          const float2 a = stats[0][r], c = stats[1][r], d = stats[2][r], e = stats[3][r];
+          const float top = fmaxf(fmaxf(a.x, c.x), fmaxf(d.x, e.x)), ref = top == -INFINITY ? 0.f : top;
+          const float all = (a.y * fast_exp2(a.x - ref) + c.y * fast_exp2(c.x - ref)) + (d.y * fast_exp2(d.x - ref) + e.y * fast_exp2(e.x - ref));
+          info[r].m = ref;
+          info[r].inv = all == 0.f ? 0.f : 1.f / all;
+        }
+        __syncthreads();
+        if (keep) {
+          for (int j = threadIdx.x; j < len; j += 256) {
+            float w = 0.f;
+            for (int r = 0; r < here; ++r) w = fmaf(fast_exp2(kept[r * len + j] - info[r].m), info[r].inv, w);
+            p.scores[record + j] = (prev ? prev[record + j] : 0.f) + w;
+          }
+          break;
+        }
+        keys.start(p, h, start, lane);
+      }
+      keys.each(start, [&](int key0, KeyCodes<D>& codes) {
+        u32x4 k[4][D / 32];
+        f32x2 pair[4];
+        f32x4 x[4];
+        take_keys<D>(codes, key0, len, lane, k, pair);
+        keys.next(p, h, key0, lane, codes);
+        const bool masked = key0 + kWeightKeys > min(first_hidden + (int)(row0 >> shift), len);
+        step_logits<D>(tq, k, pair, key0, len, masked, first_hidden, shift, (int)row0, lane, x);
+        if (pass == 0) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float top = fmaxf(fmaxf(m[r], fmaxf(x[0][r], x[1][r])), fmaxf(x[2][r], x[3][r])), ref = top == -INFINITY ? 0.f : top;
+            sum[r] = fmaf(sum[r], fast_exp2(m[r] - ref), (fast_exp2(x[0][r] - ref) + fast_exp2(x[1][r] - ref)) + (fast_exp2(x[2][r] - ref) + fast_exp2(x[3][r] - ref)));
+            m[r] = top;
+          }
+          if (keep) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (4 * (lane >> 4) + r < here) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                  const int key = key0 + 16 * t + (lane & 15);
+                  if (key < len) kept[(4 * (lane >> 4) + r) * len + key] = x[t][r];
+                }
+              }
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            float w = 0.f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (4 * (lane >> 4) + r < here) w = fmaf(fast_exp2(x[t][r] - info[4 * (lane >> 4) + r].m), info[4 * (lane >> 4) + r].inv, w);
+            w = add_xor32(add_xor16(w));
+            const int key = key0 + 16 * t + lane;
+            if (lane < 16 && key < len) p.scores[record + key] = (prev ? prev[record + key] : 0.f) + w;
+          }
+        }
+      });
+    }
+    prev = p.scores;
+    __syncthreads();
+  }
+}
+
 static int weight_chunks(int Hkv, int B, int64_t bound) {
   const int64_t items = (int64_t)B * Hkv;
-  int64_t s = 1024 / items;
+  int64_t s = 2048 / items;
   const int64_t most = (bound + 4 * kWeightKeys - 1) / (4 * kWeightKeys);
   if (s > most) s = most;
   return s < 1 ? 1 : s > 256 ? 256 : (int)s;
@@ -289,7 +465,7 @@ template <int D>
 static void launch_passes(const PromptParams& p, int64_t tiles, int chunks, int chunk_keys, hipStream_t st) {
   const int groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles);
   if (p.T_q) {
-    weight_query_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(256), 0, st>>>(p, tiles);
+    weight_query_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(1024), 0, st>>>(p, tiles);
     weight_pass_kernel<D, true><<<dim3(p.n_kv_heads * chunks, p.B, groups), dim3(256), 0, st>>>(p, tiles, chunk_keys);
     weight_join_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(64), 0, st>>>(p, tiles, chunks);
   }
@@ -301,6 +477,12 @@ int launch_weights(const PromptParams& p, int D, hipStream_t st) {
   const int chunks = weight_chunks(p.n_kv_heads, p.B, p.bound), unit = 4 * kWeightKeys;
   const int chunk_keys = (int)(((int64_t)(p.bound + chunks - 1) / chunks + unit - 1) / unit * unit);
   if (tiles > 0x7fffffffLL || (int64_t)p.n_kv_heads * chunks > 0x7fffffffLL || (tiles + kGroupTiles - 1) / kGroupTiles > 65535) return SAW_EINVAL;
+  if (p.T_q <= p.B && (int64_t)p.B * p.n_kv_heads >= 256) {
+    const dim3 grid(p.n_kv_heads, p.B);
+    if (D == 128) weight_step_kernel<128><<<grid, dim3(256), 0, st>>>(p);
+    else weight_step_kernel<64><<<grid, dim3(256), 0, st>>>(p);
+    return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;
+  }
   if (D == 128) launch_passes<128>(p, tiles, chunks, chunk_keys, st);
   else launch_passes<64>(p, tiles, chunks, chunk_keys, st);
   return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;

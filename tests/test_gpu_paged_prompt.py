@@ -248,6 +248,21 @@ def test_weights_under_rotations(saw, options):
     pc.check(got, want, tol)
 
 
+@pytest.mark.parametrize("n", [[1] * 40, [0, 3, 0, 1, 36] + [0] * 35], ids=["one each", "uneven"])
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8), (128, 1)])
+def test_weights_of_a_decode_step(saw, n, d, G):
+    """Batches that fill the chip: one launch, whose shared memory holds the logits of some sequences and not of others."""
+    lens = [1, 16, 5000, 40, 300] + list(range(100, 2200, 60))
+    c = Case(saw, n, lens, Hkv=8, G=G, d=d, h=d, seed=3)
+    prev = np.random.default_rng(1).random((40, 8, 5003)).astype(np.float32)
+    want, tol = _scores(c, prev)
+    start = torch.from_numpy(prev).cuda()
+    got = saw.paged_attn_weights(c.cache, *c.args, prev=start, scores=start, max_seq_len=5000).cpu()
+    for b, L in enumerate(lens):
+        pc.check(got[b, :, :L], want[b, :, :L], tol[b, :, :L], b)
+        assert np.array_equal(got[b, :, L:].numpy(), prev[b, :, L:])
+
+
 def test_weights_add_up_in_place_and_to_the_number_of_rows(saw):
     """Every row's weights sum to one; a second call on the record itself doubles it."""
     c = Case(saw, [4, 1, 0, 3], [300, 17, 9, 2])
