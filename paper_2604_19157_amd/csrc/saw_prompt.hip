@@ -81,7 +81,9 @@ struct CodePieces {
 // c s - s z of the eight codes of a word, as 16-bit values in channel order
 template <typename M>
 __device__ __forceinline__ u32x4 widen_codes(uint32_t w, float s, float sz) {
-  const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
+  uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
+  // (kept as they are: the compiler would take every code out of w by itself, an instruction each, where the conversion can name its byte)
+  asm("" : "+v"(even), "+v"(odd));
   u32x4 x;
   x.x = M::pack(fmaf((float)(even & 0xff), s, -sz), fmaf((float)(odd & 0xff), s, -sz));
   x.y = M::pack(fmaf((float)((even >> 8) & 0xff), s, -sz), fmaf((float)((odd >> 8) & 0xff), s, -sz));
@@ -576,7 +578,7 @@ struct PromptPlan { int rows, waves, splits; };
 static PromptPlan prompt_plan(bool int4, int G, int Hkv, int64_t T, int B, int64_t max_k_len) {
   PromptPlan r = {128, 4, 1};
   int64_t want = 512;
-  if (int4 && T * G <= 64 * (int64_t)B) { r.rows = 32; want = 1280; }
+  if (int4 && T * G <= 64 * (int64_t)B) { r.rows = 32; want = 900; }
   const int64_t blocks = row_tiles(T, G, r.rows, B) * Hkv;
   int64_t s = want / blocks, most = (max_k_len + 255) / 256;
   if (s > most) s = most;
