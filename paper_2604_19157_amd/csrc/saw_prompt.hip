@@ -520,8 +520,6 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   finish_rows<D, kKvInt4, kHalfBit>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, qf, scale, st, lane);
 }
 
-constexpr int kMaxKeySplits = 64;
-
 // Joins the partial records of a row: one wavefront a row.
 template <int D, bool INT4>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int splits) {
@@ -573,14 +571,26 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int s
   for (int e = 0; e < E; ++e) store_elem(p.out, p.dtype, row * D + E * lane + e, o[e]);
 }
 
-// How a call is handed out: rows of a block, wavefronts of it, splits of the keys.
-struct PromptPlan { int rows, waves, splits; };
-static PromptPlan prompt_plan(bool int4, int G, int Hkv, int64_t T, int B, int64_t max_k_len) {
-  PromptPlan r = {128, 4, 1};
+// How a call is handed out: rows of a block, splits of the keys.
+//   * INT4 pages and at most 64 rows a sequence on average: blocks of 32 rows whose wavefronts share out the keys (32 sequences of 512 to 4096
+//     tokens, 32 query / 8 kv heads: 5 new tokens 54 us, 181 in blocks of 128 rows; 16 tokens 85, 24 tokens, in blocks of 128, 200);
+//   * 4096 rows a sequence and more, and a block for every compute unit: 256 rows, eight wavefronts, so that keys are brought in (and
+//     codes widened) half as often (8192 causal tokens 520 us, 544 in blocks of 128; 2048 tokens over 16384 in the pages 708 and 777; but 19
+//     packed prompts of 60 to 1437 tokens 181 and 178, four short ones 13.2 and 11.2);
+//   * 128 rows otherwise.
+// Keys are split while a call has fewer blocks than the chip holds, two for a compute unit (few rows: where it has under 900 of four
+// wavefronts that go their own ways; 640: 80 us instead of 59, 2560: 67), into parts of 256 keys at least.  A split where the
+// chip is full already costs its records: two sequences of 2000 tokens, 512 blocks, 88 us, in two splits 161.
+struct PromptPlan { int rows, splits; };
+constexpr int kMaxKeySplits = 64;
+static PromptPlan prompt_plan(bool int4, int D, int G, int Hkv, int64_t T, int B, int64_t max_k_len) {
+  PromptPlan r = {128, 1};
   int64_t want = 512;
   if (int4 && T * G <= 64 * (int64_t)B) { r.rows = 32; want = 900; }
+  else if ((D == 128 || !int4) && T * G >= 4096 * (int64_t)B && row_tiles(T, G, 256, B) * Hkv >= 256) r.rows = 256;
   const int64_t blocks = row_tiles(T, G, r.rows, B) * Hkv;
   int64_t s = want / blocks, most = (max_k_len + 255) / 256;
+  if (r.rows == 256) s = 1;
   if (s > most) s = most;
   r.splits = s < 1 ? 1 : s > kMaxKeySplits ? kMaxKeySplits : (int)s;
   return r;
@@ -592,14 +602,15 @@ static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream
   const int64_t rows = p.T_q * p.n_q_heads;
   const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads), plan.splits), by_row((unsigned)((rows + 3) / 4)), block(256);
   if (KV == kKvInt4 && D == kDenseD && p.dense_k) prompt_query_kernel<D><<<by_row, block, 0, st>>>(p);
-  if (plan.rows == 32) few_rows_kernel<D><<<grid, block, 0, st>>>(p);
-  else prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
+  if (KV == kKvInt4 && plan.rows == 32) few_rows_kernel<D><<<grid, block, 0, st>>>(p);
+  else if (plan.rows == 128) prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
+  else if constexpr (D == 128 || KV != kKvInt4) prompt_kernel<D, KV, 8><<<grid, dim3(512), 0, st>>>(p);
   if (plan.splits > 1 || (KV == kKvInt4 && p.dense_v)) prompt_merge_kernel<D, KV == kKvInt4><<<by_row, block, 0, st>>>(p, plan.splits);
 }
 
 int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
   const int64_t rows = p.T_q * p.n_q_heads;
-  const PromptPlan plan = prompt_plan(int4, p.group, p.n_kv_heads, p.T_q, p.B, p.bound);
+  const PromptPlan plan = prompt_plan(int4, D, p.group, p.n_kv_heads, p.T_q, p.B, p.bound);
   if (row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads > 0x7fffffffLL || rows / 4 >= 0x7fffffffLL) return SAW_EINVAL;
   if (int4) {
     // (behind the records: rows of D + 2 floats)
@@ -618,11 +629,11 @@ int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
 }
 
 size_t prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len) {
-  const PromptPlan plan = prompt_plan(false, Hq / Hkv, Hkv, T, B, max_k_len);
+  const PromptPlan plan = prompt_plan(false, D, Hq / Hkv, Hkv, T, B, max_k_len);
   return 16 + (plan.splits > 1 ? record_bytes(D, T * Hq, plan.splits) : 0);
 }
 size_t paged_prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len) {
-  const PromptPlan plan = prompt_plan(true, Hq / Hkv, Hkv, T, B, max_k_len);
+  const PromptPlan plan = prompt_plan(true, D, Hq / Hkv, Hkv, T, B, max_k_len);
   const int64_t rows = T * Hq;
   return 32 + record_bytes(D, rows, plan.splits) + (size_t)(rows + 3) / 4 * 16 + (size_t)rows * D * 2;
 }

@@ -116,6 +116,13 @@ def test_rotations(saw, options, dtype):
     pc.check(saw.paged_prompt_attn(c.cache, *c.args), want, tol)
 
 
+def test_a_long_chunk(saw):
+    """Blocks of 256 rows."""
+    c = Case(saw, [1024], [1100], Hkv=16, G=4, seed=8)
+    want, tol = c.attention()
+    pc.check(saw.paged_prompt_attn(c.cache, *c.args), want, tol)
+
+
 def test_queries_in_front_of_all_tokens_and_empty_sequences(saw):
     """More queries than tokens: the first rows see nothing and are zero; rows of no sequence stay as they were."""
     c = Case(saw, [6, 4, 0, 2], [2, 0, 7, 2])

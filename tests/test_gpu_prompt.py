@@ -178,6 +178,19 @@ def test_captured_and_replayed_on_another_stream(saw, n_q, n_k):
     assert torch.equal(other, here)
 
 
+@pytest.mark.parametrize("d,G,Hkv,n,n_k", [(128, 8, 2, 5120, 5120), (64, 8, 16, 600, 630)])
+def test_long_prompts(saw, d, G, Hkv, n, n_k):
+    """Long enough for the large blocks: rows at the ends and around a block's border, of the first and last heads."""
+    q, k, v = pc.rand((n, Hkv * G, d), 1, BF), pc.rand((n_k, Hkv, d), 2, BF), pc.rand((n_k, Hkv, d), 3, BF)
+    got = saw.prompt_attn(q.cuda(), k.cuda(), v.cuda(), torch.tensor([0, n], dtype=torch.int32).cuda(), torch.tensor([0, n_k], dtype=torch.int32).cuda()).cpu()
+    for g in (0, Hkv - 1):
+        heads = slice(g * G, (g + 1) * G)
+        for i in [0, 1, 31, 32, 33, 63, 64, n // 2 + 5, n - 33, n - 1]:
+            L = n_k - n + i + 1
+            want, tol = pc.prompt_reference(q[i:i + 1, heads], k[:L, g:g + 1], v[:L, g:g + 1], [0, 1], [0, L], True)
+            pc.check(got[i:i + 1, heads], want, tol, (g, i))
+
+
 def test_no_queries_is_a_no_op(saw):
     q, k = torch.empty((0, 4, 128), dtype=BF, device="cuda"), pc.rand((5, 2, 128), 1, BF).cuda()
     assert saw.prompt_attn(q, k, k, torch.zeros(2, dtype=torch.int32, device="cuda"), torch.tensor([0, 5], dtype=torch.int32).cuda()).shape == (0, 4, 128)
