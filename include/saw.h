@@ -447,11 +447,14 @@ int saw_paged_attn_weights(const saw_cache_t* cache, const void* q, int32_t dtyp
  *   kept        device, [B][n_kv_heads][budget] int32: the old positions of the kept tokens, ascending; -1 from new_lens[b] on
  *   scores_out  device, [B][n_kv_heads][score_out_stride >= budget] float32 or NULL: the kept tokens' scores, 0 from new_lens[b] to
  *               budget; must not overlap `scores`.
+ *   workspace   at least saw_evict_workspace_bytes(...) bytes, 16-byte aligned, one per call in flight.  That is 0 for most calls (NULL
+ *               will do then); few long sequences are selected from by several blocks each, which exchange what they count there.
  */
+size_t saw_evict_workspace_bytes(const saw_cache_t* cache, int32_t B, int64_t max_seq_len);
 int saw_evict_pages(const saw_cache_t* cache, const float* scores, int64_t score_stride, const int32_t* page_table,
                     int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t B, int32_t max_seq_len, int32_t budget, int32_t recent,
                     const int32_t* dst_table, int32_t dst_pages_per_seq, int32_t* new_lens, int32_t* kept, float* scores_out,
-                    int64_t score_out_stride, saw_stream_t stream);
+                    int64_t score_out_stride, void* workspace, size_t workspace_bytes, saw_stream_t stream);
 
 /*
  * 16-bit-KV comparison path (the unquantised cache the paper measures INT4 against):

@@ -93,7 +93,9 @@ def lib() -> ctypes.CDLL:
         L.saw_prompt_attn.argtypes = [vp, vp, vp, i32, i32, i32, i32, i64, i64, i64, i64, i64, vp, vp, i32, i64, i32, f32, vp, vp, sz, vp]
         L.saw_paged_prompt_attn.argtypes = [cp, vp, i32, i64, i64, i32, vp, i32, vp, i32, vp, i32, f32, vp, vp, sz, vp]
         L.saw_paged_attn_weights.argtypes = [cp, vp, i32, i64, i64, i32, vp, i32, vp, i32, vp, i32, f32, vp, vp, i64, vp, sz, vp]
-        L.saw_evict_pages.argtypes = [cp, vp, i64, vp, i32, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, i64, vp]
+        L.saw_evict_workspace_bytes.restype = sz
+        L.saw_evict_workspace_bytes.argtypes = [cp, i32, i64]
+        L.saw_evict_pages.argtypes = [cp, vp, i64, vp, i32, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, i64, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -379,8 +381,13 @@ def paged_attn_weights(cache: Cache, q, cu_q, page_table, seq_lens, prev=None, s
     return scores
 
 
+def evict_workspace_bytes(cache: Cache, n_seqs, max_seq_len) -> int:
+    st = cache.struct()
+    return int(lib().saw_evict_workspace_bytes(ctypes.byref(st), n_seqs, max_seq_len))
+
+
 def evict_pages(cache: Cache, scores, page_table, seq_lens, dst_table, budget, recent=0, max_seq_len=0, new_lens=None, kept=None,
-                scores_out=None):
+                scores_out=None, workspace=None):
     """saw_evict_pages: keeps ``budget`` tokens of every (sequence, kv head) by ``scores [B][Hkv][n]`` fp32, the last ``recent`` among them,
     and copies them to the pages of ``dst_table``; returns ``(new_lens [B], kept [B][Hkv][budget], scores_out [B][Hkv][>= budget])``."""
     B, dev = seq_lens.numel(), scores.device
@@ -390,7 +397,12 @@ def evict_pages(cache: Cache, scores, page_table, seq_lens, dst_table, budget, r
         kept = torch.empty((B, cache.n_kv_heads, budget), dtype=torch.int32, device=dev)
     if scores_out is None:
         scores_out = torch.empty((B, cache.n_kv_heads, budget), dtype=torch.float32, device=dev)
-    _check((_native or _marshal()).evict(cache, scores, page_table, seq_lens, dst_table, budget, recent, max_seq_len, new_lens, kept, scores_out),
+    if workspace is None:
+        need = evict_workspace_bytes(cache, B, max_seq_len if max_seq_len > 0 else page_table.shape[1] * cache.page_size)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _check((_native or _marshal()).evict(cache, scores, page_table, seq_lens, dst_table, budget, recent, max_seq_len, new_lens, kept, scores_out,
+                                         workspace),
            "saw_evict_pages")
     return new_lens, kept, scores_out
 

@@ -403,9 +403,9 @@ PyObject* attn_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (cache, scores, page_table, seq_lens, dst_table, budget, recent, max_seq_len, new_lens, kept, scores_out or None)
+// (cache, scores, page_table, seq_lens, dst_table, budget, recent, max_seq_len, new_lens, kept, scores_out or None, workspace or None)
 PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call(n, 11, [&](Held& held) {
+  return call(n, 12, [&](Held& held) {
     saw_cache_t c;
     cache_of(a[0], c, held);
     const at::Tensor &scores = tensor(a[1]), &pt = tensor(a[2]), &lens = tensor(a[3]), &dst = tensor(a[4]), &now = tensor(a[8]), &kept = tensor(a[9]);
@@ -421,8 +421,17 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t* const nl = (int32_t*)offsets(now, B, "new_lens is a contiguous int32 vector of seq_lens' length");
     on_this_gpu(scores, pt, lens, dst, now, kept);
     if (out) on_this_gpu(tensor(a[10]));
+    void* ws = nullptr;
+    size_t ws_bytes = 0;
+    if (a[11] != Py_None) {
+      const at::Tensor& w = tensor(a[11]);
+      check(w.is_contiguous(), "the workspace is contiguous");
+      on_this_gpu(w);
+      ws = w.data_ptr();
+      ws_bytes = (size_t)w.nbytes();
+    }
     return run(present(&saw_evict_pages), &c, from, stride, table, (int32_t)pt.size(1), sl, (int32_t)B, bound, budget, recent, to, (int32_t)dst.size(1), nl,
-               (int32_t*)kept.data_ptr(), out, out_stride, stream());
+               (int32_t*)kept.data_ptr(), out, out_stride, ws, ws_bytes, stream());
   });
 }
 

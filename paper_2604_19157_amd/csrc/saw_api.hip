@@ -291,7 +291,8 @@ static bool make_plan(const saw_cache_t* c, int B, int G, bool fixed, int max_pa
 // ---- calls of packed queries and eviction ----
 int launch_prompt(PromptParams, int D, bool int4, hipStream_t);
 int launch_weights(const PromptParams&, int D, hipStream_t);
-int launch_evict(const EvictParams&, int B, int D, hipStream_t);
+int launch_evict(const EvictParams&, int B, int D, void* ws, hipStream_t);
+size_t evict_bytes(int64_t rows, int64_t bound);
 size_t prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len);
 size_t paged_prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len);
 size_t weights_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len);
@@ -838,10 +839,15 @@ int saw_paged_attn_weights(const saw_cache_t* c, const void* q, int32_t dtype, i
   return launch_weights(p, c->head_dim, (hipStream_t)stream);
 }
 
+size_t saw_evict_workspace_bytes(const saw_cache_t* c, int32_t B, int64_t max_seq_len) {
+  if (!c || !shape_ok(c) || B < 1 || B > 65535 || max_seq_len < 1 || max_seq_len > 0x7fffffffLL) return 0;
+  return evict_bytes((int64_t)B * c->n_kv_heads, max_seq_len);
+}
+
 int saw_evict_pages(const saw_cache_t* c, const float* scores, int64_t score_stride, const int32_t* page_table,
                     int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t B, int32_t max_seq_len, int32_t budget, int32_t recent,
                     const int32_t* dst_table, int32_t dst_pages_per_seq, int32_t* new_lens, int32_t* kept, float* scores_out,
-                    int64_t score_out_stride, saw_stream_t stream) {
+                    int64_t score_out_stride, void* workspace, size_t workspace_bytes, saw_stream_t stream) {
   if (!c) return SAW_ENULL;
   if (!shape_ok(c) || c->n_kv_heads > 65535 || B < 1 || B > 65535 || max_pages_per_seq < 1 || dst_pages_per_seq < 1) return SAW_EINVAL;
   const int64_t cap = (int64_t)max_pages_per_seq * c->page_size;
@@ -854,13 +860,17 @@ int saw_evict_pages(const saw_cache_t* c, const float* scores, int64_t score_str
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || (((uintptr_t)c->k_meta) & 7u) || (((uintptr_t)c->v_meta) & 7u)) return SAW_EINVAL;
   if (!aligned4(scores) || !aligned4(page_table) || !aligned4(seq_lens) || !aligned4(dst_table) || !aligned4(new_lens) || !aligned4(kept) || !aligned4(scores_out))
     return SAW_EINVAL;
+  const size_t need = evict_bytes((int64_t)B * c->n_kv_heads, bound);
+  if (need && !workspace) return SAW_ENULL;
+  if (!aligned16(workspace)) return SAW_EINVAL;
+  if (workspace_bytes < need) return SAW_EWORKSPACE;
   EvictParams p = {};
   p.codes[0] = c->k_codes; p.codes[1] = c->v_codes; p.meta[0] = c->k_meta; p.meta[1] = c->v_meta;
   p.scores = scores; p.score_stride = score_stride; p.page_table = page_table; p.seq_lens = seq_lens; p.dst_table = dst_table;
   p.max_pages = max_pages_per_seq; p.dst_pages = dst_pages_per_seq; p.num_pages = c->num_pages; p.n_kv_heads = c->n_kv_heads;
   p.bound = bound; p.budget = budget; p.recent = recent; p.new_lens = new_lens; p.kept = kept;
   p.scores_out = scores_out; p.score_out_stride = score_out_stride;
-  return launch_evict(p, B, c->head_dim, (hipStream_t)stream);
+  return launch_evict(p, B, c->head_dim, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -70,6 +70,66 @@ __device__ __forceinline__ void for_scores(const float* s, int j0, int j1, int t
   batch_scores<1>(s, batch_scores<4>(s, j, j1, thread, threads, f), j1, thread, threads, f);
 }
 
+// The last score that is kept: positions from `old` on and scores above it are, of its equals the first.  (Compared as floats, which agrees
+// with the keys but for NaN: if that is the last that is kept, every number is above it.)
+struct Last {
+  float score;
+  bool nan;
+  int old;
+  __device__ Last(uint32_t key, int old) : score(score_of(key)), nan(key == 0), old(old) {}
+  __device__ bool above(int at, float f) const { return at >= old || (nan ? f == f : f > score); }
+  __device__ bool tie(int at, float f) const { return at < old && (nan ? f != f : f == score); }
+};
+
+// Kept positions of [j0, j1) by each of the block's 16 wavefronts: they count what they keep, then write it behind what the wavefronts in
+// front of them keep, and the block behind `done` kept tokens with `tied` equals of the last among them.
+__device__ __forceinline__ void write_kept(const float* s, int j0, int j1, int wave, int lane, const Last& last, int want, int done, int tied,
+                                           int2* sums, int32_t* kept, float* out) {
+  int above = 0, ties = 0;
+  for_scores(s, j0, j1, lane, 64, [&](int at, float f) {
+    above += __popcll(__ballot(at < j1 && last.above(at, f)));
+    ties += __popcll(__ballot(at < j1 && last.tie(at, f)));
+  });
+  if (lane == 0) sums[wave] = make_int2(above, ties);
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) { done += sums[w].x; tied += sums[w].y; }
+  for_scores(s, j0, j1, lane, 64, [&](int at, float f) {
+    const bool over = at < j1 && last.above(at, f), tie = at < j1 && last.tie(at, f);
+    const uint64_t om = __ballot(over), tm = __ballot(tie);
+    if (om | tm) {
+      int to = done + min(tied, want) + __builtin_amdgcn_mbcnt_hi((uint32_t)(om >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)om, 0));
+      bool keep = over;
+      if (tm) {
+        const int t = tied + __builtin_amdgcn_mbcnt_hi((uint32_t)(tm >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)tm, 0));
+        to += min(t, want) - min(tied, want);
+        keep = over || (tie && t < want);
+      }
+      if (keep) {
+        kept[to] = at;
+        if (out) out[to] = f;
+      }
+      done += __popcll(om);
+      tied += __popcll(tm);
+    }
+  });
+}
+
+// Keys of [0, n) whose first digit is that of `prefix`, appended to `list` by the block's threads; `count` starts at zero.
+__device__ __forceinline__ void list_candidates(const float* s, int j0, int j1, int tid, int lane, uint32_t prefix, uint32_t* list, int* count) {
+  const uint64_t below = (1ull << lane) - 1;
+  for_scores(s, j0, j1, tid, 1024, [&](int j, float f) {
+    const uint32_t key = score_key(f);
+    const bool take = j < j1 && key >> 21 == prefix >> 21;
+    const uint64_t m = __ballot(take);
+    if (m) {                                      // (one addition a wavefront)
+      int at = 0;
+      if (lane == 0) at = atomicAdd(count, __popcll(m));
+      at = __builtin_amdgcn_readfirstlane(at) + __popcll(m & below);
+      if (take) list[at] = key;
+    }
+  });
+}
+
 // Kept positions of one (sequence, kv head), in ascending order, by one block.  The key of the last score that is kept is found 11, 11 and
 // 10 bits at a time; scores that share its first digit are listed in shared memory on the way, so that they alone are looked at for the
 // others (where more than 16384 do, all scores are read again).  Then each wavefront counts what it keeps of its share of the positions
@@ -100,7 +160,6 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictParams p) {
   __shared__ uint32_t listed[kListed];
   __shared__ int count;
   __shared__ int2 sums[16];
-  const uint64_t below = (1ull << lane) - 1;
   uint32_t prefix = 0;
   int want = p.budget - p.recent;               // of the tokens in front of `old`
   int candidates = -1;                          // listed keys; -1: not listed
@@ -129,56 +188,158 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictParams p) {
     if (digit == 0) {
       candidates = pick[2] <= kListed ? 0 : -1;
       if (candidates == 0) {
-        for_scores(s, 0, old, tid, 1024, [&](int j, float f) {
-          const uint32_t key = score_key(f);
-          const bool take = j < old && key >> 21 == prefix >> 21;
-          const uint64_t m = __ballot(take);
-          if (m) {                                // (one addition a wavefront)
-            int at = 0;
-            if (lane == 0) at = atomicAdd(&count, __popcll(m));
-            at = __builtin_amdgcn_readfirstlane(at) + __popcll(m & below);
-            if (take) listed[at] = key;
-          }
-        });
+        list_candidates(s, 0, old, tid, lane, prefix, listed, &count);
         __syncthreads();
         candidates = count;
       }
     }
     __syncthreads();
   }
-  // `want` of the tokens whose key is `prefix` are kept, the lowest positions first.  (Compared as floats, which agrees with the keys
-  // but for NaN: if that is the last that is kept, every number is above it.)
-  const float last = score_of(prefix);
-  const bool nan = prefix == 0;
+  // `want` of the tokens whose key is `prefix` are kept, the lowest positions first
+  const Last last(prefix, old);
   const int share = (len + 1023) / 1024 * 64, j0 = wave * share, j1 = min(len, j0 + share);
-  int above = 0, ties = 0;
-  for_scores(s, j0, j1, lane, 64, [&](int at, float f) {
-    above += __popcll(__ballot(at < j1 && (at >= old || (nan ? f == f : f > last))));
-    ties += __popcll(__ballot(at < j1 && at < old && (nan ? f != f : f == last)));
-  });
-  if (lane == 0) sums[wave] = make_int2(above, ties);
+  write_kept(s, j0, j1, wave, lane, last, want, 0, 0, sums, kept, out);
+}
+
+// The same for few long rows, by a block for every 8192 positions in three launches: digits of the segments; candidates of the segments, whose
+// first digit every block picks by itself from all segments' counts; the remaining digits, again by every block, and the segment's kept
+// positions.  (One block a row took 120 us for 131072 tokens, bound by the instructions that a single compute unit issues.)
+constexpr int kSegment = 8192;
+
+struct SegmentSpace {
+  int* hist;                // [row][segment][kBins]
+  uint32_t* list;           // [row][segment][kSegment]
+  int2* counts;             // [row][segment]: scores above the first digit of the last, candidates
+  int segments;
+  __host__ __device__ SegmentSpace(void* ws, int64_t rows, int segments) : segments(segments) {
+    hist = (int*)ws;
+    list = (uint32_t*)(hist + rows * segments * kBins);
+    counts = (int2*)(list + rows * segments * kSegment);
+  }
+};
+
+__device__ __forceinline__ void clear(int* hist, int tid) {
+  for (int i = tid; i < kBins * kCopies; i += 1024) hist[i] = 0;
+}
+
+__global__ __launch_bounds__(1024) void evict_digit_kernel(EvictParams p, SegmentSpace ws) {
+  const int b = blockIdx.z, h = blockIdx.y, seg = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int len = min(max(p.seq_lens[b], 0), p.bound), old = max(len - p.recent, 0);
+  const int j0 = seg * kSegment, j1 = min(old, j0 + kSegment);
+  if (len <= p.budget || j0 >= len) return;
+  const int64_t row = (int64_t)b * p.n_kv_heads + h;
+  __shared__ int hist[kBins * kCopies];
+  clear(hist, tid);
   __syncthreads();
-  int done = 0, tied = 0;                        // of the wavefronts in front: kept for their key, ties
-  for (int w = 0; w < wave; ++w) { done += sums[w].x; tied += sums[w].y; }
-  for_scores(s, j0, j1, lane, 64, [&](int at, float f) {
-    const bool over = at < j1 && (at >= old || (nan ? f == f : f > last)), tie = at < j1 && at < old && (nan ? f != f : f == last);
-    const uint64_t om = __ballot(over), tm = __ballot(tie);
-    if (om | tm) {
-      int to = done + min(tied, want) + __builtin_amdgcn_mbcnt_hi((uint32_t)(om >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)om, 0));
-      bool keep = over;
-      if (tm) {
-        const int t = tied + __builtin_amdgcn_mbcnt_hi((uint32_t)(tm >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)tm, 0));
-        to += min(t, want) - min(tied, want);
-        keep = over || (tie && t < want);
-      }
-      if (keep) {
-        kept[to] = at;
-        if (out) out[to] = f;
-      }
-      done += __popcll(om);
-      tied += __popcll(tm);
-    }
+  for_scores(p.scores + row * p.score_stride, j0, j1, tid, 1024, [&](int j, float f) {
+    if (j < j1) atomicAdd(&hist[(score_key(f) >> 21) * kCopies + lane % kCopies], 1);
   });
+  __syncthreads();
+  for (int d = tid; d < kBins; d += 1024) ws.hist[(row * ws.segments + seg) * kBins + d] = bin_of(hist, d);
+}
+
+// first digit of the last key that is kept, from the segments' counts
+__device__ __forceinline__ void pick_first(const SegmentSpace& ws, int64_t row, int segments, int want, int tid, int lane, int* hist, int (&pick)[3]) {
+  for (int d = tid; d < kBins; d += 1024) {
+    int n = 0;
+#pragma unroll 4
+    for (int g = 0; g < segments; ++g) n += ws.hist[(row * ws.segments + g) * kBins + d];
+    hist[d * kCopies] = n;
+#pragma unroll
+    for (int c = 1; c < kCopies; ++c) hist[d * kCopies + c] = 0;
+  }
+  __syncthreads();
+  if (tid < 64) pick_bin(hist, want, lane, pick);
+  __syncthreads();
+}
+
+__global__ __launch_bounds__(1024) void evict_list_kernel(EvictParams p, SegmentSpace ws) {
+  const int b = blockIdx.z, h = blockIdx.y, seg = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int len = min(max(p.seq_lens[b], 0), p.bound), old = max(len - p.recent, 0);
+  const int j0 = seg * kSegment, j1 = min(old, j0 + kSegment);
+  if (len <= p.budget || j0 >= len) return;
+  const int64_t row = (int64_t)b * p.n_kv_heads + h;
+  __shared__ int hist[kBins * kCopies];
+  __shared__ int pick[3];
+  __shared__ int count, above;
+  if (tid == 0) count = above = 0;
+  pick_first(ws, row, (len + kSegment - 1) / kSegment, p.budget - p.recent, tid, lane, hist, pick);
+  list_candidates(p.scores + row * p.score_stride, j0, j1, tid, lane, (uint32_t)pick[0] << 21, ws.list + (row * ws.segments + seg) * kSegment, &count);
+  int mine = 0;                                  // scores of larger digits
+  for (int d = tid; d < kBins; d += 1024)
+    if (d > pick[0]) mine += ws.hist[(row * ws.segments + seg) * kBins + d];
+  if (mine) atomicAdd(&above, mine);
+  __syncthreads();
+  if (tid == 0) ws.counts[row * ws.segments + seg] = make_int2(above, count);
+}
+
+__global__ __launch_bounds__(1024) void evict_write_kernel(EvictParams p, SegmentSpace ws) {
+  const int b = blockIdx.z, h = blockIdx.y, seg = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int len = min(max(p.seq_lens[b], 0), p.bound), old = max(len - p.recent, 0), n = min(len, p.budget);
+  const int64_t row = (int64_t)b * p.n_kv_heads + h;
+  const float* const s = p.scores + row * p.score_stride;
+  int32_t* const kept = p.kept + row * p.budget;
+  float* const out = p.scores_out ? p.scores_out + row * p.score_out_stride : nullptr;
+  if (h == 0 && seg == 0 && tid == 0) p.new_lens[b] = n;
+  // (every block a part of what lies behind the kept tokens, or of a sequence that is kept whole)
+  for (int i = (len <= p.budget ? 0 : n) + seg * 1024 + tid; i < p.budget; i += 1024 * (int)gridDim.x) {
+    kept[i] = i < n ? i : -1;
+    if (out) out[i] = i < n ? s[i] : 0.f;
+  }
+  const int j0 = seg * kSegment, j1 = min(len, j0 + kSegment);
+  if (len <= p.budget || j0 >= len) return;
+  __shared__ int hist[kBins * kCopies];
+  __shared__ int pick[3];
+  __shared__ int2 sums[16];
+  __shared__ int before[2];
+  const int segments = (len + kSegment - 1) / kSegment;
+  if (tid == 0) before[0] = before[1] = 0;
+  pick_first(ws, row, segments, p.budget - p.recent, tid, lane, hist, pick);
+  uint32_t prefix = (uint32_t)pick[0] << 21;
+  int want = pick[1];
+  for (int digit = 1; digit < 3; ++digit) {
+    const int shift = digit == 1 ? 10 : 0, bins = digit == 1 ? kBins : 1024, above = digit == 1 ? 21 : 10;
+    __syncthreads();
+    clear(hist, tid);
+    __syncthreads();
+    for (int g = wave; g < segments; g += 16) {              // (a wavefront a list)
+      const int64_t at = row * ws.segments + g;
+      const int m = ws.counts[at].y;
+      const uint32_t* const list = ws.list + at * kSegment;
+#pragma unroll 4
+      for (int i = lane; i < m; i += 64) {
+        const uint32_t key = list[i];
+        if (key >> above == prefix >> above) atomicAdd(&hist[((key >> shift) & (bins - 1)) * kCopies + lane % kCopies], 1);
+      }
+    }
+    __syncthreads();
+    if (wave == 0) pick_bin(hist, want, lane, pick);
+    __syncthreads();
+    prefix |= (uint32_t)pick[0] << shift;
+    want = pick[1];
+  }
+  // kept in front of the segment, and equals of the last among the candidates there
+  for (int g = wave; g < seg; g += 16) {
+    const int64_t at = row * ws.segments + g;
+    const int2 c = ws.counts[at];
+    const uint32_t* const list = ws.list + at * kSegment;
+    int above = 0, ties = 0;
+#pragma unroll 4
+    for (int i = lane; i < c.y; i += 64) {
+      above += list[i] > prefix;
+      ties += list[i] == prefix;
+    }
+    for (int d = 1; d < 64; d <<= 1) { above += __shfl_xor(above, d); ties += __shfl_xor(ties, d); }
+    if (lane == 0) {
+      // (positions from `old` on are kept; where a segment in front of this one reaches them its end does)
+      atomicAdd(&before[0], above + c.x + max(0, min(len, (g + 1) * kSegment) - max(old, g * kSegment)));
+      atomicAdd(&before[1], ties);
+    }
+  }
+  __syncthreads();
+  const Last last(prefix, old);
+  const int share = kSegment / 16, w0 = j0 + wave * share;
+  write_kept(s, w0, min(j1, w0 + share), wave, lane, last, want, before[0], before[1], sums, kept, out);
 }
 
 template <int D>
@@ -199,8 +360,26 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
   }
 }
 
-int launch_evict(const EvictParams& p, int B, int D, hipStream_t st) {
-  evict_select_kernel<<<dim3(p.n_kv_heads, B), dim3(1024), 0, st>>>(p);
+// Segments are worth their three launches while rows alone leave compute units without work and are long: 8 rows of 131072 tokens 136 us in
+// all with a block a row; 8 of 16384 level.
+static int evict_segments(int64_t rows, int64_t bound) { return rows < 128 && bound > 16384 ? (int)((bound + kSegment - 1) / kSegment) : 0; }
+size_t evict_bytes(int64_t rows, int64_t bound) {
+  const size_t segments = evict_segments(rows, bound);
+  return segments * rows * (kBins * 4 + kSegment * 4 + 8);
+}
+
+int launch_evict(const EvictParams& p, int B, int D, void* ws, hipStream_t st) {
+  const int64_t rows = (int64_t)B * p.n_kv_heads;
+  const int segments = evict_segments(rows, p.bound);
+  if (segments) {
+    const SegmentSpace space(ws, rows, segments);
+    const dim3 grid(segments, p.n_kv_heads, B);
+    evict_digit_kernel<<<grid, dim3(1024), 0, st>>>(p, space);
+    evict_list_kernel<<<grid, dim3(1024), 0, st>>>(p, space);
+    evict_write_kernel<<<grid, dim3(1024), 0, st>>>(p, space);
+  } else {
+    evict_select_kernel<<<dim3(p.n_kv_heads, B), dim3(1024), 0, st>>>(p);
+  }
   const int per = 256 / (D / 32);
   const dim3 grid((p.budget + per - 1) / per, p.n_kv_heads, B);
   if (D == 128) evict_move_kernel<128><<<grid, dim3(256), 0, st>>>(p);

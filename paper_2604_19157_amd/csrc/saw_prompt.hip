@@ -601,10 +601,13 @@ template <int D, int KV>
 static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream_t st) {
   const int64_t rows = p.T_q * p.n_q_heads;
   const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads), plan.splits), by_row((unsigned)((rows + 3) / 4)), block(256);
-  if (KV == kKvInt4 && D == kDenseD && p.dense_k) prompt_query_kernel<D><<<by_row, block, 0, st>>>(p);
-  if (KV == kKvInt4 && plan.rows == 32) few_rows_kernel<D><<<grid, block, 0, st>>>(p);
-  else if (plan.rows == 128) prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
-  else if constexpr (D == 128 || KV != kKvInt4) prompt_kernel<D, KV, 8><<<grid, dim3(512), 0, st>>>(p);
+  if constexpr (KV == kKvInt4 && D == kDenseD)
+    if (p.dense_k) prompt_query_kernel<D><<<by_row, block, 0, st>>>(p);
+  if (plan.rows == 128) prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
+  if constexpr (KV == kKvInt4)
+    if (plan.rows == 32) few_rows_kernel<D><<<grid, block, 0, st>>>(p);
+  if constexpr (D == 128 || KV != kKvInt4)
+    if (plan.rows == 256) prompt_kernel<D, KV, 8><<<grid, dim3(512), 0, st>>>(p);
   if (plan.splits > 1 || (KV == kKvInt4 && p.dense_v)) prompt_merge_kernel<D, KV == kKvInt4><<<by_row, block, 0, st>>>(p, plan.splits);
 }
 

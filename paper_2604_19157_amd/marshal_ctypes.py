@@ -157,15 +157,16 @@ def attn_weights(cache, q, cu_q, page_table, seq_lens, prev, scores, max_seq_len
                                           workspace.nbytes, b._stream())
 
 
-def evict(cache, scores, page_table, seq_lens, dst_table, budget, recent, max_seq_len, new_lens, kept, scores_out):
+def evict(cache, scores, page_table, seq_lens, dst_table, budget, recent, max_seq_len, new_lens, kept, scores_out, workspace):
     B = seq_lens.numel()
     _counts(budget, recent, max_seq_len)
     assert _record(scores, B, cache.n_kv_heads) and (scores_out is None or _record(scores_out, B, cache.n_kv_heads))
     assert kept.dtype == torch.int32 and kept.is_contiguous() and kept.shape == (B, cache.n_kv_heads, budget)
     assert _vector(seq_lens, B) and _vector(new_lens, B) and _table(page_table, B) and _table(dst_table, B)
-    _on_this_gpu(scores, page_table, seq_lens, dst_table, new_lens, kept, *([] if scores_out is None else [scores_out]))
+    _on_this_gpu(scores, page_table, seq_lens, dst_table, new_lens, kept, *(x for x in (scores_out, workspace) if x is not None))
+    assert workspace is None or workspace.is_contiguous()
     st = cache.struct()
     return b.lib().saw_evict_pages(ctypes.byref(st), b._ptr(scores), scores.shape[2], b._ptr(page_table), page_table.shape[1],
                                    b._ptr(seq_lens), B, max_seq_len, budget, recent, b._ptr(dst_table), dst_table.shape[1],
                                    b._ptr(new_lens), b._ptr(kept), b._ptr(scores_out), 0 if scores_out is None else scores_out.shape[2],
-                                   b._stream())
+                                   b._ptr(workspace), 0 if workspace is None else workspace.nbytes, b._stream())

@@ -100,6 +100,24 @@ def test_scores_of_every_kind(saw, kind):
     c.check(c.run(saw))
 
 
+@pytest.mark.parametrize("lens,budget,recent", [([40000], 5000, 700), ([20000, 0, 8192, 8193, 30], 8192, 0), ([30000, 17000], 9000, 8999), ([16385], 1, 0),
+                                                 ([50000], 30000, 20000)], ids=str)
+@pytest.mark.parametrize("kind", ["random", "few", "constant", "nan"])
+def test_long_rows(saw, lens, budget, recent, kind):
+    """Few long rows are selected from by several blocks each."""
+    rng = np.random.default_rng(budget)
+    s = rng.random((len(lens), 2, max(lens) + 3)).astype(np.float32)
+    if kind == "few":
+        s = rng.integers(0, 5, s.shape).astype(np.float32)
+    elif kind == "constant":
+        s[:] = -2.5
+    elif kind == "nan":
+        s[rng.random(s.shape) < 0.7] = np.nan
+    c = Case(saw, lens, budget, recent, scores=s)
+    assert saw.evict_workspace_bytes(c.cache, len(lens), max(lens)) > 0
+    c.check(c.run(saw))
+
+
 def test_rows_further_apart_than_needed(saw):
     c = Case(saw, [300, 200], 100, 10, width=517)
     out = torch.full((2, 2, 333), 8.0, device="cuda")
