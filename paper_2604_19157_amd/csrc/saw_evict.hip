@@ -11,7 +11,7 @@ __device__ __forceinline__ uint32_t score_key(float f) {
 }
 __device__ __forceinline__ float score_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
-constexpr int kBins = 2048, kCopies = 4, kListed = 16384, kAtOnce = 16;
+constexpr int kBins = 2048, kCopies = 4, kListed = 8192, kAtOnce = 16;
 
 // The largest bin d such that the bins above it hold fewer than `want` entries, and how many are still wanted of it: by the first
 // wavefront, 32 bins a lane.  (A single thread that walked the bins took 8 us a digit.)
@@ -132,10 +132,10 @@ __device__ __forceinline__ void list_candidates(const float* s, int j0, int j1, 
 
 // Kept positions of one (sequence, kv head), in ascending order, by one block.  The key of the last score that is kept is found 11, 11 and
 // 10 bits at a time; scores that share its first digit are listed in shared memory on the way, so that they alone are looked at for the
-// others (where more than 16384 do, all scores are read again).  Then each wavefront counts what it keeps of its share of the positions
+// others (where more than 8192 do, all scores are read again).  Then each wavefront counts what it keeps of its share of the positions
 // and writes it behind the wavefronts in front of it; of equal keys the lowest positions are kept.
 // Bound by the latency of a single block's four readings of the scores, which stay in L2: 131072 tokens, 8 blocks on the chip.
-__global__ __launch_bounds__(1024) void evict_select_kernel(EvictParams p) {
+__global__ __launch_bounds__(1024, 8) void evict_select_kernel(EvictParams p) {
   const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = min(max(p.seq_lens[b], 0), p.bound);
   const int64_t row = (int64_t)b * p.n_kv_heads + h;
