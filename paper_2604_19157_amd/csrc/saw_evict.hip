@@ -342,21 +342,43 @@ __global__ __launch_bounds__(1024) void evict_write_kernel(EvictParams p, Segmen
   write_kept(s, w0, min(j1, w0 + share), wave, lane, last, want, before[0], before[1], sums, kept, out);
 }
 
+// The kept tokens' codes and pairs, a thread for 16 bytes of K and of V of four tokens: where a token lies takes three loads one after the
+// other, so that four of these chains have to be under way at once.  Bound by the memory: reads of 64 bytes at a time, writes of whole
+// tiles (48 sequences, 2048 tokens kept, 226 MB).
 template <int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
-  constexpr int LPV = D / 32;                    // 16-byte pieces of a vector's codes
-  const int t = blockIdx.x * (256 / LPV) + threadIdx.x / LPV, part = threadIdx.x % LPV;
+  constexpr int LPV = D / 32, kEach = 4, kStep = 256 / LPV;      // 16-byte pieces of a vector's codes; tokens of a thread; tokens at once
+  const int t0 = blockIdx.x * (kEach * kStep) + threadIdx.x / LPV, part = threadIdx.x % LPV;
   const int b = blockIdx.z, h = blockIdx.y;
-  if (t >= min(min(max(p.seq_lens[b], 0), p.bound), p.budget)) return;
-  const int j = p.kept[((int64_t)b * p.n_kv_heads + h) * p.budget + t];
-  if (j < 0) return;
-  const int from = p.page_table[(int64_t)b * p.max_pages + (j >> 4)], to = p.dst_table[(int64_t)b * p.dst_pages + (t >> 4)];
-  if (from < 0 || from >= p.num_pages || to < 0 || to >= p.num_pages) return;
-  const int64_t src = ((int64_t)from * p.n_kv_heads + h) * 16 + (j & 15), dst = ((int64_t)to * p.n_kv_heads + h) * 16 + (t & 15);
+  const int n = min(min(max(p.seq_lens[b], 0), p.bound), p.budget);
+  if (t0 >= n) return;
+  const int32_t* const kept = p.kept + ((int64_t)b * p.n_kv_heads + h) * p.budget;
+  int j[kEach], from[kEach], to[kEach];
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    ((u32x4*)(p.codes[w] + dst * (D / 2)))[part] = ((const u32x4*)(p.codes[w] + src * (D / 2)))[part];
-    if (part == w) ((u32x2*)p.meta[w])[dst] = ((const u32x2*)p.meta[w])[src];
+  for (int k = 0; k < kEach; ++k) j[k] = kept[min(t0 + k * kStep, n - 1)];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    from[k] = p.page_table[(int64_t)b * p.max_pages + (max(j[k], 0) >> 4)];
+    to[k] = p.dst_table[(int64_t)b * p.dst_pages + (min(t0 + k * kStep, n - 1) >> 4)];
+  }
+  u32x4 codes[kEach][2];
+  u32x2 pair[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int page = from[k] >= 0 && from[k] < p.num_pages ? from[k] : 0;
+    const int64_t src = ((int64_t)page * p.n_kv_heads + h) * 16 + (j[k] & 15);
+    codes[k][0] = ((const u32x4*)(p.codes[0] + src * (D / 2)))[part];
+    codes[k][1] = ((const u32x4*)(p.codes[1] + src * (D / 2)))[part];
+    pair[k] = ((const u32x2*)(part == 0 ? p.meta[0] : p.meta[1]))[src];
+  }
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int t = t0 + k * kStep;
+    if (t >= n || from[k] < 0 || from[k] >= p.num_pages || to[k] < 0 || to[k] >= p.num_pages) continue;
+    const int64_t dst = ((int64_t)to[k] * p.n_kv_heads + h) * 16 + (t & 15);
+    ((u32x4*)(p.codes[0] + dst * (D / 2)))[part] = codes[k][0];
+    ((u32x4*)(p.codes[1] + dst * (D / 2)))[part] = codes[k][1];
+    if (part < 2) ((u32x2*)p.meta[part])[dst] = pair[k];
   }
 }
 
@@ -380,7 +402,7 @@ int launch_evict(const EvictParams& p, int B, int D, void* ws, hipStream_t st) {
   } else {
     evict_select_kernel<<<dim3(p.n_kv_heads, B), dim3(1024), 0, st>>>(p);
   }
-  const int per = 256 / (D / 32);
+  const int per = 4 * 256 / (D / 32);
   const dim3 grid((p.budget + per - 1) / per, p.n_kv_heads, B);
   if (D == 128) evict_move_kernel<128><<<grid, dim3(256), 0, st>>>(p);
   else evict_move_kernel<64><<<grid, dim3(256), 0, st>>>(p);
