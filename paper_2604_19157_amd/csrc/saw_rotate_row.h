@@ -6,6 +6,8 @@
 namespace saw {
 
 // q R and o R^T of one row in LDS (128 floats; of 64 channels the first half)
+// LOADS: of a learned rotation's rows at once, 8 where registers are short
+template <int LOADS = 16>
 __device__ __forceinline__ void rotate_row(const PromptParams& p, float* x, int D, int lane) {
   if (p.rot_k) {
     if (p.has_signs)
@@ -15,7 +17,7 @@ __device__ __forceinline__ void rotate_row(const PromptParams& p, float* x, int 
     for (int c = lane; c < D; c += 64) x[c] *= had_norm(p.had_block);
     wave_sync();
   }
-  if (p.dense_k) wave_lds_matvec128<1>(x, p.dense, lane);
+  if (p.dense_k) wave_lds_matvec128<1, LOADS>(x, p.dense, lane);
 }
 __device__ __forceinline__ void unrotate_row(const PromptParams& p, float* x, int D, int lane) {
   if (p.dense_v) wave_lds_matvec128<1>(x, p.dense + kDenseD * kDenseD, lane);

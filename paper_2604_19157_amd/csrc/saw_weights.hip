@@ -48,7 +48,7 @@ __device__ __forceinline__ f32x2 put_query_row(const PromptParams& p, int64_t to
 #pragma unroll
   for (int e = 0; e < E; ++e) x[lane + 64 * e] = load_elem(p.q, p.dtype, src + lane + 64 * e);
   wave_sync();
-  rotate_row(p, x, D, lane);
+  rotate_row<8>(p, x, D, lane);
   float top = 0.f, total = 0.f;
 #pragma unroll
   for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[lane + 64 * e] * p.scale));
@@ -141,13 +141,18 @@ struct KeyStream {
   }
 };
 
-// codes - 8 of a word, in the order 0 4 1 5 2 6 3 7: 0x6400 + c is 1024 + c
-__device__ __forceinline__ u32x4 centred(uint32_t w) {
+// codes - 8 of a word, in the order 0 4 1 5 2 6 3 7: 0x6400 + c is 1024 + c.  (The two constants in registers: with both as literals the
+// masking is two instructions.)
+struct CodeBits {
+  uint32_t mask, one;
+  __device__ __forceinline__ CodeBits() { asm("v_mov_b32 %0, 0xf000f\n\tv_mov_b32 %1, 0x64006400" : "=&v"(mask), "=v"(one)); }
+};
+__device__ __forceinline__ u32x4 centred(uint32_t w, CodeBits bits) {
   u32x4 r;
   const f16x2 off = {(_Float16)1032.f, (_Float16)1032.f};
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u) - off);
+    r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, ((w >> (4 * i)) & bits.mask) | bits.one) - off);
   return r;
 }
 
@@ -156,6 +161,7 @@ template <int D>
 struct TileQueries {
   u32x4 q[2][D / 32];
   float scale[4], sum_q[4];       // of rows 4 (lane / 16) + 0..3
+  __device__ __forceinline__ u32x4 limb(int l, int ks) const { return q[l][ks]; }
   __device__ __forceinline__ void load(const u32x4* limbs, const RowInfo* info, int lane) {
 #pragma unroll
     for (int l = 0; l < 2; ++l)
@@ -170,39 +176,40 @@ struct TileQueries {
   }
 };
 
-// Logits of 16 rows and 64 keys: x[t][r] of row 4 (lane / 16) + r and key 16 t + lane % 16, in log2 units; hidden ones and those behind the
-// sequence's end -infinity.
+// ... and one in shared memory, from where its limbs are read again for every 16 keys: registers for four wavefronts a SIMD.
 template <int D>
-__device__ __forceinline__ void step_logits(const TileQueries<D>& tq, const u32x4 (&k)[4][D / 32], const f32x2 (&pair)[4], int key0, int len,
-                                            bool masked, int first_hidden, int shift, int row0, int lane, f32x4 (&x)[4]) {
+struct SharedQueries {
+  const u32x4* limbs;             // (the lane's)
+  float scale[4], sum_q[4];
+  __device__ __forceinline__ u32x4 limb(int l, int ks) const { return limbs[(l * (D / 32) + ks) * 64]; }
+};
+
+// 16 of a step's keys as operand registers; the pair of a slot behind the end, which may hold anything, becomes zero.
+template <int D>
+__device__ __forceinline__ f32x2 key_codes(const KeyCodes<D>& codes, CodeBits bits, int t, int key0, int len, int lane, u32x4 (&k)[D / 32]) {
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int l = 1; l >= 0; --l)
-#pragma unroll
-      for (int ks = 0; ks < D / 32; ++ks) s = mfma16(tq.q[l][ks], k[t][ks], s);
-    const float z8 = pair[t].y - 8.f;
-    const int key = key0 + 16 * t + (lane & 15);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      x[t][r] = fmaf(-z8, tq.sum_q[r], s[r]) * pair[t].x * tq.scale[r];
-      // (row i sees the keys in front of first_hidden + its token)
-      if (masked && (key >= len || key >= first_hidden + ((row0 + 4 * (lane >> 4) + r) >> shift))) x[t][r] = -INFINITY;
-    }
-  }
+  for (int ks = 0; ks < D / 32; ++ks) k[ks] = centred(codes.w[t][ks], bits);
+  return key0 + 16 * t + (lane & 15) < len ? codes.pair[t] : f32x2{0.f, 0.f};
 }
 
-// A step's codes as operand registers; pairs of slots behind the end, which may hold anything, become zero.
-template <int D>
-__device__ __forceinline__ void take_keys(const KeyCodes<D>& codes, int key0, int len, int lane, u32x4 (&k)[4][D / 32], f32x2 (&pair)[4]) {
+// Logits of 16 rows and 16 keys: of row 4 (lane / 16) + r and the lane's key, in log2 units; hidden ones and those behind the sequence's end
+// -infinity.
+template <int D, typename Q>
+__device__ __forceinline__ f32x4 tile_logits16(const Q& tq, const u32x4 (&k)[D / 32], f32x2 pair, int key, int len, bool masked,
+                                               int first_hidden, int shift, int row0, int lane) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f}, x;
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    pair[t] = codes.pair[t];
-    if (key0 + 16 * t + (lane & 15) >= len) pair[t] = f32x2{0.f, 0.f};
+  for (int l = 1; l >= 0; --l)
 #pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) k[t][ks] = centred(codes.w[t][ks]);
+    for (int ks = 0; ks < D / 32; ++ks) s = mfma16(tq.limb(l, ks), k[ks], s);
+  const float z8 = pair.y - 8.f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    x[r] = fmaf(-z8, tq.sum_q[r], s[r]) * pair.x * tq.scale[r];
+    // (row i sees the keys in front of first_hidden + its token)
+    if (masked && (key >= len || key >= first_hidden + ((row0 + 4 * (lane >> 4) + r) >> shift))) x[r] = -INFINITY;
   }
+  return x;
 }
 
 // One pass over a chunk of the keys of a (sequence, kv head).  STATS: maximum and sum of each row of a group of row tiles over the
@@ -228,6 +235,7 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
     wave_sync();
   }
   const int64_t record = ((int64_t)b * p.n_kv_heads + h) * p.score_stride;
+  const CodeBits bits;
   TileQueries<D> tq;
   int held = -1;                // the row tile in tq: a single one is loaded once
   KeyStream<D> keys;
@@ -238,7 +246,8 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
     u32x4 k[4][D / 32];
     f32x2 pair[4];
     float total[4] = {0.f, 0.f, 0.f, 0.f};
-    take_keys<D>(codes, key0, len, lane, k, pair);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) pair[t] = key_codes<D>(codes, bits, t, key0, len, lane, k[t]);
     keys.next(p, h, key0, lane, codes);
     // the first row that sees a key of the step: key0 < first_hidden + token
     const int first_token = max(key0 - first_hidden + 1, 0);
@@ -250,7 +259,8 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
       f32x4 x[4];
       if (g != held) tq.load(ws.limbs + at * 2 * (D / 32) * 64, info, lane);
       held = g;
-      step_logits<D>(tq, k, pair, key0, len, masked, first_hidden, shift, row0, lane, x);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) x[t] = tile_logits16<D>(tq, k[t], pair[t], key0 + 16 * t + (lane & 15), len, masked, first_hidden, shift, row0, lane);
       if constexpr (STATS) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -323,123 +333,162 @@ __global__ __launch_bounds__(64) void weight_join_kernel(PromptParams p, int64_t
 
 // Statistics and weights in one launch, for batches of few rows a sequence that fill the chip by themselves (a decode step): a block takes
 // a (sequence, kv head), reads its keys once and keeps the logits in shared memory while they fit; longer ones are worked out again.
-// Sequences of more rows take a row tile after the other, the later ones on top of what the earlier wrote.
-constexpr int kKeptLogits = 16384;
+// Sequences of more rows take a row tile after the other, the later ones on top of what the earlier wrote.  What bounds it is how many
+// wavefronts a SIMD has to cover one another's waits: four of them, 128 registers each, which is why a step works on 16 keys at a time.
+constexpr int kKeptLogits = 16384, kStepWaves = 8;
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void weight_step_kernel(PromptParams p) {
+__global__ __launch_bounds__(64 * kStepWaves, 4) void weight_step_kernel(PromptParams p) {
   __shared__ __attribute__((aligned(16))) float kept[kKeptLogits];
   __shared__ u32x4 limbs[2 * (D / 32) * 64];
   __shared__ RowInfo info[kWeightRows];
-  __shared__ float2 stats[4][kWeightRows];
+  __shared__ float2 stats[kStepWaves][kWeightRows];
+  constexpr int kThreads = 64 * kStepWaves, kStride = kWeightKeys * kStepWaves;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x, b = blockIdx.y;
   const int len = min(max(p.seq_lens[b], 0), p.bound);
   int begin, n;
   packed_range(p.cu_q, b, p.T_q, begin, n);
   const int shift = __builtin_ctz(p.group), first_hidden = len - n + 1;
-  const int64_t rows = (int64_t)n * p.group, record = ((int64_t)b * p.n_kv_heads + h) * p.score_stride;
+  const int rows = n << shift;
+  const int64_t record = ((int64_t)b * p.n_kv_heads + h) * p.score_stride;
   const float* prev = p.prev;
+  const int32_t* const pages = p.page_table + (int64_t)b * p.max_pages;
   if (rows == 0)
-    for (int j = threadIdx.x; j < len; j += 256) p.scores[record + j] = prev ? prev[record + j] : 0.f;
+    for (int j = threadIdx.x; j < len; j += kThreads) p.scores[record + j] = prev ? prev[record + j] : 0.f;
   if (len == 0) return;
-  for (int64_t row0 = 0; row0 < rows; row0 += kWeightRows) {
-    const int here = (int)min((int64_t)kWeightRows, rows - row0);
-    const int start = kWeightKeys * wave;
-    KeyStream<D> keys;
-    keys.pages = p.page_table + (int64_t)b * p.max_pages;
-    keys.end = keys.len = len;
-    keys.stride = 4 * kWeightKeys;
-    keys.start(p, h, start, lane);
-    for (int r = wave; r < kWeightRows; r += 4) {
-      const int64_t row = row0 + min(r, here - 1);
-      // (a wavefront's row is turned over in its part of the logits' memory)
-      const f32x2 v = put_query_row<D>(p, begin + (row >> shift), h * p.group + (int)(row & (p.group - 1)), kept + 128 * wave, (uint16_t*)limbs, r, lane);
-      if (lane == 0) info[r] = RowInfo{v.x, v.y, 0.f, 0.f};
-      if (r + 4 >= here && r + 4 < kWeightRows) {                          // (the same row for the places that are left)
-        for (int s = r + 4; s < kWeightRows; s += 4) {
-#pragma unroll
-          for (int l = 0; l < 2; ++l)
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks)
-              if (lane < 4) limbs[(l * (D / 32) + ks) * 64 + 16 * lane + s] = u32x4{0, 0, 0, 0};
-          if (lane == 0) info[s] = RowInfo{0.f, 0.f, 0.f, 0.f};
-        }
-        break;
+  for (int row0 = 0; row0 < rows; row0 += kWeightRows) {
+    const int here = min(kWeightRows, rows - row0), start = kWeightKeys * wave;
+    KeyCodes<D> codes;
+    TilePages ids;
+    auto first = [&] {
+      if (start >= len) return;
+      ids.fetch(pages, start / kWeightKeys, len);
+      request_keys<D>(p, ids, h, lane, codes);
+      ids.fetch(pages, (start + kStride) / kWeightKeys, len);
+    };
+    first();
+    for (int r = wave; r < kWeightRows; r += kStepWaves) {
+      if (r < here) {
+        const int row = row0 + r;
+        // (a wavefront's row is turned over in its part of the logits' memory)
+        const f32x2 v = put_query_row<D>(p, begin + (row >> shift), h * p.group + (row & (p.group - 1)), kept + 128 * wave, (uint16_t*)limbs, r, lane);
+        if (lane == 0) info[r] = RowInfo{v.x, v.y, 0.f, 0.f};
+      } else {                                                             // (rows behind the last: nothing)
+        for (int i = lane; i < 2 * (D / 32) * 4; i += 64) limbs[i / 4 * 64 + 16 * (i % 4) + r] = u32x4{0, 0, 0, 0};
+        if (lane == 0) info[r] = RowInfo{0.f, 0.f, 0.f, 0.f};
       }
     }
     __syncthreads();
-    TileQueries<D> tq;
-    tq.load(limbs, info, lane);
-    const bool keep = (int64_t)here * len <= kKeptLogits;
-    float m[4], sum[4];
+    SharedQueries<D> tq;
+    tq.limbs = limbs + lane;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) { m[r] = -INFINITY; sum[r] = 0.f; }
-    for (int pass = 0; pass < 2; ++pass) {
-      if (pass == 1) {
-        // rows' maxima and sums over all lanes and wavefronts
+    for (int r = 0; r < 4; ++r) {
+      tq.scale[r] = info[4 * (lane >> 4) + r].scale;
+      tq.sum_q[r] = info[4 * (lane >> 4) + r].sum_q;
+    }
+    const bool keep = (int64_t)here * len <= kKeptLogits;
+    const CodeBits bits;
+    // every step's logits, by rows 4 (lane / 16) + r and keys 16 t + lane % 16
+    auto steps = [&](auto use) {
+      for (int key0 = start; key0 < len; key0 += kStride) {
+        const bool masked = key0 + kWeightKeys > min(first_hidden + (row0 >> shift), len);
+        f32x4 x[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          u32x4 k[D / 32];
+          const f32x2 pair = key_codes<D>(codes, bits, t, key0, len, lane, k);
+          x[t] = tile_logits16<D>(tq, k, pair, key0 + 16 * t + (lane & 15), len, masked, first_hidden, shift, row0, lane);
+          asm volatile("" ::: "memory");                                   // (or the limbs would be kept in registers after all)
+        }
+        if (key0 + kStride < len) {
+          request_keys<D>(p, ids, h, lane, codes);
+          ids.fetch(pages, (key0 + 2 * kStride) / kWeightKeys, len);
+        }
+        use(key0, x);
+      }
+    };
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (keep) {
+      steps([&](int key0, const f32x4 (&x)[4]) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float top = row_allmax(m[r]), part = row_allsum(sum[r] * fast_exp2(m[r] - (top == -INFINITY ? 0.f : top)));
-          if ((lane & 15) == 0) stats[wave][4 * (lane >> 4) + r] = make_float2(top, part);
-        }
-        __syncthreads();
-        if (threadIdx.x < kWeightRows) {
-          const int r = threadIdx.x;
-          const float2 a = stats[0][r], c = stats[1][r], d = stats[2][r], e = stats[3][r];
-          const float top = fmaxf(fmaxf(a.x, c.x), fmaxf(d.x, e.x)), ref = top == -INFINITY ? 0.f : top;
-          const float all = (a.y * fast_exp2(a.x - ref) + c.y * fast_exp2(c.x - ref)) + (d.y * fast_exp2(d.x - ref) + e.y * fast_exp2(e.x - ref));
-          info[r].m = ref;
-          info[r].inv = all == 0.f ? 0.f : 1.f / all;
-        }
-        __syncthreads();
-        if (keep) {
-          for (int j = threadIdx.x; j < len; j += 256) {
-            float w = 0.f;
-            for (int r = 0; r < here; ++r) w = fmaf(fast_exp2(kept[r * len + j] - info[r].m), info[r].inv, w);
-            p.scores[record + j] = (prev ? prev[record + j] : 0.f) + w;
+          m[r] = fmaxf(fmaxf(m[r], fmaxf(x[0][r], x[1][r])), fmaxf(x[2][r], x[3][r]));
+          if (4 * (lane >> 4) + r < here) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const int key = key0 + 16 * t + (lane & 15);
+              if (key < len) kept[(4 * (lane >> 4) + r) * len + key] = x[t][r];
+            }
           }
-          break;
         }
-        keys.start(p, h, start, lane);
+      });
+    } else {
+      steps([&](int, const f32x4 (&x)[4]) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float top = fmaxf(fmaxf(m[r], fmaxf(x[0][r], x[1][r])), fmaxf(x[2][r], x[3][r])), ref = top == -INFINITY ? 0.f : top;
+          sum[r] = fmaf(sum[r], fast_exp2(m[r] - ref), (fast_exp2(x[0][r] - ref) + fast_exp2(x[1][r] - ref)) + (fast_exp2(x[2][r] - ref) + fast_exp2(x[3][r] - ref)));
+          m[r] = top;
+        }
+      });
+    }
+    // rows' maxima, and sums so far, over all lanes and wavefronts
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float top = row_allmax(m[r]), part = row_allsum(sum[r] * fast_exp2(m[r] - (top == -INFINITY ? 0.f : top)));
+      if ((lane & 15) == 0) stats[wave][4 * (lane >> 4) + r] = make_float2(top, part);
+    }
+    __syncthreads();
+    if (threadIdx.x < kWeightRows) {
+      float top = -INFINITY, all = 0.f;
+#pragma unroll
+      for (int w = 0; w < kStepWaves; ++w) top = fmaxf(top, stats[w][threadIdx.x].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int w = 0; w < kStepWaves; ++w) all += stats[w][threadIdx.x].y * fast_exp2(stats[w][threadIdx.x].x - ref);
+      info[threadIdx.x].m = ref;
+      info[threadIdx.x].inv = all == 0.f ? 0.f : 1.f / all;
+    }
+    __syncthreads();
+    if (keep) {
+      // weights in the logits' places and their sums, a row after the other
+      for (int r = 0; r < here; ++r) {
+        float part = 0.f;
+        const float ref = info[r].m;
+        for (int j = threadIdx.x; j < len; j += kThreads) {
+          const float w = fast_exp2(kept[r * len + j] - ref);
+          kept[r * len + j] = w;
+          part += w;
+        }
+        part = add_xor32(add_xor16(row_allsum(part)));
+        if (lane == 0) stats[wave][r].y = part;
       }
-      keys.each(start, [&](int key0, KeyCodes<D>& codes) {
-        u32x4 k[4][D / 32];
-        f32x2 pair[4];
-        f32x4 x[4];
-        take_keys<D>(codes, key0, len, lane, k, pair);
-        keys.next(p, h, key0, lane, codes);
-        const bool masked = key0 + kWeightKeys > min(first_hidden + (int)(row0 >> shift), len);
-        step_logits<D>(tq, k, pair, key0, len, masked, first_hidden, shift, (int)row0, lane, x);
-        if (pass == 0) {
+      __syncthreads();
+      if ((int)threadIdx.x < here) {
+        float all = 0.f;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float top = fmaxf(fmaxf(m[r], fmaxf(x[0][r], x[1][r])), fmaxf(x[2][r], x[3][r])), ref = top == -INFINITY ? 0.f : top;
-            sum[r] = fmaf(sum[r], fast_exp2(m[r] - ref), (fast_exp2(x[0][r] - ref) + fast_exp2(x[1][r] - ref)) + (fast_exp2(x[2][r] - ref) + fast_exp2(x[3][r] - ref)));
-            m[r] = top;
-          }
-          if (keep) {
+        for (int w = 0; w < kStepWaves; ++w) all += stats[w][threadIdx.x].y;
+        info[threadIdx.x].inv = all == 0.f ? 0.f : 1.f / all;
+      }
+      __syncthreads();
+      for (int j = threadIdx.x; j < len; j += kThreads) {
+        float w = 0.f;
+        for (int r = 0; r < here; ++r) w = fmaf(kept[r * len + j], info[r].inv, w);
+        p.scores[record + j] = (prev ? prev[record + j] : 0.f) + w;
+      }
+    } else {
+      first();
+      steps([&](int key0, const f32x4 (&x)[4]) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (4 * (lane >> 4) + r < here) {
+        for (int t = 0; t < 4; ++t) {
+          float w = 0.f;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                  const int key = key0 + 16 * t + (lane & 15);
-                  if (key < len) kept[(4 * (lane >> 4) + r) * len + key] = x[t][r];
-                }
-              }
-          }
-        } else {
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            float w = 0.f;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (4 * (lane >> 4) + r < here) w = fmaf(fast_exp2(x[t][r] - info[4 * (lane >> 4) + r].m), info[4 * (lane >> 4) + r].inv, w);
-            w = add_xor32(add_xor16(w));
-            const int key = key0 + 16 * t + lane;
-            if (lane < 16 && key < len) p.scores[record + key] = (prev ? prev[record + key] : 0.f) + w;
-          }
+          for (int r = 0; r < 4; ++r)
+            if (4 * (lane >> 4) + r < here) w = fmaf(fast_exp2(x[t][r] - info[4 * (lane >> 4) + r].m), info[4 * (lane >> 4) + r].inv, w);
+          w = add_xor32(add_xor16(w));
+          const int key = key0 + 16 * t + lane;
+          if (lane < 16 && key < len) p.scores[record + key] = (prev ? prev[record + key] : 0.f) + w;
         }
       });
     }
@@ -479,8 +528,8 @@ int launch_weights(const PromptParams& p, int D, hipStream_t st) {
   if (tiles > 0x7fffffffLL || (int64_t)p.n_kv_heads * chunks > 0x7fffffffLL || (tiles + kGroupTiles - 1) / kGroupTiles > 65535) return SAW_EINVAL;
   if (p.T_q <= p.B && (int64_t)p.B * p.n_kv_heads >= 256) {
     const dim3 grid(p.n_kv_heads, p.B);
-    if (D == 128) weight_step_kernel<128><<<grid, dim3(256), 0, st>>>(p);
-    else weight_step_kernel<64><<<grid, dim3(256), 0, st>>>(p);
+    if (D == 128) weight_step_kernel<128><<<grid, dim3(64 * kStepWaves), 0, st>>>(p);
+    else weight_step_kernel<64><<<grid, dim3(64 * kStepWaves), 0, st>>>(p);
     return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;
   }
   if (D == 128) launch_passes<128>(p, tiles, chunks, chunk_keys, st);
