@@ -521,12 +521,22 @@ static void launch_passes(const PromptParams& p, int64_t tiles, int chunks, int 
   weight_pass_kernel<D, false><<<dim3(p.n_kv_heads * chunks, p.B), dim3(256), 0, st>>>(p, tiles, chunk_keys);
 }
 
+// One launch where a sequence has about one query: short contexts, whose four launches take longer than a block of one compute unit for each
+// (sequence, kv head) (1 x 1000 tokens x 8 kv heads 13 us, 19 in two passes; 8 x 2000 20.5 and 22.9; x 4000 32 and 29), or batches that fill
+// the chip, the sooner if the logits fit shared memory (24 x 4000 36 and 58; 24 of 1000 to 8000 tokens, which do not, 97 and 71; 64 of 4000 to
+// 10000 186 and 280).  Several queries a sequence are level (32 x 5 over 1000 tokens 35 and 39, 8 x 5 29 and 23).
+static bool one_launch(const PromptParams& p) {
+  const int64_t items = (int64_t)p.B * p.n_kv_heads;
+  if (p.T_q > p.B) return false;
+  return (int64_t)p.bound * p.group <= kKeptLogits ? items >= 128 || p.bound <= 2048 : items >= 256;
+}
+
 int launch_weights(const PromptParams& p, int D, hipStream_t st) {
   const int64_t tiles = row_tiles(p.T_q, p.group, kWeightRows, p.B);
   const int chunks = weight_chunks(p.n_kv_heads, p.B, p.bound), unit = 4 * kWeightKeys;
   const int chunk_keys = (int)(((int64_t)(p.bound + chunks - 1) / chunks + unit - 1) / unit * unit);
   if (tiles > 0x7fffffffLL || (int64_t)p.n_kv_heads * chunks > 0x7fffffffLL || (tiles + kGroupTiles - 1) / kGroupTiles > 65535) return SAW_EINVAL;
-  if (p.T_q <= p.B && (int64_t)p.B * p.n_kv_heads >= 256) {
+  if (one_launch(p)) {
     const dim3 grid(p.n_kv_heads, p.B);
     if (D == 128) weight_step_kernel<128><<<grid, dim3(64 * kStepWaves), 0, st>>>(p);
     else weight_step_kernel<64><<<grid, dim3(64 * kStepWaves), 0, st>>>(p);
