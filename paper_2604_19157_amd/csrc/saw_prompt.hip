@@ -339,17 +339,17 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
     const int threads = 64 * NW;
     TilePages ids;
     auto request = [&](int t, Pieces& c) {
-      ids.ready(p);
+      ids.ready(p, h);
 #pragma unroll
       for (int j = 0; j < Pieces::kEach; ++j) {
         const int piece = j * threads + threadIdx.x, value = piece >= Pieces::kPieces / 2, i = value ? piece - Pieces::kPieces / 2 : piece;
         const int key = i / (D / 32);
-        const int64_t vec = ids.vector_of(p, h, key);
-        c.codes[j] = ((const u32x4*)((value ? p.v_codes : p.k_codes) + vec * (D / 2)))[i % (D / 32)];
-        c.pair[j] = ((const f32x2*)(value ? p.v_meta : p.k_meta))[vec];
+        const uint32_t tile = ids.tile_of(key);
+        c.codes[j] = ((const u32x4*)vector_codes<D>(value ? p.v_codes : p.k_codes, tile, key))[i % (D / 32)];
+        c.pair[j] = *vector_pair(value ? p.v_meta : p.k_meta, tile, key);
         if (t * kTileKeys + key >= len) c.pair[j] = f32x2{0.f, 0.f};         // (slots behind the end may hold anything)
       }
-      c.key_pair = ((const f32x2*)p.k_meta)[ids.vector_of(p, h, lane)];
+      c.key_pair = *vector_pair(p.k_meta, ids.tile_of(lane), lane);
       if (t * kTileKeys + lane >= len) c.key_pair = f32x2{0.f, 0.f};
     };
     auto put = [&](int buf, const Pieces& c) {                               // returns the tile's power of two
@@ -420,21 +420,22 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   f32x2 kpair[2], vpair[kPieces];
   TilePages ids;
   auto request = [&] {
-    ids.ready(p);
+    ids.ready(p, h);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const int64_t vec = ids.vector_of(p, h, 32 * kb + (lane & 31));
-      const u32x4* const src = (const u32x4*)(p.k_codes + vec * (D / 2) + (lane >> 5) * (D / 4));
+      const int key = 32 * kb + (lane & 31);
+      const uint32_t tile = ids.tile_of(key);
+      const u32x4* const src = (const u32x4*)(vector_codes<D>(p.k_codes, tile, key) + (lane >> 5) * (D / 4));
 #pragma unroll
       for (int i = 0; i < kWords / 4; ++i) kc[kb][i] = src[i];
-      kpair[kb] = ((const f32x2*)p.k_meta)[vec];
+      kpair[kb] = *vector_pair(p.k_meta, tile, key);
     }
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
-      const int piece = 64 * j + lane;
-      const int64_t vec = ids.vector_of(p, h, piece / kPieces);
-      vc[j] = ((const u32x4*)(p.v_codes + vec * (D / 2)))[piece % kPieces];
-      vpair[j] = ((const f32x2*)p.v_meta)[vec];
+      const int piece = 64 * j + lane, key = piece / kPieces;
+      const uint32_t tile = ids.tile_of(key);
+      vc[j] = ((const u32x4*)vector_codes<D>(p.v_codes, tile, key))[piece % kPieces];
+      vpair[j] = *vector_pair(p.v_meta, tile, key);
     }
   };
   if (t0 + wave < t1) {

@@ -78,21 +78,28 @@ constexpr int kTileKeys = 64;
 struct TilePages {
   int ahead;
   __device__ __forceinline__ void fetch(const int32_t* pages, int tile, int len) { ahead = pages[min(4 * tile + (int)(threadIdx.x & 3), (len - 1) >> 4)]; }
-  __device__ __forceinline__ void ready(const PromptParams& p) {
+  // (page, kv head) tiles of the pools, counted in 32 bits: 2^32 of them would be 2 TiB of codes and more
+  uint32_t at[4];
+  __device__ __forceinline__ void ready(const PromptParams& p, int h) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      id[i] = __builtin_amdgcn_readlane(ahead, i);
-      if (id[i] < 0 || id[i] >= p.num_pages) id[i] = 0;
+      const int id = __builtin_amdgcn_readlane(ahead, i);
+      at[i] = (uint32_t)(id < 0 || id >= p.num_pages ? 0 : id) * (uint32_t)p.n_kv_heads + (uint32_t)h;
     }
   }
-  int id[4];
-  // vector of key `key` of the tile in the pools of kv head h
-  __device__ __forceinline__ int64_t vector_of(const PromptParams& p, int h, int key) const {
+  __device__ __forceinline__ uint32_t tile_of(int key) const {              // of key `key` of the 64
     const int i = key >> 4;
-    const int page = i == 0 ? id[0] : i == 1 ? id[1] : i == 2 ? id[2] : id[3];
-    return ((int64_t)page * p.n_kv_heads + h) * 16 + (key & 15);
+    return i == 0 ? at[0] : i == 1 ? at[1] : i == 2 ? at[2] : at[3];
   }
 };
+// A vector's codes and its (scale, zero) pair, in pools of 16 vectors a tile.
+template <int D>
+__device__ __forceinline__ const uint8_t* vector_codes(const uint8_t* codes, uint32_t tile, int key) {
+  return codes + (uint64_t)tile * (8 * D) + (uint32_t)(key & 15) * (D / 2);
+}
+__device__ __forceinline__ const f32x2* vector_pair(const float* meta, uint32_t tile, int key) {
+  return (const f32x2*)((const char*)meta + (uint64_t)tile * 128 + (uint32_t)(key & 15) * 8);
+}
 
 // A tile of 64 keys in shared memory: rows of D 16-bit values in 16-byte chunks, the chunks of a row exchanged so that whatever a
 // read takes at once (256 bytes a clock) lies on different banks.  K: operand reads take one chunk of 16 rows.  V: transposing reads take 32

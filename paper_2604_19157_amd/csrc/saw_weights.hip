@@ -91,11 +91,11 @@ struct KeyCodes {
 };
 template <int D>
 __device__ __forceinline__ void request_keys(const PromptParams& p, TilePages& ids, int h, int lane, KeyCodes<D>& k) {
-  ids.ready(p);
+  ids.ready(p, h);
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    const int64_t vec = ids.vector_of(p, h, 16 * t + (lane & 15));
-    const uint8_t* const src = p.k_codes + vec * (D / 2) + (lane >> 4) * (D / 8);
+    const int key = 16 * t + (lane & 15);
+    const uint8_t* const src = vector_codes<D>(p.k_codes, ids.at[t], key) + (lane >> 4) * (D / 8);
     if constexpr (D == 128) {
       const u32x4 x = *(const u32x4*)src;
 #pragma unroll
@@ -105,7 +105,7 @@ __device__ __forceinline__ void request_keys(const PromptParams& p, TilePages& i
 #pragma unroll
       for (int i = 0; i < 2; ++i) k.w[t][i] = x[i];
     }
-    k.pair[t] = ((const f32x2*)p.k_meta)[vec];
+    k.pair[t] = *vector_pair(p.k_meta, ids.at[t], key);
   }
 }
 // A wavefront's steps, every `stride` keys: two of them on their way while a third is worked on, page ids one further ahead.
