@@ -302,7 +302,10 @@ static bool group_ok(int n_q_heads, int n_kv_heads) {
   const int g = n_q_heads / n_kv_heads;
   return g == 1 || g == 2 || g == 4 || g == 8;
 }
-static bool tokens_ok(int64_t T, int B) { return T >= 0 && T <= 0x7fffffffLL && B >= 1 && B <= 65535; }
+// (positions and rows are counted in 32 bits, with room for a tile behind the last)
+constexpr int64_t kMaxTokens = 0x7fff0000LL;
+static bool tokens_ok(int64_t T, int B) { return T >= 0 && T <= kMaxTokens && B >= 1 && B <= 65535; }
+static bool rows_ok(int64_t T, int Hq) { return T * Hq <= kMaxTokens; }
 static bool aligned4(const void* p) { return (((uintptr_t)p) & 3u) == 0; }
 
 static float log2_scale(float sm_scale, int head_dim) {
@@ -318,7 +321,7 @@ static int paged_args(const saw_cache_t* c, const void* q, int dtype, int64_t T,
   if (dtype != SAW_F16 && dtype != SAW_BF16) return SAW_EINVAL;
   if (!group_ok(Hq, c->n_kv_heads) || !tokens_ok(T, B) || max_pages < 1) return SAW_EINVAL;
   const int64_t cap = (int64_t)max_pages * c->page_size;
-  if (cap > 0x7fffffffLL || max_seq_len > cap) return SAW_EINVAL;
+  if (cap > 0x7fffffffLL || max_seq_len > cap || (max_seq_len <= 0 ? cap : max_seq_len) > kMaxTokens || !rows_ok(T, Hq)) return SAW_EINVAL;
   if (!isfinite(sm_scale)) return SAW_EINVAL;
   if (q_stride < (int64_t)Hq * c->head_dim || (q_stride & 7)) return SAW_EINVAL;
   if (!c->k_codes || !c->k_meta || (values && (!c->v_codes || !c->v_meta)) || !cu_q || !pt || !seq_lens || (T && (!q || !ws))) return SAW_ENULL;
@@ -773,7 +776,7 @@ int saw_kv16_paged_decode_attn(const saw_cache_t* c, const void* k_pages, const 
 }
 
 size_t saw_prompt_workspace_bytes(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, int64_t T_q, int32_t B, int64_t max_k_len) {
-  if ((head_dim != 64 && head_dim != 128) || !group_ok(n_q_heads, n_kv_heads) || !tokens_ok(T_q, B) || max_k_len < 0 || max_k_len > 0x7fffffffLL) return 0;
+  if ((head_dim != 64 && head_dim != 128) || !group_ok(n_q_heads, n_kv_heads) || !tokens_ok(T_q, B) || !rows_ok(T_q, n_q_heads) || max_k_len < 0 || max_k_len > kMaxTokens) return 0;
   return prompt_bytes(head_dim, n_q_heads, n_kv_heads, T_q, B, max_k_len);
 }
 
@@ -782,7 +785,7 @@ int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, 
                     const int32_t* cu_k, int32_t B, int64_t max_k_len, int32_t causal, float sm_scale, void* out, void* workspace,
                     size_t workspace_bytes, saw_stream_t stream) {
   if (dtype != SAW_F16 && dtype != SAW_BF16) return SAW_EINVAL;
-  if ((head_dim != 64 && head_dim != 128) || !group_ok(n_q_heads, n_kv_heads) || !tokens_ok(T_q, B) || !tokens_ok(T_k, B)) return SAW_EINVAL;
+  if ((head_dim != 64 && head_dim != 128) || !group_ok(n_q_heads, n_kv_heads) || !tokens_ok(T_q, B) || !tokens_ok(T_k, B) || !rows_ok(T_q, n_q_heads)) return SAW_EINVAL;
   if (!isfinite(sm_scale)) return SAW_EINVAL;
   const int64_t kv = (int64_t)n_kv_heads * head_dim;
   if (q_stride < (int64_t)n_q_heads * head_dim || k_stride < kv || v_stride < kv || ((q_stride | k_stride | v_stride) & 7)) return SAW_EINVAL;
@@ -799,7 +802,7 @@ int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, 
 }
 
 size_t saw_paged_prompt_workspace_bytes(const saw_cache_t* c, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len) {
-  if (!c || !shape_ok(c) || !group_ok(n_q_heads, c->n_kv_heads) || !tokens_ok(T, B) || max_seq_len < 1 || max_seq_len > 0x7fffffffLL) return 0;
+  if (!c || !shape_ok(c) || !group_ok(n_q_heads, c->n_kv_heads) || !tokens_ok(T, B) || !rows_ok(T, n_q_heads) || max_seq_len < 1 || max_seq_len > kMaxTokens) return 0;
   return paged_prompt_bytes(c->head_dim, n_q_heads, c->n_kv_heads, T, B, max_seq_len);
 }
 
@@ -820,7 +823,7 @@ int saw_paged_prompt_attn(const saw_cache_t* c, const void* q, int32_t dtype, in
 }
 
 size_t saw_attn_weights_workspace_bytes(const saw_cache_t* c, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len) {
-  if (!c || !shape_ok(c) || !group_ok(n_q_heads, c->n_kv_heads) || !tokens_ok(T, B) || max_seq_len < 1 || max_seq_len > 0x7fffffffLL) return 0;
+  if (!c || !shape_ok(c) || !group_ok(n_q_heads, c->n_kv_heads) || !tokens_ok(T, B) || !rows_ok(T, n_q_heads) || max_seq_len < 1 || max_seq_len > kMaxTokens) return 0;
   return weights_bytes(c->head_dim, n_q_heads, c->n_kv_heads, T, B, max_seq_len);
 }
 
@@ -840,7 +843,7 @@ int saw_paged_attn_weights(const saw_cache_t* c, const void* q, int32_t dtype, i
 }
 
 size_t saw_evict_workspace_bytes(const saw_cache_t* c, int32_t B, int64_t max_seq_len) {
-  if (!c || !shape_ok(c) || B < 1 || B > 65535 || max_seq_len < 1 || max_seq_len > 0x7fffffffLL) return 0;
+  if (!c || !shape_ok(c) || B < 1 || B > 65535 || max_seq_len < 1 || max_seq_len > kMaxTokens) return 0;
   return evict_bytes((int64_t)B * c->n_kv_heads, max_seq_len);
 }
 
@@ -851,7 +854,7 @@ int saw_evict_pages(const saw_cache_t* c, const float* scores, int64_t score_str
   if (!c) return SAW_ENULL;
   if (!shape_ok(c) || c->n_kv_heads > 65535 || B < 1 || B > 65535 || max_pages_per_seq < 1 || dst_pages_per_seq < 1) return SAW_EINVAL;
   const int64_t cap = (int64_t)max_pages_per_seq * c->page_size;
-  if (cap > 0x7fffffffLL || max_seq_len > cap) return SAW_EINVAL;
+  if (cap > 0x7fffffffLL || max_seq_len > cap || (max_seq_len <= 0 ? cap : max_seq_len) > kMaxTokens) return SAW_EINVAL;
   const int32_t bound = max_seq_len <= 0 ? (int32_t)cap : max_seq_len;
   if (budget < 1 || recent < 0 || recent > budget || (int64_t)dst_pages_per_seq * c->page_size < budget) return SAW_EINVAL;
   if (score_stride < bound || (scores_out && score_out_stride < budget)) return SAW_EINVAL;

@@ -75,7 +75,7 @@ struct CodePieces {
   static_assert(kEach * 64 * NW == kPieces, "whole pieces per thread");
   u32x4 codes[kEach];
   f32x2 pair[kEach];
-  f32x2 key_pair;           // of key `lane` of the tile, for the tile's exponent
+  f32x2 key_pair, value_pair;   // of key `lane` of the tile, for the tile's exponents
 };
 
 // c s - s z of the eight codes of a word, as 16-bit values in channel order
@@ -101,8 +101,40 @@ __device__ __forceinline__ void put_piece(char* tile, int row, int piece, u32x4 
   }
 }
 
-// The power of two that a tile's keys are divided by: the largest lands just below 2^15.
-__device__ __forceinline__ int key_exponent(float top) { return max((int)(__float_as_uint(top) >> 23) - 127, -100) - 14; }
+// The largest that a token's values can be, from its pair alone; zero if that is no number (it shows in the result by itself).
+__device__ __forceinline__ float largest_value(f32x2 pair) {
+  const float sz = pair.x * pair.y, most = fmaxf(fabsf(sz), fabsf(fmaf(15.f, pair.x, -sz)));
+  return most < INFINITY ? most : 0.f;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+// The power of two that dequantised keys, or values and the output sums with them, are divided by: the first tile's largest lands at 2^6,
+// and it is raised where a tile's would pass 2^15.  So fp16 holds any scale: a number is off by half a step (2^-11), or by 2^-31 of the
+// largest so far.  mine: the largest of a lane's keys.  (A power for every tile by itself would be a maximum over all lanes for each:
+// 2048 tokens over 16384 760 us, ragged fp16 chunks 174.)
+struct Unit {
+  int e = 0;
+  float limit = 0.f;
+  // true: raised by 2^by
+  __device__ __forceinline__ bool fit(float mine, bool first, int& by) {
+    if (!first && !__any(mine >= limit)) return false;
+    const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_xor32(max_xor16(row_allmax_positive(mine))))));
+    const int to = max((int)(__float_as_uint(top) >> 23) - 127, -100) - 6;
+    by = min(to - e, 126);
+    e = to;
+    limit = to + 15 > 127 ? INFINITY : power_of_two(to + 15);
+    return !first;
+  }
+  __device__ __forceinline__ float down() const { return power_of_two(-e); }
+  __device__ __forceinline__ float up() const { return power_of_two(e); }
+};
+template <int D>
+__device__ __forceinline__ void rescale(RowState<D>& st, float by) {
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st.o[t][r] *= by;
+}
 
 // The queries of a lane column as B operand: channels of k-step ks, half h and place i have bits (ks, h, i), h at bit HALF_BIT.  Those for
 // the INT4 pages are rotated here, in registers, and become fp16 times 2^-e (prompt_query_kernel does the same for a learned rotation);
@@ -148,10 +180,10 @@ __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token,
 }
 
 // The end of a wavefront's 32 rows: outputs, or partial records [split][row][D] and [split][row] (maximum, sum) where the keys are split
-// or a learned rotation has to be undone.
+// or a learned rotation has to be undone.  scale: of the rows' logits; unit: of the output sums.
 template <int D, int KV, int HALF_BIT>
 __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile& rt, int w0, int last, int row, int h, int64_t token, int head,
-                                            int k0, int len, int t0, int t1, const u32x4 (&qf)[D / 16], float scale, RowState<D>& st, int lane) {
+                                            int k0, int len, int t0, int t1, const u32x4 (&qf)[D / 16], float scale, float unit, RowState<D>& st, int lane) {
   constexpr bool kInt4 = KV == kKvInt4;
   const int shift = __builtin_ctz(p.group);
   const float sum = add_xor32(st.sum);
@@ -175,7 +207,7 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
       const int64_t mine = (int64_t)(rt.begin + tok_i) * p.n_q_heads + h * p.group + ((w0 + i) & (p.group - 1));
       const int sees = p.causal ? max(min(len, len - rt.n + tok_i + 1), 0) : len;
       const int end = min(sees, t1 * kTileKeys);
-      const float unit = __shfl(scale, i);
+      const float row_scale = __shfl(scale, i);
       float q[E], acc[E], m = -INFINITY, den = 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e) { q[e] = 0.f; acc[e] = 0.f; }
@@ -188,7 +220,7 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
             const uint32_t w = __shfl((int)qf[ks][d], i + 32 * half), x = v & 1 ? w >> 16 : w & 0xffffu;
-            if (v >> 1 == 4 * ks + d) q[e] = (KV == kKvBf16 ? bf16_to_f32(x) : f16_to_f32(x)) * unit;
+            if (v >> 1 == 4 * ks + d) q[e] = (KV == kKvBf16 ? bf16_to_f32(x) : f16_to_f32(x)) * row_scale;
           }
       }
       for (int j = t0 * kTileKeys; j < end; ++j) {
@@ -237,13 +269,13 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
-        *(f32x4*)(records + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) = f32x4{st.o[t][r], st.o[t][r + 1], st.o[t][r + 2], st.o[t][r + 3]};
+        *(f32x4*)(records + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) = f32x4{st.o[t][r] * unit, st.o[t][r + 1] * unit, st.o[t][r + 2] * unit, st.o[t][r + 3] * unit};
     return;
   }
   float inv = sum == 0.f ? 0.f : 1.f / sum;
   float x[D / 2];
 #pragma unroll
-  for (int i = 0; i < D / 2; ++i) x[i] = st.o[i / 16][i % 16];
+  for (int i = 0; i < D / 2; ++i) x[i] = kInt4 ? st.o[i / 16][i % 16] * unit : st.o[i / 16][i % 16];
   if (kInt4 && p.rot_v) {
     fwht_rows<D, 2>(x, p.had_block, lane);                               // (accumulators: the half is bit 2 of the channel)
     if (p.has_signs) sign_rows<D, 2>(x, p.signs, lane);
@@ -263,14 +295,13 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
 // Attention of packed rows.  A block takes 32 rows per wavefront and goes over the keys in tiles of 64, double-buffered in shared memory,
 // one barrier a tile.  Keys and values of 16 bits come from memory straight into the buffer (each transfer has a whole tile's
 // products to arrive in).  Those of the INT4 pages are requested a tile ahead into registers and written behind the tile's products:
-// K as fp16 times a power of two of the tile (its largest value just below 2^15, so that fp16 holds any scale; relative rounding 2^-11),
-// V as bf16 (2^-8, the output's own), each once per block and not once per row.
+// as fp16 times powers of two (Unit), each once per block and not once per row.
 template <int D, int KV, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
   constexpr int R = 32 * NW, kRow = 2 * D, kTile = kTileKeys * kRow, kInstr = kTile / 1024, kRpi = 1024 / kRow;
   constexpr bool kInt4 = KV == kKvInt4;
-  using M1 = typename std::conditional<KV == kKvBf16, MathBf16, MathF16>::type;      // queries and keys
-  using M2 = typename std::conditional<KV == kKvF16, MathF16, MathBf16>::type;       // weights and values
+  using M1 = typename std::conditional<KV == kKvBf16, MathBf16, MathF16>::type;      // queries and keys, weights and values
+  using M2 = M1;
   __shared__ __attribute__((aligned(1024))) char lds[2][2][kTile];       // [buffer][K, V]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % p.n_kv_heads;
@@ -302,6 +333,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) st.o[t][r] = 0.f;
 
+  Unit keys, values;                                                      // (INT4)
   auto products = [&](int buf, int t, float tile_scale) {
     if (t * kTileKeys >= wend) return;
     f32x16 s[2];
@@ -350,22 +382,22 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
         if (t * kTileKeys + key >= len) c.pair[j] = f32x2{0.f, 0.f};         // (slots behind the end may hold anything)
       }
       c.key_pair = *vector_pair(p.k_meta, ids.tile_of(lane), lane);
-      if (t * kTileKeys + lane >= len) c.key_pair = f32x2{0.f, 0.f};
+      c.value_pair = *vector_pair(p.v_meta, ids.tile_of(lane), lane);
+      if (t * kTileKeys + lane >= len) c.key_pair = c.value_pair = f32x2{0.f, 0.f};
     };
-    auto put = [&](int buf, const Pieces& c) {                               // returns the tile's power of two
-      float top = fmaxf(fabsf(c.key_pair.x * c.key_pair.y), fabsf(c.key_pair.x * (15.f - c.key_pair.y)));
-      if (!(top < INFINITY)) top = 0.f;
-      top = max_xor32(max_xor16(row_allmax_positive(top)));
-      const int ex = key_exponent(top);
-      const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+    auto put = [&](int buf, const Pieces& c, bool first) {                   // returns what the tile's logits are to be multiplied by
+      int by;
+      keys.fit(largest_value(c.key_pair), first, by);
+      if (values.fit(largest_value(c.value_pair), first, by)) rescale<D>(st, power_of_two(-by));
+      const float down = keys.down(), down_v = values.down();
 #pragma unroll
       for (int j = 0; j < Pieces::kEach; ++j) {
         const int piece = j * threads + threadIdx.x, value = piece >= Pieces::kPieces / 2, i = value ? piece - Pieces::kPieces / 2 : piece;
         const float s = c.pair[j].x, sz = s * c.pair[j].y;
-        if (value) put_piece<M2, D, true>(lds[buf][1], i / (D / 32), i % (D / 32), c.codes[j], s, sz);
+        if (value) put_piece<M2, D, true>(lds[buf][1], i / (D / 32), i % (D / 32), c.codes[j], s * down_v, sz * down_v);
         else put_piece<M1, D, false>(lds[buf][0], i / (D / 32), i % (D / 32), c.codes[j], s * down, sz * down);
       }
-      return __uint_as_float((uint32_t)(127 + ex) << 23);
+      return keys.up();
     };
     Pieces c;
     float tile_scale = 1.f;
@@ -373,7 +405,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
       ids.fetch(pages, t0, len);
       request(t0, c);
       ids.fetch(pages, t0 + 1, len);
-      tile_scale = put(0, c);
+      tile_scale = put(0, c, true);
     }
     for (int t = t0; t < t1; ++t) {
       const int buf = (t - t0) & 1;
@@ -383,10 +415,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
         ids.fetch(pages, t + 2, len);
       }
       products(buf, t, scale * tile_scale);
-      if (t + 1 < t1) tile_scale = put(buf ^ 1, c);
+      if (t + 1 < t1) tile_scale = put(buf ^ 1, c, false);
     }
   }
-  finish_rows<D, KV, 3>(p, rt, w0, last, row, h, token, head, k0, len, t0, t1, qf, scale, st, lane);
+  finish_rows<D, KV, 3>(p, rt, w0, last, row, h, token, head, k0, len, t0, t1, qf, scale, kInt4 ? values.up() : 1.f, st, lane);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
@@ -452,6 +484,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) st.o[t][r] = 0.f;
 
+  Unit keys, values;
   for (int t = t0 + wave; t < t1; t += NW) {
     // (slots behind the end may hold anything)
     float top = 0.f, s[2], sz[2];
@@ -460,11 +493,17 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
       const bool there = t * kTileKeys + 32 * kb + (lane & 31) < len;
       s[kb] = there ? kpair[kb].x : 0.f;
       sz[kb] = there ? kpair[kb].x * kpair[kb].y : 0.f;
-      const float most = fmaxf(fabsf(sz[kb]), fabsf(fmaf(15.f, s[kb], -sz[kb])));
-      if (most < INFINITY) top = fmaxf(top, most);
+      if (there) top = fmaxf(top, largest_value(kpair[kb]));
     }
-    const int ex = key_exponent(max_xor16(row_allmax_positive(top)));
-    const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+    int by;
+    keys.fit(top, t == t0 + wave, by);
+    const float down = keys.down();
+    top = 0.f;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j)
+      if (t * kTileKeys + (64 * j + lane) / kPieces < len) top = fmaxf(top, largest_value(vpair[j]));
+    if (values.fit(top, t == t0 + wave, by)) rescale<D>(st, power_of_two(-by));
+    const float down_v = values.down();
     f32x16 x[2];
     u32x4 pf[4];
 #pragma unroll
@@ -479,7 +518,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     for (int j = 0; j < kPieces; ++j) {
       const int key = (64 * j + lane) / kPieces;
       const bool there = t * kTileKeys + key < len;
-      put_piece<MathBf16, D, true>(mine, key, lane % kPieces, vc[j], there ? vpair[j].x : 0.f, there ? vpair[j].x * vpair[j].y : 0.f);
+      put_piece<MathF16, D, true>(mine, key, lane % kPieces, vc[j], there ? vpair[j].x * down_v : 0.f, there ? vpair[j].x * vpair[j].y * down_v : 0.f);
     }
     wave_sync();
     if (t + NW < t1) {
@@ -487,11 +526,12 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
       ids.fetch(pages, t + 2 * NW, len);
     }
     if ((t + 1) * kTileKeys > kfull) tile_mask(x, sees - t * kTileKeys, lane);
-    tile_weights<D, MathBf16>(x, scale * __uint_as_float((uint32_t)(127 + ex) << 23), st, pf);
-    tile_values<D, MathBf16>(mine, pf, st, lane);
+    tile_weights<D, MathF16>(x, scale * keys.up(), st, pf);
+    tile_values<D, MathF16>(mine, pf, st, lane);
   }
   // the other wavefronts' states join the first's
   wave_sync();
+  rescale<D>(st, values.up());
   if (wave > 0) {
 #pragma unroll
     for (int i = 0; i < D / 2; i += 4) *(f32x4*)(mine + i * 256 + 16 * lane) = f32x4{st.o[i / 16][i % 16], st.o[i / 16][i % 16 + 1], st.o[i / 16][i % 16 + 2], st.o[i / 16][i % 16 + 3]};
@@ -505,8 +545,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   const float ref = m == -INFINITY ? 0.f : m;
   const float alpha = fast_exp2(st.m - ref);
   st.sum *= alpha;
-#pragma unroll
-  for (int i = 0; i < D / 2; ++i) st.o[i / 16][i % 16] *= alpha;
+  rescale<D>(st, alpha);
   for (int w = 1; w < NW; ++w) {
     const float a = fast_exp2(join[w][lane].x - ref);
     st.sum = fmaf(a, join[w][lane].y, st.sum);
@@ -518,7 +557,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     }
   }
   st.m = m;
-  finish_rows<D, kKvInt4, kHalfBit>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, qf, scale, st, lane);
+  finish_rows<D, kKvInt4, kHalfBit>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, qf, scale, 1.f, st, lane);
 }
 
 // Joins the partial records of a row: one wavefront a row.

@@ -3,7 +3,7 @@
 Bounds.  With u the half step of the output's type (bf16 2^-8, fp16 2^-11), w the exact weights of a row, A = sum_j w_j |v_j| per channel and
 e the most that a logit can be off, an output is off by at most
     u |o| + A (u_p + exp(2 e) - 1 + 2^-20 + n 2^-22)          (1 + a few u for products of these)
-  u_p      rounding of a weight before the product with V (its type's half step; over the INT4 pages weight and value enter as bf16, 2^-7)
+  u_p      rounding of a weight before the product with V (its type's half step; over the INT4 pages weight and value enter as fp16, 2^-10)
   2 e      in the exponent: a weight's logit and its sum's, off in opposite directions
   2^-20    the exponential and the division;  n 2^-22   sums of n terms in fp32, of weights and of the product (each at most n 2^-23)
 and e = scale (sum_c |q_c k_c|) (d 2^-23 + u_q) + 2^-22 |logit|, u_q the rounding of query and key

@@ -87,8 +87,10 @@ class Case:
             # 2^-24 s |z| + 2^-24 |x| <= 2^-23 s (|z| + 15) before it is rounded to 16 bits, also where c = z)
             off = [2.0 ** -23 * self.step(x, b, g, L) for x in "kv"]
             q = np.sqrt(self.d) * np.linalg.norm(self.q[rows, j].double().numpy(), axis=1) * self.d ** -0.5    # scale sum |q~| at most
-            tol[rows, j] = pc.bound(o, A, top, big, L, self.d, u, 2.0 ** -7, 2.0 ** -10 + 2.0 ** -18, q * off[0].max())
-            tol[rows, j] += 1.01 * np.sqrt(max(mix, 1) if self.mask & 2 else 1) * (w @ off[1])[:, None]
+            tol[rows, j] = pc.bound(o, A, top, big, L, self.d, u, 2.0 ** -10, 2.0 ** -10 + 2.0 ** -18, q * off[0].max())
+            # (and fp16's smallest step: a weight of less than 2^-14 of the row's largest is off by 2^-25 of it, a value by 2^-31 of the largest)
+            least = (2.0 ** -25 * w.max(1) * np.abs(v).max(1).sum() + 2.0 ** -31 * self.step("v", b, g, L).max())[:, None]
+            tol[rows, j] += 1.01 * np.sqrt(max(mix, 1) if self.mask & 2 else 1) * ((w @ off[1])[:, None] + least)
         return out, tol
 
 
@@ -132,6 +134,26 @@ def test_queries_in_front_of_all_tokens_and_empty_sequences(saw):
     want, tol = c.attention()
     pc.check(out[:12], want, tol)
     assert torch.count_nonzero(out[:4]) == 0 and torch.count_nonzero(out[6:10]) == 0 and bool((out[12:] == 5).all())
+
+
+@pytest.mark.parametrize("n", [3, 80])
+def test_scales_of_very_different_size(saw, n):
+    """Scales over forty powers of two within a sequence, growing and shrinking along it; zero vectors between them."""
+    for power in (1e-12, 1e9):
+        c = Case(saw, [n], [400], d=128, h=1, seed=6)
+        steps = np.geomspace(1, power, 400).astype(np.float32)
+        for pos in range(400):
+            page, slot = c.pt[0, pos // 16], pos % 16
+            for w in "kv":
+                c.ref[w + "_meta"][page, :, slot, 0] *= steps[pos] if w == "v" else np.float32(1e-3) * steps[pos] ** np.float32(0.25)
+            if pos % 50 == 7:
+                c.ref["v_meta"][page, :, slot] = (1, 0)
+                c.ref["v_codes"][page, :, slot] = 0
+        for name in ("k_meta", "v_meta", "v_codes"):
+            t = getattr(c.cache, name)
+            t.copy_(torch.from_numpy(np.ascontiguousarray(c.ref[name])).reshape(t.shape))
+        want, tol = c.attention()
+        pc.check(saw.paged_prompt_attn(c.cache, *c.args), want, tol, power)
 
 
 def test_agrees_with_the_decode_call(saw):

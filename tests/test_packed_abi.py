@@ -34,7 +34,7 @@ PROMPT = dict(q=A, k=A, v=A, dtype=2, head_dim=128, n_q_heads=32, n_kv_heads=8, 
 
 @pytest.mark.parametrize("change,code", [
     (dict(dtype=3), EINVAL), (dict(dtype=0), EINVAL), (dict(head_dim=96), EINVAL), (dict(n_q_heads=24), EINVAL), (dict(n_q_heads=20), EINVAL),
-    (dict(n_kv_heads=0), EINVAL), (dict(n_q_heads=0), EINVAL), (dict(T_q=-1), EINVAL), (dict(T_k=-1), EINVAL), (dict(T_q=1 << 31), EINVAL), (dict(B=0), EINVAL),
+    (dict(n_kv_heads=0), EINVAL), (dict(n_q_heads=0), EINVAL), (dict(T_q=-1), EINVAL), (dict(T_k=-1), EINVAL), (dict(T_q=1 << 31), EINVAL), (dict(T_q=1 << 26), EINVAL), (dict(T_k=(1 << 31) - 1), EINVAL), (dict(B=0), EINVAL),
     (dict(B=65536), EINVAL), (dict(q_stride=4088), EINVAL), (dict(q_stride=4100), EINVAL), (dict(k_stride=1016), EINVAL), (dict(v_stride=1020), EINVAL),
     (dict(k_stride=1028), EINVAL), (dict(sm_scale=math.nan), EINVAL), (dict(sm_scale=math.inf), EINVAL), (dict(q=None), ENULL), (dict(k=None), ENULL),
     (dict(v=None), ENULL), (dict(cu_q=None), ENULL), (dict(cu_k=None), ENULL), (dict(out=None), ENULL), (dict(workspace=None), ENULL), (dict(q=A + 8), EINVAL),
@@ -46,7 +46,7 @@ def test_prompt_refusals(saw, change, code):
 
 PAGED = dict(cache=None, q=A, dtype=2, T=100, q_stride=4096, n_q_heads=32, cu_q=A, B=2, page_table=A, max_pages=100, seq_lens=A, max_seq_len=0, sm_scale=0.0,
              out=A, workspace=A, workspace_bytes=1 << 40, stream=None)
-SHARED = [(dict(dtype=3), EINVAL), (dict(n_q_heads=12), EINVAL), (dict(n_q_heads=128), EINVAL), (dict(T=-1), EINVAL), (dict(q_stride=4095), EINVAL),
+SHARED = [(dict(dtype=3), EINVAL), (dict(n_q_heads=12), EINVAL), (dict(n_q_heads=128), EINVAL), (dict(T=-1), EINVAL), (dict(T=1 << 26), EINVAL), (dict(max_pages=(1 << 27) - 1), EINVAL), (dict(q_stride=4095), EINVAL),
           (dict(q_stride=4104 - 4), EINVAL), (dict(B=0), EINVAL), (dict(B=65536), EINVAL), (dict(max_pages=0), EINVAL), (dict(max_pages=1 << 28), EINVAL),
           (dict(max_seq_len=1601), EINVAL), (dict(sm_scale=math.nan), EINVAL), (dict(q=None), ENULL), (dict(cu_q=None), ENULL), (dict(page_table=None), ENULL),
           (dict(seq_lens=None), ENULL), (dict(workspace=None), ENULL), (dict(q=A + 8), EINVAL), (dict(workspace=A + 8), EINVAL), (dict(workspace_bytes=8), EWORKSPACE)]
