@@ -21,7 +21,7 @@ def saw():
 
 
 class Case:
-    def __init__(self, saw, n, lens, Hkv=2, G=4, d=128, h=128, mask=3, dtype=BF, signs=False, dense=False, seed=0):
+    def __init__(self, saw, n, lens, Hkv=2, G=4, d=128, h=128, mask=3, dtype=BF, signs=False, dense=False, seed=0, offsets=True):
         """A cache of random codes, scales and zero-points (any number is a stored value), queries scaled so that logits spread over a few units."""
         rng = np.random.default_rng(seed)
         self.n, self.lens, self.h, self.mask, self.d, self.G, self.Hkv = n, np.asarray(lens, np.int32), h, mask, d, G, Hkv
@@ -38,7 +38,7 @@ class Case:
             self.ref[w + "_codes"][...] = rng.integers(0, 256, self.ref[w + "_codes"].shape)
             m = self.ref[w + "_meta"]
             m[..., 0] = rng.uniform(0.02, 0.3, m.shape[:-1])
-            m[..., 1] = np.where(rng.random(m.shape[:-1]) < 0.1, rng.integers(-60, 80, m.shape[:-1]), rng.integers(4, 12, m.shape[:-1]))
+            m[..., 1] = np.where(rng.random(m.shape[:-1]) < (0.1 if offsets else 0), rng.integers(-60, 80, m.shape[:-1]), rng.integers(4, 12, m.shape[:-1]))
         self.signs = synth.random_signs(d, seed + 1) if signs else None
         self.dense = synth.random_orthogonal(d, seed + 2) if dense else None
         self.cu = pc.offsets(n)
@@ -104,6 +104,20 @@ def test_attention(saw, n, lens, d, G, dtype):
     c = Case(saw, n, lens, G=G, d=d, h=d, dtype=dtype, seed=len(n) + d)
     want, tol = c.attention()
     pc.check(saw.paged_prompt_attn(c.cache, *c.args), want, tol)
+
+
+@pytest.mark.parametrize("n,lens", [([1, 5], [200, 333]), ([150], [400])], ids=str)
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d,h", [(128, 128), (64, 16), (128, 1)])
+def test_attention_over_ordinary_codes(saw, d, h, dtype, n, lens):
+    """Zero-points inside the codes' range, as the store writes them for values of both signs: the roundings are small against the values, so
+    that the mean error is held to one and a half half steps of fp16 on top of the output's own (roundings of query, key, weight and value of like size)."""
+    c = Case(saw, n, lens, d=d, h=h, dtype=dtype, seed=11, offsets=False)
+    want, tol = c.attention()
+    got = saw.paged_prompt_attn(c.cache, *c.args)
+    pc.check(got, want, tol)
+    off = np.linalg.norm(got.double().cpu().numpy() - want) / np.linalg.norm(want)
+    assert off < pc.U[dtype] + 1.5 * 2.0 ** -11 * max(1.0, np.abs(want).max() / np.abs(want).mean()) ** 0.5
 
 
 OPTIONS = [dict(h=1), dict(h=16), dict(h=32, mask=1), dict(h=64, mask=2), dict(h=128, signs=True), dict(h=128, dense=True),
