@@ -278,7 +278,14 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const f32x2 mi = *(const f32x2*)&info[4 * (lane >> 4) + r].m;
-          const bool there = row0 + 4 * (lane >> 4) + r < rows;
+          bool there = row0 + 4 * (lane >> 4) + r < rows;
+          if (masked && __any(mi.y != mi.y)) {
+            // (a row whose sum is no number: nor is any of its weights, but for those of the keys that it does not see)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+              if (there && mi.y != mi.y && x[t][r] != -INFINITY) total[t] = mi.y;
+            there = there && mi.y == mi.y;
+          }
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             const float w = fast_exp2(x[t][r] - mi.x) * mi.y;
@@ -469,9 +476,14 @@ __global__ __launch_bounds__(64 * kStepWaves, 4) void weight_step_kernel(PromptP
         float all = 0.f;
 #pragma unroll
         for (int w = 0; w < kStepWaves; ++w) all += stats[w][threadIdx.x].y;
-        info[threadIdx.x].inv = all == 0.f ? 0.f : 1.f / all;
+        info[threadIdx.x].inv = all == 0.f ? 0.f : all == all ? 1.f / all : 1.f;
+        if (all != all) info[threadIdx.x].m = all;
       }
       __syncthreads();
+      // (weights of a row whose sum is no number, as above)
+      for (int r = 0; r < here; ++r)
+        if (info[r].m != info[r].m)
+          for (int j = threadIdx.x; j < min(len, first_hidden + ((row0 + r) >> shift)); j += kThreads) kept[r * len + j] = info[r].m;
       for (int j = threadIdx.x; j < len; j += kThreads) {
         float w = 0.f;
         for (int r = 0; r < here; ++r) w = fmaf(kept[r * len + j], info[r].inv, w);
@@ -485,7 +497,8 @@ __global__ __launch_bounds__(64 * kStepWaves, 4) void weight_step_kernel(PromptP
           float w = 0.f;
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (4 * (lane >> 4) + r < here) w = fmaf(fast_exp2(x[t][r] - info[4 * (lane >> 4) + r].m), info[4 * (lane >> 4) + r].inv, w);
+            if (4 * (lane >> 4) + r < here && x[t][r] != -INFINITY)
+              w = fmaf(fast_exp2(x[t][r] - info[4 * (lane >> 4) + r].m), info[4 * (lane >> 4) + r].inv, w);
           w = add_xor32(add_xor16(w));
           const int key = key0 + 16 * t + lane;
           if (lane < 16 && key < len) p.scores[record + key] = (prev ? prev[record + key] : 0.f) + w;

@@ -335,6 +335,24 @@ def test_weights_of_slots_that_are_not_seen(saw, bad):
     assert torch.equal(saw.paged_attn_weights(c.cache, *c.args, max_seq_len=32), clean)
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("lens", [[60, 30], [5000, 30], [60] + [30] * 40, [5000] + [30] * 40], ids=len)
+def test_weights_of_a_query_that_is_no_number(saw, bad, lens):
+    """It shows at the positions that it sees and nowhere else."""
+    n = [10, 2] + [0] * (len(lens) - 2)
+    c = Case(saw, n, lens, Hkv=8, seed=5)
+    want, tol = _scores(c, np.zeros((len(n), 8, max(lens)), np.float32))
+    only = Case(saw, [5, 2] + n[2:], lens, Hkv=8, seed=5)                  # the queries behind the fifth, alone
+    only.q = torch.cat([c.q[5:10], c.q[10:]])
+    behind, tol_behind = _scores(only, np.zeros((len(n), 8, max(lens)), np.float32))
+    c.args[0][4] = bad
+    got = saw.paged_attn_weights(c.cache, *c.args, max_seq_len=max(lens)).cpu()
+    sees = lens[0] - 5                                                     # positions that query 4 of 10 sees
+    assert bool(torch.isnan(got[0, :, :sees]).all())
+    pc.check(got[0, :, sees:lens[0]], behind[0, :, sees:lens[0]], tol_behind[0, :, sees:lens[0]])
+    pc.check(got[1:], want[1:], tol[1:])
+
+
 @pytest.mark.parametrize("n,lens,G", [([1, 1], [5000, 9000], 4), ([1], [20000], 8), ([2, 33], [7000, 3001], 2), ([1] * 40, list(range(100, 1300, 30)), 4)], ids=str)
 def test_long_contexts_split(saw, n, lens, G):
     c = Case(saw, n, lens, G=G, seed=2)
