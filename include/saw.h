@@ -401,8 +401,8 @@ int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, 
  *   out         device, dense [T][n_q_heads][head_dim] of dtype, 16-byte aligned; rows of no sequence are left as they were.
  *   workspace   at least saw_paged_prompt_workspace_bytes(...) bytes, 16-byte aligned, one per call in flight.
  * Rotated queries and dequantised keys enter their product as fp16 times powers of two (a query's of its row, keys' of the
- * sequence), weights and dequantised values theirs as fp16 too: half a step each, 2^-11, and 2^-25 of the largest value that a row
- * meets; everything between and all sums are fp32.  Page ids of visible tokens outside
+ * sequence), weights and dequantised values theirs as fp16 too: half a step each, 2^-11, and 2^-19 of the largest value that a row
+ * meets, whatever the size of those that it does not see; everything between and all sums are fp32.  Page ids of visible tokens outside
  * [0, num_pages) are read as page 0.  Alignment of the pools as for the decode calls.  T == 0 is a no-op.
  */
 size_t saw_paged_prompt_workspace_bytes(const saw_cache_t* cache, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len);

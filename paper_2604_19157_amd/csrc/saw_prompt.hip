@@ -108,17 +108,28 @@ __device__ __forceinline__ float largest_value(f32x2 pair) {
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
+__device__ __forceinline__ float wave_max(float x) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_xor32(max_xor16(row_allmax_positive(x))))));
+}
+
 // The power of two that dequantised keys, or values and the output sums with them, are divided by: the first tile's largest lands at 2^6,
 // and it is raised where a tile's would pass 2^15.  So fp16 holds any scale: a number is off by half a step (2^-11), or by 2^-31 of the
-// largest so far.  mine: the largest of a lane's keys.  (A power for every tile by itself would be a maximum over all lanes for each:
-// 2048 tokens over 16384 760 us, ragged fp16 chunks 174.)
+// largest so far.  (A power for every tile by itself would be a maximum over all lanes for each: 2048 tokens over 16384 760 us, ragged
+// fp16 chunks 174.)
+//   Rows need not see the key that sets the unit.  `floor` is no more than the largest that any row met (of keys that all of the
+// wavefront's rows see); where the unit is set by one 2^12 times as large the sums are given up, and finish_rows takes the rows again key
+// by key.
 struct Unit {
   int e = 0;
-  float limit = 0.f;
-  // true: raised by 2^by
-  __device__ __forceinline__ bool fit(float mine, bool first, int& by) {
+  float limit = 0.f, floor = 0.f;
+  bool lost = false;
+  // mine: the largest of the lane's keys; all_see: of those that every row sees, `whole`: all of the tile.  true: raised by 2^by
+  template <typename F>
+  __device__ __forceinline__ bool fit(float mine, bool first, bool whole, int& by, F all_see) {
     if (!first && !__any(mine >= limit)) return false;
-    const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_xor32(max_xor16(row_allmax_positive(mine))))));
+    const float top = wave_max(mine);
+    floor = whole ? top : fmaxf(floor, wave_max(all_see()));
+    lost = lost || top > 4096.f * floor;
     const int to = max((int)(__float_as_uint(top) >> 23) - 127, -100) - 6;
     by = min(to - e, 126);
     e = to;
@@ -385,10 +396,13 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
       c.value_pair = *vector_pair(p.v_meta, ids.tile_of(lane), lane);
       if (t * kTileKeys + lane >= len) c.key_pair = c.value_pair = f32x2{0.f, 0.f};
     };
-    auto put = [&](int buf, const Pieces& c, bool first) {                   // returns what the tile's logits are to be multiplied by
+    const int seen = max(sees_of(w0), t0 * kTileKeys + 1);                   // keys in front of it are seen by every row that sees any
+    auto put = [&](int buf, const Pieces& c, int t) {                        // returns what the tile's logits are to be multiplied by
+      const bool whole = (t + 1) * kTileKeys <= seen, mine = t * kTileKeys + lane < seen;
+      const float key = largest_value(c.key_pair), value = largest_value(c.value_pair);
       int by;
-      keys.fit(largest_value(c.key_pair), first, by);
-      if (values.fit(largest_value(c.value_pair), first, by)) rescale<D>(st, power_of_two(-by));
+      keys.fit(key, t == t0, whole, by, [&] { return mine ? key : 0.f; });
+      if (values.fit(value, t == t0, whole, by, [&] { return mine ? value : 0.f; })) rescale<D>(st, power_of_two(-by));
       const float down = keys.down(), down_v = values.down();
 #pragma unroll
       for (int j = 0; j < Pieces::kEach; ++j) {
@@ -405,7 +419,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
       ids.fetch(pages, t0, len);
       request(t0, c);
       ids.fetch(pages, t0 + 1, len);
-      tile_scale = put(0, c, true);
+      tile_scale = put(0, c, t0);
     }
     for (int t = t0; t < t1; ++t) {
       const int buf = (t - t0) & 1;
@@ -415,9 +429,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
         ids.fetch(pages, t + 2, len);
       }
       products(buf, t, scale * tile_scale);
-      if (t + 1 < t1) tile_scale = put(buf ^ 1, c, false);
+      if (t + 1 < t1) tile_scale = put(buf ^ 1, c, t + 1);
     }
   }
+  if (keys.lost || values.lost) st.o[0][0] = NAN;
   finish_rows<D, KV, 3>(p, rt, w0, last, row, h, token, head, k0, len, t0, t1, qf, scale, kInt4 ? values.up() : 1.f, st, lane);
 }
 
@@ -485,24 +500,35 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     for (int r = 0; r < 16; ++r) st.o[t][r] = 0.f;
 
   Unit keys, values;
+  const int seen = max(sees_of(rt.row0), (t0 + wave) * kTileKeys + 1);
   for (int t = t0 + wave; t < t1; t += NW) {
     // (slots behind the end may hold anything)
-    float top = 0.f, s[2], sz[2];
+    float s[2], sz[2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const bool there = t * kTileKeys + 32 * kb + (lane & 31) < len;
       s[kb] = there ? kpair[kb].x : 0.f;
       sz[kb] = there ? kpair[kb].x * kpair[kb].y : 0.f;
-      if (there) top = fmaxf(top, largest_value(kpair[kb]));
     }
-    int by;
-    keys.fit(top, t == t0 + wave, by);
-    const float down = keys.down();
-    top = 0.f;
+    auto largest_key = [&](int end) {
+      float top = 0.f;
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j)
-      if (t * kTileKeys + (64 * j + lane) / kPieces < len) top = fmaxf(top, largest_value(vpair[j]));
-    if (values.fit(top, t == t0 + wave, by)) rescale<D>(st, power_of_two(-by));
+      for (int kb = 0; kb < 2; ++kb)
+        if (t * kTileKeys + 32 * kb + (lane & 31) < end) top = fmaxf(top, largest_value(kpair[kb]));
+      return top;
+    };
+    auto largest_of_values = [&](int end) {
+      float top = 0.f;
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j)
+        if (t * kTileKeys + (64 * j + lane) / kPieces < end) top = fmaxf(top, largest_value(vpair[j]));
+      return top;
+    };
+    int by;
+    const bool whole = (t + 1) * kTileKeys <= seen;
+    keys.fit(largest_key(len), t == t0 + wave, whole, by, [&] { return largest_key(seen); });
+    const float down = keys.down();
+    if (values.fit(largest_of_values(len), t == t0 + wave, whole, by, [&] { return largest_of_values(seen); })) rescale<D>(st, power_of_two(-by));
     const float down_v = values.down();
     f32x16 x[2];
     u32x4 pf[4];
@@ -532,6 +558,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   // the other wavefronts' states join the first's
   wave_sync();
   rescale<D>(st, values.up());
+  if (keys.lost || values.lost) st.o[0][0] = NAN;
   if (wave > 0) {
 #pragma unroll
     for (int i = 0; i < D / 2; i += 4) *(f32x4*)(mine + i * 256 + 16 * lane) = f32x4{st.o[i / 16][i % 16], st.o[i / 16][i % 16 + 1], st.o[i / 16][i % 16 + 2], st.o[i / 16][i % 16 + 3]};

@@ -200,6 +200,23 @@ def test_slots_and_pages_that_are_not_seen_count_for_nothing(saw, bad):
         pool.copy_(keep)
 
 
+@pytest.mark.parametrize("size", [1e-30, 1e4, 1e12, 1e30])
+@pytest.mark.parametrize("n,lens", [([40, 3], [50, 21]), ([40, 3], [330, 21]), ([5, 3], [50, 21]), ([5, 3], [330, 700]), ([5], [4000]), ([300], [300])], ids=str)
+def test_the_size_of_tokens_that_are_not_seen_counts_for_nothing(saw, n, lens, size):
+    """A token of any finite scale: the queries in front of it give what they give without it."""
+    c = Case(saw, n, lens, h=1)
+    want, tol = c.attention()
+    first = int(c.cu[1]) // 2                       # of sequence 0: queries from here on see the token at its end
+    at = lens[0] - n[0] + first
+    for pool in (c.cache.k_meta, c.cache.v_meta):
+        keep = pool.clone()
+        pool[c.pt[0, at // 16], :, at % 16, 0] = size
+        got = saw.paged_prompt_attn(c.cache, *c.args)
+        pc.check(got[:first], want[:first], tol[:first])
+        pc.check(got[n[0]:], want[n[0]:], tol[n[0]:])
+        pool.copy_(keep)
+
+
 def test_page_ids_out_of_range_read_page_0(saw):
     c = Case(saw, [20], [60])
     pt = c.args[2].clone()
