@@ -88,8 +88,8 @@ struct TilePages {
     }
   }
   __device__ __forceinline__ uint32_t tile_of(int key) const {              // of key `key` of the 64
-    const int i = key >> 4;
-    return i == 0 ? at[0] : i == 1 ? at[1] : i == 2 ? at[2] : at[3];
+    const uint32_t lo = key & 16 ? at[1] : at[0], hi = key & 16 ? at[3] : at[2];
+    return key & 32 ? hi : lo;
   }
 };
 // A vector's codes and its (scale, zero) pair, in pools of 16 vectors a tile.
