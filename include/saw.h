@@ -370,7 +370,8 @@ int saw_flatten_dequant(const saw_cache_t* cache, const int32_t* page_table,
  *               (strides: at least a token's elements, multiples of 8; bases 16-byte aligned)
  *   cu_q, cu_k  device, [B + 1] int32, not decreasing: sequence b has the queries cu_q[b] .. cu_q[b + 1] - 1 and the keys
  *               cu_k[b] .. cu_k[b + 1] - 1.  Either number may be zero.  Offsets are clamped to [0, T_q] and [0, T_k].
- *   max_k_len   host-side upper bound on a sequence's keys, <= 0: T_k.  It only decides how the work is split.
+ *   max_k_len   host-side upper bound on a sequence's keys, <= 0: T_k.  It only decides how the work is split.  The size of the
+ *               workspace is asked for with the same bound (T_k where the call's is <= 0).
  *   causal      0: every query sees all keys of its sequence.  Otherwise the last query sees all of them and every query before it
  *               one less than its successor: query i of n_q sees keys 0 .. n_k - n_q + i (the ends are aligned, so that a prefix of
  *               keys without queries may stand in front).  Queries that see nothing get zeros.
@@ -423,7 +424,7 @@ int saw_paged_prompt_attn(const saw_cache_t* cache, const void* q, int32_t dtype
  *   score_stride  floats between rows, at least max_seq_len (its value where <= 0 stands for it).
  *   workspace   at least saw_attn_weights_workspace_bytes(...) bytes, 16-byte aligned.
  * All in fp32 (queries as two fp16 limbs, 2^-22 of a row's largest channel); the sums have a fixed order.  A query that sees
- * nothing adds nothing.  T == 0 leaves prev + 0.
+ * nothing adds nothing.  T == 0 leaves prev + 0.  T n_q_heads / n_kv_heads + 16 B up to 2^24 - 2^9.
  */
 size_t saw_attn_weights_workspace_bytes(const saw_cache_t* cache, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len);
 int saw_paged_attn_weights(const saw_cache_t* cache, const void* q, int32_t dtype, int64_t T, int64_t q_stride, int32_t n_q_heads,

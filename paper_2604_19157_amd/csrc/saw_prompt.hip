@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void prompt_query_kernel(PromptParams p) {
   constexpr int E = D / 64;
   __shared__ __attribute__((aligned(16))) float rows[4][128];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n = p.T_q * p.n_q_heads, row = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t n = p.T_q * p.n_q_heads, row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave;
   if (row >= n) return;
   const int64_t at = row / p.n_q_heads * p.q_stride + row % p.n_q_heads * D;
   float* const x = rows[wave];
@@ -593,7 +593,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int s
   constexpr int E = D / 64;
   __shared__ __attribute__((aligned(16))) float rotated[4][128];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t rows = p.T_q * p.n_q_heads, row = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t rows = p.T_q * p.n_q_heads, row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave;
   if (row >= rows) return;
   const int64_t token = row / p.n_q_heads;
   const int b = last_not_above(p.B, token, lane, [&](int i) { return clamped_offset(p.cu_q, i, p.T_q); });
@@ -666,8 +666,9 @@ static size_t record_bytes(int D, int64_t rows, int splits) { return (size_t)row
 
 template <int D, int KV>
 static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream_t st) {
-  const int64_t rows = p.T_q * p.n_q_heads;
-  const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads), plan.splits), by_row((unsigned)((rows + 3) / 4)), block(256);
+  const int64_t quads = (p.T_q * p.n_q_heads + 3) / 4;                   // (a grid's width is counted in threads, in 32 bits)
+  const unsigned wide = (unsigned)(quads < 1 << 22 ? quads : 1 << 22);
+  const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads), plan.splits), by_row(wide, (unsigned)((quads + wide - 1) / wide)), block(256);
   if constexpr (KV == kKvInt4 && D == kDenseD)
     if (p.dense_k) prompt_query_kernel<D><<<by_row, block, 0, st>>>(p);
   if (plan.rows == 128) prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
@@ -681,7 +682,7 @@ static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream
 int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
   const int64_t rows = p.T_q * p.n_q_heads;
   const PromptPlan plan = prompt_plan(int4, D, p.group, p.n_kv_heads, p.T_q, p.B, p.bound);
-  if (row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads > 0x7fffffffLL || rows / 4 >= 0x7fffffffLL) return SAW_EINVAL;
+  if (row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads * (plan.rows == 256 ? 512 : 256) > 0xffffffffLL) return SAW_EINVAL;
   if (int4) {
     // (behind the records: rows of D + 2 floats)
     p.query_scale = p.ws + ((D + 2) * rows * plan.splits + 3) / 4 * 4;

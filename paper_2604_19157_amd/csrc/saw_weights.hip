@@ -548,7 +548,8 @@ int launch_weights(const PromptParams& p, int D, hipStream_t st) {
   const int64_t tiles = row_tiles(p.T_q, p.group, kWeightRows, p.B);
   const int chunks = weight_chunks(p.n_kv_heads, p.B, p.bound), unit = 4 * kWeightKeys;
   const int chunk_keys = (int)(((int64_t)(p.bound + chunks - 1) / chunks + unit - 1) / unit * unit);
-  if (tiles > 0x7fffffffLL || (int64_t)p.n_kv_heads * chunks > 0x7fffffffLL || (tiles + kGroupTiles - 1) / kGroupTiles > 65535) return SAW_EINVAL;
+  // (grids: widths below 2^32 threads, groups of tiles below 2^16)
+  if ((int64_t)p.n_kv_heads * chunks * 256 > 0xffffffffLL || (tiles + kGroupTiles - 1) / kGroupTiles > 65535) return SAW_EINVAL;
   if (one_launch(p)) {
     const dim3 grid(p.n_kv_heads, p.B);
     if (D == 128) weight_step_kernel<128><<<grid, dim3(64 * kStepWaves), 0, st>>>(p);

@@ -78,6 +78,16 @@ def test_weights_refusals(saw, change, code):
     assert saw.lib().saw_paged_attn_weights(*{**WEIGHTS, "cache": ctypes.byref(c), **change}.values()) == code
 
 
+def test_grids_beyond_32_bits_are_refused(saw):
+    """Launches are counted in 32 bits of threads, and the weights' groups of rows in 16."""
+    wide = dict(n_kv_heads=1024, n_q_heads=1024, T_q=1, q_stride=1024 * 128, k_stride=1024 * 128, v_stride=1024 * 128, B=65535)
+    assert saw.lib().saw_prompt_attn(*{**PROMPT, **wide}.values()) == EINVAL
+    many = _cache(saw, n_kv_heads=1024)
+    assert saw.lib().saw_paged_prompt_attn(*{**PAGED, "cache": ctypes.byref(many), "n_q_heads": 1024, "q_stride": 1024 * 128, "T": 1, "B": 65535}.values()) == EINVAL
+    c = _cache(saw)
+    assert saw.lib().saw_paged_attn_weights(*{**WEIGHTS, "cache": ctypes.byref(c), "T": 1 << 22}.values()) == EINVAL
+
+
 @pytest.mark.parametrize("change,code", CACHES, ids=str)
 def test_weights_refuse_caches(saw, change, code):
     c = _cache(saw, **change)
