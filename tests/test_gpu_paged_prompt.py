@@ -378,3 +378,45 @@ def test_long_contexts_split(saw, n, lens, G):
     prev = np.zeros((len(n), 2, max(lens)), np.float32)
     want, tol = _scores(c, prev)
     pc.check(saw.paged_attn_weights(c.cache, *c.args, prev=torch.from_numpy(prev).cuda(), max_seq_len=max(lens)), want, tol)
+
+
+# ---- the calls together ----
+def test_pools_beyond_32_bits(saw):
+    """Pages at the end of pools of 4.9 GiB of codes each: what they give at the front."""
+    c = Case(saw, [5, 90], [700, 333], Hkv=8)
+    num, used = 640000, c.cache.num_pages
+    big = saw.Cache(num, 8, 128, 128, 3)
+    for name in ("k_codes", "v_codes", "k_meta", "v_meta"):
+        getattr(big, name)[num - used:].copy_(getattr(c.cache, name))
+    q, cu, pt, lens = c.args
+    far = torch.where(pt < used, pt + (num - used), pt + num)
+    assert torch.equal(saw.paged_prompt_attn(big, q, cu, far, lens), saw.paged_prompt_attn(c.cache, *c.args))
+    scores = saw.paged_attn_weights(c.cache, *c.args)
+    assert torch.equal(saw.paged_attn_weights(big, q, cu, far, lens), scores)
+    dst = torch.arange(num // 2, num // 2 + 2 * 16, dtype=torch.int32, device="cuda").view(2, 16)
+    _, kept, _ = saw.evict_pages(big, scores, far, lens, dst, 256, 20)
+    for b in range(2):
+        for g in (0, 7):
+            j = kept[b, g].long()
+            for name in ("k_codes", "v_codes", "k_meta", "v_meta"):
+                old, new = getattr(c.cache, name), getattr(big, name)
+                assert torch.equal(new[dst[b].long(), g].flatten(0, 1), old[pt[b].long()[j // 16], g, j % 16])
+
+
+def test_two_streams_at_once(saw):
+    """Calls with workspaces of their own do not meet."""
+    cases = [Case(saw, [5] * 8, [900 + 40 * i for i in range(8)], Hkv=8, seed=s) for s in (1, 2)]
+    want = [(saw.paged_prompt_attn(c.cache, *c.args), saw.paged_attn_weights(c.cache, *c.args)) for c in cases]
+    ws = [(torch.empty(saw.paged_prompt_workspace_bytes(c.cache, c.args[0], 8, c.pt.shape[1] * 16), dtype=torch.uint8, device="cuda"),
+           torch.empty(saw.attn_weights_workspace_bytes(c.cache, c.args[0], 8, c.pt.shape[1] * 16), dtype=torch.uint8, device="cuda")) for c in cases]
+    got = [(torch.zeros_like(a), torch.zeros_like(b)) for a, b in want]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, s, w, g in zip(cases, streams, ws, got):
+            with torch.cuda.stream(s):
+                saw.paged_prompt_attn(c.cache, *c.args, out=g[0], workspace=w[0])
+                saw.paged_attn_weights(c.cache, *c.args, scores=g[1], workspace=w[1])
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])

@@ -77,6 +77,20 @@ def test_tokens_at_a_stride(saw, d, G):
     assert torch.equal(got, saw.prompt_attn(q.contiguous(), k.contiguous(), v.contiguous(), cq))
 
 
+def test_strides_beyond_32_bits(saw):
+    """Tokens 2^21 elements apart: the last lie behind 2^32 elements."""
+    far = torch.empty((2100, 1 << 21), dtype=BF, device="cuda")
+    x = [pc.rand((2100, h, 128), 7 + i, BF).cuda() for i, h in enumerate((4, 2, 2))]
+    views, at = [], 64
+    for t in x:
+        v = far[:, at:at + t[0].numel()].unflatten(1, t.shape[1:])
+        v.copy_(t)
+        views.append(v)
+        at += t[0].numel()
+    cu = torch.tensor([0, 2000, 2100], dtype=torch.int32, device="cuda")
+    assert torch.equal(saw.prompt_attn(*views, cu), saw.prompt_attn(*x, cu))
+
+
 @pytest.mark.parametrize("d", [128, 64])
 def test_rows_of_no_sequence_are_left_as_they_were(saw, d):
     q, k = pc.rand((200, 8, d), 3, BF).cuda(), pc.rand((200, 2, d), 4, BF).cuda()
