@@ -69,6 +69,12 @@ __device__ __forceinline__ f32x2 put_query_row(const PromptParams& p, int64_t to
   return f32x2{__uint_as_float((uint32_t)(127 + ex) << 23), total};
 }
 
+// A row behind the last: zero.
+template <int D>
+__device__ __forceinline__ void put_no_row(u32x4* limbs, int r, int lane) {
+  for (int i = lane; i < 2 * (D / 32) * 4; i += 64) limbs[i / 4 * 64 + 16 * (i % 4) + r] = u32x4{0, 0, 0, 0};
+}
+
 // Rotated queries of a row tile as operand registers: a wavefront a row.
 template <int D>
 __global__ __launch_bounds__(1024) void weight_query_kernel(PromptParams p, int64_t tiles) {
@@ -78,8 +84,14 @@ __global__ __launch_bounds__(1024) void weight_query_kernel(PromptParams p, int6
   RowTile rt;
   if (!find_row_tile(p, blockIdx.x, kWeightRows, lane, rt)) return;
   const int64_t at = (int64_t)blockIdx.x * p.n_kv_heads + h;
-  const int row = rt.row0 + min(r, rt.rows - 1);                          // (rows behind the last: the last again, never looked at)
-  const f32x2 v = put_query_row<D>(p, rt.begin + row / p.group, h * p.group + row % p.group, rows[r], (uint16_t*)(ws.limbs + at * 2 * (D / 32) * 64), r, lane);
+  u32x4* const limbs = ws.limbs + at * 2 * (D / 32) * 64;
+  f32x2 v = {1.f, 0.f};
+  if (r < rt.rows) {
+    const int row = rt.row0 + r;
+    v = put_query_row<D>(p, rt.begin + row / p.group, h * p.group + row % p.group, rows[r], (uint16_t*)limbs, r, lane);
+  } else {
+    put_no_row<D>(limbs, r, lane);
+  }
   if (lane == 0) ws.info[at * kWeightRows + r] = RowInfo{v.x, v.y, 0.f, 0.f};
 }
 
@@ -160,7 +172,8 @@ __device__ __forceinline__ u32x4 centred(uint32_t w, CodeBits bits) {
 template <int D>
 struct TileQueries {
   u32x4 q[2][D / 32];
-  float scale[4], sum_q[4];       // of rows 4 (lane / 16) + 0..3
+  f32x4 info[4];                  // of rows 4 (lane / 16) + 0..3
+  float sum_q[4];
   __device__ __forceinline__ u32x4 limb(int l, int ks) const { return q[l][ks]; }
   __device__ __forceinline__ void load(const u32x4* limbs, const RowInfo* info, int lane) {
 #pragma unroll
@@ -169,9 +182,8 @@ struct TileQueries {
       for (int ks = 0; ks < D / 32; ++ks) q[l][ks] = limbs[(l * (D / 32) + ks) * 64 + lane];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const f32x2 v = *(const f32x2*)&info[4 * (lane >> 4) + r].scale;
-      scale[r] = v.x;
-      sum_q[r] = v.y;
+      this->info[r] = *(const f32x4*)&info[4 * (lane >> 4) + r];
+      sum_q[r] = this->info[r].y;
     }
   }
 };
@@ -192,11 +204,9 @@ __device__ __forceinline__ f32x2 key_codes(const KeyCodes<D>& codes, CodeBits bi
   return key0 + 16 * t + (lane & 15) < len ? codes.pair[t] : f32x2{0.f, 0.f};
 }
 
-// Logits of 16 rows and 16 keys: of row 4 (lane / 16) + r and the lane's key, in log2 units; hidden ones and those behind the sequence's end
-// -infinity.
+// Logits of 16 rows and 16 keys, in log2 units divided by the rows' scales: of row 4 (lane / 16) + r and the lane's key.
 template <int D, typename Q>
-__device__ __forceinline__ f32x4 tile_logits16(const Q& tq, const u32x4 (&k)[D / 32], f32x2 pair, int key, int len, bool masked,
-                                               int first_hidden, int shift, int row0, int lane) {
+__device__ __forceinline__ f32x4 tile_logits16(const Q& tq, const u32x4 (&k)[D / 32], f32x2 pair) {
   f32x4 s = {0.f, 0.f, 0.f, 0.f}, x;
 #pragma unroll
   for (int l = 1; l >= 0; --l)
@@ -204,13 +214,23 @@ __device__ __forceinline__ f32x4 tile_logits16(const Q& tq, const u32x4 (&k)[D /
     for (int ks = 0; ks < D / 32; ++ks) s = mfma16(tq.limb(l, ks), k[ks], s);
   const float z8 = pair.y - 8.f;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    x[r] = fmaf(-z8, tq.sum_q[r], s[r]) * pair.x * tq.scale[r];
-    // (row i sees the keys in front of first_hidden + its token)
-    if (masked && (key >= len || key >= first_hidden + ((row0 + 4 * (lane >> 4) + r) >> shift))) x[r] = -INFINITY;
-  }
+  for (int r = 0; r < 4; ++r) x[r] = fmaf(-z8, tq.sum_q[r], s[r]) * pair.x;
   return x;
 }
+// Hidden ones and those behind the sequence's end become -infinity.  (Row i sees the keys in front of first_hidden + its token.)
+__device__ __forceinline__ void hide(f32x4& x, int key, int len, int first_hidden, int shift, int row0, int lane) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (key >= min(len, first_hidden + ((row0 + 4 * (lane >> 4) + r) >> shift))) x[r] = -INFINITY;
+}
+
+// Maximum and sum over rows of 16 lanes of four numbers at once: a step's operands are four instructions old, as far as DPP asks for.
+#define ROW_STEP4(op, how)                                                                                                         \
+  op " %0, %0, %0 " how " row_mask:0xf bank_mask:0xf\n\t" op " %1, %1, %1 " how " row_mask:0xf bank_mask:0xf\n\t"              \
+  op " %2, %2, %2 " how " row_mask:0xf bank_mask:0xf\n\t" op " %3, %3, %3 " how " row_mask:0xf bank_mask:0xf\n\t"
+#define ROW_ALL4(op) "s_nop 1\n\t" ROW_STEP4(op, "row_ror:1") ROW_STEP4(op, "row_ror:2") ROW_STEP4(op, "row_ror:4") ROW_STEP4(op, "row_ror:8")
+__device__ __forceinline__ void row_allmax4(float (&v)[4]) { asm(ROW_ALL4("v_max_f32_dpp") : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3])); }
+__device__ __forceinline__ void row_allsum4(float (&v)[4]) { asm(ROW_ALL4("v_add_f32_dpp") : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3])); }
 
 // One pass over a chunk of the keys of a (sequence, kv head).  STATS: maximum and sum of each row of a group of row tiles over the
 // chunk; otherwise the weights of the chunk's keys over all rows.
@@ -238,6 +258,11 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
   const CodeBits bits;
   TileQueries<D> tq;
   int held = -1;                // the row tile in tq: a single one is loaded once
+  auto load_tile = [&](int g) {
+    const int64_t at = (first_tile + g) * p.n_kv_heads + h;
+    tq.load(ws.limbs + at * 2 * (D / 32) * 64, ws.info + at * kWeightRows, lane);
+    held = g;
+  };
   KeyStream<D> keys;
   keys.pages = p.page_table + (int64_t)b * p.max_pages;
   keys.end = k1; keys.stride = 4 * kWeightKeys; keys.len = len;
@@ -252,46 +277,63 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
     // the first row that sees a key of the step: key0 < first_hidden + token
     const int first_token = max(key0 - first_hidden + 1, 0);
     for (int g = max(g0, (int)(((int64_t)first_token << shift) / kWeightRows)); g < g1; ++g) {
-      const int64_t at = (first_tile + g) * p.n_kv_heads + h;
-      const RowInfo* const info = ws.info + at * kWeightRows;
       const int row0 = g * kWeightRows;
       const bool masked = key0 + kWeightKeys > min(first_hidden + (row0 >> shift), len);
       f32x4 x[4];
-      if (g != held) tq.load(ws.limbs + at * 2 * (D / 32) * 64, info, lane);
-      held = g;
+      if (g != held) load_tile(g);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) x[t] = tile_logits16<D>(tq, k[t], pair[t], key0 + 16 * t + (lane & 15), len, masked, first_hidden, shift, row0, lane);
+      for (int t = 0; t < 4; ++t) x[t] = tile_logits16<D>(tq, k[t], pair[t]);
+      if (masked)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) hide(x[t], key0 + 16 * t + (lane & 15), len, first_hidden, shift, row0, lane);
+      f32x4 info[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) info[r] = tq.info[r];
+      // (The next tile's queries arrive behind the exponentials: 32 tokens of 64 heads over 16000 keys 103 us, 111 without.  With 64
+      // channels the registers for it cost a wavefront a SIMD: 86 us, 75 without.)
+      if (D == 128 && g + 1 < g1) load_tile(g + 1);
       if constexpr (STATS) {
+        float2* const mine = &stats[wave][(g - g0) * kWeightRows + 4 * (lane >> 4)];
+        float top[4], sum[4], m[4], old[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top[r] = fmaxf(fmaxf(x[0][r], x[1][r]), fmaxf(x[2][r], x[3][r]));
+        row_allmax4(top);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float top = row_allmax(fmaxf(fmaxf(x[0][r], x[1][r]), fmaxf(x[2][r], x[3][r])));
-          float2* const mine = &stats[wave][(g - g0) * kWeightRows + 4 * (lane >> 4) + r];
-          const float2 old = *mine;
-          const float m = fmaxf(old.x, top), ref = m == -INFINITY ? 0.f : m;
-          const float part = row_allsum((fast_exp2(x[0][r] - ref) + fast_exp2(x[1][r] - ref)) + (fast_exp2(x[2][r] - ref) + fast_exp2(x[3][r] - ref)));
-          const float sum = fmaf(old.y, fast_exp2(old.x - ref), part);
-          wave_sync();
-          if ((lane & 15) == 0) *mine = make_float2(m, sum);
+          const float2 was = mine[r];
+          m[r] = fmaxf(was.x, top[r] * info[r].x);
+          const float ref = m[r] == -INFINITY ? 0.f : m[r];
+          sum[r] = (fast_exp2(fmaf(x[0][r], info[r].x, -ref)) + fast_exp2(fmaf(x[1][r], info[r].x, -ref))) +
+                   (fast_exp2(fmaf(x[2][r], info[r].x, -ref)) + fast_exp2(fmaf(x[3][r], info[r].x, -ref)));
+          old[r] = was.y * fast_exp2(was.x - ref);
         }
+        row_allsum4(sum);
+        wave_sync();
+        if ((lane & 15) == 0)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mine[r] = make_float2(m[r], old[r] + sum[r]);
         wave_sync();
       } else {
+        f32x2 mi[4];
+        bool none = false;                                                 // (a row whose sum is no number: nor is any of its weights,
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const f32x2 mi = *(const f32x2*)&info[4 * (lane >> 4) + r].m;
-          bool there = row0 + 4 * (lane >> 4) + r < rows;
-          if (masked && __any(mi.y != mi.y)) {
-            // (a row whose sum is no number: nor is any of its weights, but for those of the keys that it does not see)
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-              if (there && mi.y != mi.y && x[t][r] != -INFINITY) total[t] = mi.y;
-            there = there && mi.y == mi.y;
-          }
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const float w = fast_exp2(x[t][r] - mi.x) * mi.y;
-            if (there) total[t] += w;
-          }
+        for (int r = 0; r < 4; ++r) {                                      // but for those of the keys that it does not see)
+          mi[r] = f32x2{info[r].z, info[r].w};
+          none = none || mi[r].y != mi[r].y;
         }
+        if (masked && __any(none))
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (mi[r].y != mi[r].y) {
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+                if (x[t][r] != -INFINITY) total[t] = mi[r].y;
+              mi[r].y = 0.f;
+            }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) total[t] = fmaf(fast_exp2(fmaf(x[t][r], info[r].x, -mi[r].x)), mi[r].y, total[t]);
       }
     }
     if constexpr (!STATS) {
@@ -334,7 +376,7 @@ __global__ __launch_bounds__(64) void weight_join_kernel(PromptParams p, int64_t
   sum = add_xor32(add_xor16(sum * fast_exp2(m - ref)));
   if (lane < 16) {
     ws.info[at].m = ref;
-    ws.info[at].inv = sum == 0.f ? 0.f : 1.f / sum;
+    ws.info[at].inv = sum == 0.f || r >= rt.rows ? 0.f : 1.f / sum;
   }
 }
 
@@ -381,9 +423,9 @@ __global__ __launch_bounds__(64 * kStepWaves, 4) void weight_step_kernel(PromptP
         // (a wavefront's row is turned over in its part of the logits' memory)
         const f32x2 v = put_query_row<D>(p, begin + (row >> shift), h * p.group + (row & (p.group - 1)), kept + 128 * wave, (uint16_t*)limbs, r, lane);
         if (lane == 0) info[r] = RowInfo{v.x, v.y, 0.f, 0.f};
-      } else {                                                             // (rows behind the last: nothing)
-        for (int i = lane; i < 2 * (D / 32) * 4; i += 64) limbs[i / 4 * 64 + 16 * (i % 4) + r] = u32x4{0, 0, 0, 0};
-        if (lane == 0) info[r] = RowInfo{0.f, 0.f, 0.f, 0.f};
+      } else {
+        put_no_row<D>(limbs, r, lane);
+        if (lane == 0) info[r] = RowInfo{1.f, 0.f, 0.f, 0.f};
       }
     }
     __syncthreads();
@@ -405,7 +447,10 @@ __global__ __launch_bounds__(64 * kStepWaves, 4) void weight_step_kernel(PromptP
         for (int t = 0; t < 4; ++t) {
           u32x4 k[D / 32];
           const f32x2 pair = key_codes<D>(codes, bits, t, key0, len, lane, k);
-          x[t] = tile_logits16<D>(tq, k, pair, key0 + 16 * t + (lane & 15), len, masked, first_hidden, shift, row0, lane);
+          x[t] = tile_logits16<D>(tq, k, pair);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[t][r] *= tq.scale[r];
+          if (masked) hide(x[t], key0 + 16 * t + (lane & 15), len, first_hidden, shift, row0, lane);
           asm volatile("" ::: "memory");                                   // (or the limbs would be kept in registers after all)
         }
         if (key0 + kStride < len) {
