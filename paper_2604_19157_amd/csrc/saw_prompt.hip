@@ -190,6 +190,13 @@ __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token,
   return p.scale;
 }
 
+// This split's (maximum, sum) of every row, behind the records of all splits.
+template <int D>
+__device__ __forceinline__ float2* partial_sums(const PromptParams& p) {
+  const int64_t rows = p.T_q * p.n_q_heads;
+  return (float2*)(p.ws + (int64_t)gridDim.y * rows * D) + (int64_t)blockIdx.y * rows;
+}
+
 // The end of a wavefront's 32 rows: outputs, or partial records [split][row][D] and [split][row] (maximum, sum) where the keys are split
 // or a learned rotation has to be undone.  scale: of the rows' logits; unit: of the output sums.
 template <int D, int KV, int HALF_BIT>
@@ -209,7 +216,7 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
   const bool split = gridDim.y > 1 || (kInt4 && p.dense_v);
   const int64_t rows = p.T_q * p.n_q_heads;
   float* const records = p.ws + (int64_t)blockIdx.y * rows * D;
-  float2* const ml = (float2*)(p.ws + (int64_t)gridDim.y * rows * D) + (int64_t)blockIdx.y * rows;
+  float2* const ml = partial_sums<D>(p);
   if (__any(odd != odd)) {
     constexpr int E = D / 64;
     const RowSource<D, KV> src = {p, rt.b, h, k0, lane};
@@ -456,10 +463,15 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   const int last = rt.row0 + rt.rows - 1, row = rt.row0 + (lane & 31);
   auto sees_of = [&](int r) { return max(min(len, len - rt.n + (r >> shift) + 1), 0); };
   const int sees = row <= last ? sees_of(row) : 0, kend = sees_of(last), kfull = rt.rows == 32 ? sees_of(rt.row0) : 0;
-  const int nt = (kend + kTileKeys - 1) / kTileKeys, per = (nt + (int)gridDim.y - 1) / (int)gridDim.y;
+  // (a tile for every wavefront at least: of a short sequence the last splits have none)
+  const int nt = (kend + kTileKeys - 1) / kTileKeys, per = max((nt + (int)gridDim.y - 1) / (int)gridDim.y, NW);
   const int t0 = (int)blockIdx.y * per, t1 = min(nt, t0 + per);
   const int64_t token = rt.begin + (min(row, last) >> shift);
   const int head = h * p.group + (row & (p.group - 1));
+  if (t0 >= t1 && gridDim.y > 1) {
+    if (wave == 0 && lane < 32 && row <= last) partial_sums<D>(p)[token * p.n_q_heads + head] = make_float2(-INFINITY, 0.f);
+    return;
+  }
   const int32_t* const pages = p.page_table + (int64_t)rt.b * p.max_pages;
   char* const mine = lds[wave];
 
@@ -617,7 +629,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int s
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), min(s0 + k, splits - 1)));
-      if (s0 + k < splits)
+      if (s0 + k < splits && w != 0.f)                                     // (a split without keys leaves no record)
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] = fmaf(w, v[k][e], o[e]);
     }
