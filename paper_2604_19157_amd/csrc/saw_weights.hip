@@ -357,27 +357,41 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
   }
 }
 
-// Joins the partial (maximum, sum) pairs of a row tile and head.
+// Joins the partial (maximum, sum) pairs of a row tile and head: a lane for every sixteenth of the chunks of a row.
 template <int D>
-__global__ __launch_bounds__(64) void weight_join_kernel(PromptParams p, int64_t tiles, int chunks) {
+__global__ __launch_bounds__(256) void weight_join_kernel(PromptParams p, int64_t tiles, int chunks) {
+  constexpr int kAhead = 4;                                               // pairs on their way at once
+  __shared__ float2 part[4][kWeightRows];
   const WeightSpace<D> ws(p.ws, tiles, p.n_kv_heads);
-  const int lane = threadIdx.x, r = lane & 15;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15;
   RowTile rt;
   if (!find_row_tile(p, blockIdx.x, kWeightRows, lane, rt)) return;
   const int64_t at = ((int64_t)blockIdx.x * p.n_kv_heads + blockIdx.y) * kWeightRows + r, step = tiles * p.n_kv_heads * kWeightRows;
   float m = -INFINITY, sum = 0.f;
-  for (int c = lane >> 4; c < chunks; c += 4) {
-    const float2 v = ws.part[c * step + at];
-    const float top = fmaxf(m, v.x), ref = top == -INFINITY ? 0.f : top;
-    sum = sum * fast_exp2(m - ref) + v.y * fast_exp2(v.x - ref);
+  for (int c0 = threadIdx.x >> 4; c0 < chunks; c0 += 16 * kAhead) {
+    float2 v[kAhead];
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) v[k] = c0 + 16 * k < chunks ? ws.part[(c0 + 16 * k) * step + at] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) top = fmaxf(top, v[k].x);
+    const float ref = top == -INFINITY ? 0.f : top;
+    sum *= fast_exp2(m - ref);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) sum = fmaf(v[k].y, fast_exp2(v[k].x - ref), sum);
     m = top;
   }
-  const float top = max_xor32(max_xor16(m)), ref = top == -INFINITY ? 0.f : top;
+  const float here = max_xor32(max_xor16(m)), ref = here == -INFINITY ? 0.f : here;
   sum = add_xor32(add_xor16(sum * fast_exp2(m - ref)));
-  if (lane < 16) {
-    ws.info[at].m = ref;
-    ws.info[at].inv = sum == 0.f || r >= rt.rows ? 0.f : 1.f / sum;
-  }
+  if (lane < 16) part[wave][r] = make_float2(here, sum);
+  __syncthreads();
+  if (threadIdx.x >= 16) return;
+  const float top = fmaxf(fmaxf(part[0][r].x, part[1][r].x), fmaxf(part[2][r].x, part[3][r].x)), all_ref = top == -INFINITY ? 0.f : top;
+  float all = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) all = fmaf(part[w][r].y, fast_exp2(part[w][r].x - all_ref), all);
+  ws.info[at].m = all_ref;
+  ws.info[at].inv = all == 0.f || r >= rt.rows ? 0.f : 1.f / all;
 }
 
 // Statistics and weights in one launch, for batches of few rows a sequence that fill the chip by themselves (a decode step): a block takes
@@ -574,7 +588,7 @@ static void launch_passes(const PromptParams& p, int64_t tiles, int chunks, int 
   if (p.T_q) {
     weight_query_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(1024), 0, st>>>(p, tiles);
     weight_pass_kernel<D, true><<<dim3(p.n_kv_heads * chunks, p.B, groups), dim3(256), 0, st>>>(p, tiles, chunk_keys);
-    weight_join_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(64), 0, st>>>(p, tiles, chunks);
+    weight_join_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(256), 0, st>>>(p, tiles, chunks);
   }
   weight_pass_kernel<D, false><<<dim3(p.n_kv_heads * chunks, p.B), dim3(256), 0, st>>>(p, tiles, chunk_keys);
 }
