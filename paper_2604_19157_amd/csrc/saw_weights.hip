@@ -594,13 +594,14 @@ static void launch_passes(const PromptParams& p, int64_t tiles, int chunks, int 
 }
 
 // One launch where a sequence has about one query: short contexts, whose four launches take longer than a block of one compute unit for each
-// (sequence, kv head) (1 x 1000 tokens x 8 kv heads 13 us, 19 in two passes; 8 x 2000 20.5 and 22.9; x 4000 32 and 29), or batches that fill
-// the chip, the sooner if the logits fit shared memory (24 x 4000 36 and 58; 24 of 1000 to 8000 tokens, which do not, 97 and 71; 64 of 4000 to
-// 10000 186 and 280).  Several queries a sequence are level (32 x 5 over 1000 tokens 35 and 39, 8 x 5 29 and 23).
+// (sequence, kv head) (8 kv heads; one launch and two passes: 1 x 1000 tokens 13.7 us and 15.5, 8 x 1000 14.2 and 16.4; 1 x 2000 19.1 and
+// 15.5), or batches that fill the chip, the sooner if the logits fit shared memory (16 x 4000 35 and 44.6, 8 x 4000 33 and 27; 64 of 4000 to
+// 10000, which do not, 201 and 250, 24 of 1000 to 8000 102 and 66).  Several queries a sequence are level at best (32 x 5 over 1000 tokens
+// 36.5 and 37, 8 x 5 31 and 20).
 static bool one_launch(const PromptParams& p) {
   const int64_t items = (int64_t)p.B * p.n_kv_heads;
   if (p.T_q > p.B) return false;
-  return (int64_t)p.bound * p.group <= kKeptLogits ? items >= 128 || p.bound <= 2048 : items >= 256;
+  return (int64_t)p.bound * p.group <= kKeptLogits ? items >= 128 || p.bound <= 1280 : items >= 256;
 }
 
 int launch_weights(const PromptParams& p, int D, hipStream_t st) {
