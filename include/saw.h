@@ -11,6 +11,10 @@
  * for large batches), saw_flatten_dequant (the prefill-side read-back into dense 16-bit
  * buffers), saw_dequant_pages (fp32 read-back for inspection), and a 16-bit-KV paged
  * decode (saw_kv16_*) that serves as the same-run unquantised comparison.
+ * For what stands around the decode steps: saw_prompt_attn (attention of packed prompts over their own
+ * 16-bit K/V), saw_paged_prompt_attn (several new tokens of every sequence over the INT4 pages),
+ * saw_paged_attn_weights (the attention that cached tokens get, summed over steps) and
+ * saw_evict_pages (keeps the heaviest tokens of a sequence, moved to other pages).
  *
  * Conventions for every call
  *   - All data pointers are DEVICE pointers owned by the caller; the library never

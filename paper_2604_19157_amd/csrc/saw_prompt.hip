@@ -314,6 +314,12 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
 // one barrier a tile.  Keys and values of 16 bits come from memory straight into the buffer (each transfer has a whole tile's
 // products to arrive in).  Those of the INT4 pages are requested a tile ahead into registers and written behind the tile's products:
 // as fp16 times powers of two (Unit), each once per block and not once per row.
+//   Roundings: weights to the type of the values, whose half step the output has anyway; over the pages query, keys, weights and
+// values to fp16 (an output is off by 1.4e-3 in fp16 and 2.0e-3 in bf16, 1.6e-3 of it bf16's own, where keys have channels 20
+// times as large as others; two limbs of the query as in saw_weights.hip would be half as much matrix work again).
+//   Bound by the matrix cores at the clock that they leave, with the exponentials behind them: 8192 causal tokens, 32 query and 8 kv heads
+// of 128 channels, 519 us, 1.06 PFLOP/s (a library product of 8192^3 1.27); 64 channels, where a logit has half the products, 0.87; 2048
+// tokens over 16384 in the pages 715 us, 0.82, with 200 M instructions of the vector ALU, 0.3 of them for the codes.
 template <int D, int KV, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
   constexpr int R = 32 * NW, kRow = 2 * D, kTile = kTileKeys * kRow, kInstr = kTile / 1024, kRpi = 1024 / kRow;
@@ -448,6 +454,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
 // keys, every fourth tile each, so that none waits for another until they join their states at the end.  Keys go from memory to operand
 // registers - a lane holds one half of one key's channels, which the queries' k-steps follow -, values through 64 rows of shared
 // memory of the wavefront's own for the transposing reads.
+//   Bound by the vector ALU, 1360 instructions for 64 keys, over half of them for the codes: 32 sequences of 5 tokens over 512 to 4096, 88
+// MB, 52 us and 6.7 for the merge.
 template <int D>
 __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   constexpr int NW = 4, kRow = 2 * D, kTile = kTileKeys * kRow, kHalfBit = D == 128 ? 6 : 5, kWords = D / 16, kPieces = D / 32;
@@ -599,7 +607,8 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   finish_rows<D, kKvInt4, kHalfBit>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, qf, scale, 1.f, st, lane);
 }
 
-// Joins the partial records of a row: one wavefront a row.
+// Joins the partial records of a row: one wavefront a row, eight records on their way at once.  5120 rows in two splits 6.7 us, most of it
+// latency.
 template <int D, bool INT4>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int splits) {
   constexpr int E = D / 64;

@@ -8,6 +8,9 @@
 // without shared memory: a lane holds a quarter of one key's codes, and the products run over the channels in the order in which
 // four instructions take the codes out of a word (0 4 1 5 2 6 3 7), which is how the query limbs are laid out.
 // Two passes over the keys: maximum and sum of every row (split over the keys, joined by a small pass), then the weights.
+//   32 tokens of 64 heads in each of two sequences over 12000 to 16000 keys: 52 and 44 us, 6 and 5 for queries and join.  Bound by the
+// instructions of the vector ALU at two wavefronts a SIMD (14 M and 9.5 M, with 1.8 M matrix instructions in each pass); the
+// keys are 19 MB.
 #include "saw_prompt_tile.h"
 #include "saw_rotate_row.h"
 
@@ -397,7 +400,8 @@ __global__ __launch_bounds__(256) void weight_join_kernel(PromptParams p, int64_
 // Statistics and weights in one launch, for batches of few rows a sequence that fill the chip by themselves (a decode step): a block takes
 // a (sequence, kv head), reads its keys once and keeps the logits in shared memory while they fit; longer ones are worked out again.
 // Sequences of more rows take a row tile after the other, the later ones on top of what the earlier wrote.  What bounds it is how many
-// wavefronts a SIMD has to cover one another's waits: four of them, 128 registers each, which is why a step works on 16 keys at a time.
+// wavefronts a SIMD has to cover one another's waits: four of them, 128 registers each, which is why a step works on 16 keys at a time
+// (64 sequences of 512 to 4096 tokens, 95 MB, 49 us; two passes 132).
 constexpr int kKeptLogits = 16384, kStepWaves = 8;
 
 template <int D>
