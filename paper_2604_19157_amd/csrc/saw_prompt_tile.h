@@ -122,21 +122,33 @@ struct RowState {
   float m, ref, sum;      // maximum that the state refers to (log2 units, -inf: none yet; ref: 0 then); this half's sum of weights
 };
 
-// S^T of one tile against the queries in qf
+// S^T of one tile against the queries in qf.  The two halves of the keys alternate, since a product takes twice its time until its sum
+// can be added to, and operands are read six products ahead.
 template <int D, typename M1>
 __device__ __forceinline__ void tile_logits(const char* k, const u32x4 (&qf)[D / 16], f32x16 (&s)[2], int lane) {
+  constexpr int kAhead = 6, kAll = 2 * (D / 16);
+  const int row = lane & 31;
+  const char* const at = k + row * (2 * D);
 #pragma unroll
-  for (int kb = 0; kb < 2; ++kb) {
+  for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-    const int row = 32 * kb + (lane & 31);
-    const char* const at = k + row * (2 * D);
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      const u32x4 a = *(const u32x4*)(at + 16 * k_place<D>(row, 2 * ks + (lane >> 5)));
+  for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const u32x4 a = *(const u32x4*)(at + kb * 32 * (2 * D) + 16 * k_place<D>(row, 2 * ks + (lane >> 5)));
       s[kb] = M1::mfma(a, qf[ks], s[kb]);
     }
+  __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+  for (int i = 0; i < kAll - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
   }
+  __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // Keys that a lane's query does not see get -infinity; `left`: keys of the tile that it sees.
