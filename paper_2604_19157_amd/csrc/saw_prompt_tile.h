@@ -122,8 +122,8 @@ struct RowState {
   float m, ref, sum;      // maximum that the state refers to (log2 units, -inf: none yet; ref: 0 then); this half's sum of weights
 };
 
-// S^T of one tile against the queries in qf.  The two halves of the keys alternate, since a product takes twice its time until its sum
-// can be added to, and operands are read six products ahead.
+// S^T of one tile against the queries in qf.  The two halves of the keys alternate, so that a product does not wait for the sum of the one
+// before it, and operands are read six products ahead (left to itself the compiler waits for each: 8192 causal tokens 530 us instead of 522).
 template <int D, typename M1>
 __device__ __forceinline__ void tile_logits(const char* k, const u32x4 (&qf)[D / 16], f32x16 (&s)[2], int lane) {
   constexpr int kAhead = 6, kAll = 2 * (D / 16);
