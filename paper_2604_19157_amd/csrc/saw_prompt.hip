@@ -318,8 +318,8 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
 // values to fp16 (an output is off by 1.4e-3 in fp16 and 2.0e-3 in bf16, 1.6e-3 of it bf16's own, where keys have channels 20
 // times as large as others; two limbs of the query as in saw_weights.hip would be half as much matrix work again).
 //   Bound by the matrix cores at the clock that they leave, with the exponentials behind them: 8192 causal tokens, 32 query and 8 kv heads
-// of 128 channels, 519 us, 1.06 PFLOP/s (a library product of 8192^3 1.27); 64 channels, where a logit has half the products, 0.87; 2048
-// tokens over 16384 in the pages 715 us, 0.82, with 200 M instructions of the vector ALU, 0.3 of them for the codes.
+// of 128 channels, 515 us, 1.07 PFLOP/s (a library product of 8192^3 1.27); 64 channels, where a logit has half the products, 0.87; 2048
+// tokens over 16384 in the pages 700 us, 0.83, with 200 M instructions of the vector ALU, 0.3 of them for the codes.
 template <int D, int KV, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
   constexpr int R = 32 * NW, kRow = 2 * D, kTile = kTileKeys * kRow, kInstr = kTile / 1024, kRpi = 1024 / kRow;
