@@ -207,18 +207,36 @@ __device__ __forceinline__ f32x2 key_codes(const KeyCodes<D>& codes, CodeBits bi
   return key0 + 16 * t + (lane & 15) < len ? codes.pair[t] : f32x2{0.f, 0.f};
 }
 
-// Logits of 16 rows and 16 keys, in log2 units divided by the rows' scales: of row 4 (lane / 16) + r and the lane's key.
-template <int D, typename Q>
-__device__ __forceinline__ f32x4 tile_logits16(const Q& tq, const u32x4 (&k)[D / 32], f32x2 pair) {
-  f32x4 s = {0.f, 0.f, 0.f, 0.f}, x;
+// Logits of 16 rows and N times 16 keys, in log2 units divided by the rows' scales: of row 4 (lane / 16) + r and the lane's keys.  The sums
+// of the 16 keys, or of one's limbs, alternate: a product would wait for the sum of the one before it.
+template <int D, int N, typename Q>
+__device__ __forceinline__ void tile_logits16(const Q& tq, const u32x4 (&k)[N][D / 32], const f32x2 (&pair)[N], f32x4 (&x)[N]) {
+  constexpr int kLimbSums = N == 1 ? 2 : 1;
+  f32x4 s[N][kLimbSums];
 #pragma unroll
-  for (int l = 1; l >= 0; --l)
+  for (int t = 0; t < N; ++t)
 #pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) s = mfma16(tq.limb(l, ks), k[ks], s);
-  const float z8 = pair.y - 8.f;
+    for (int l = 0; l < kLimbSums; ++l) s[t][l] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if constexpr (N == 1) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) x[r] = fmaf(-z8, tq.sum_q[r], s[r]) * pair.x;
-  return x;
+    for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+      for (int l = 1; l >= 0; --l) s[0][l] = mfma16(tq.limb(l, ks), k[0][ks], s[0][l]);
+    s[0][0] += s[0][1];
+  } else {
+#pragma unroll
+    for (int l = 1; l >= 0; --l)
+#pragma unroll
+      for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+        for (int t = 0; t < N; ++t) s[t][0] = mfma16(tq.limb(l, ks), k[t][ks], s[t][0]);
+  }
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    const float z8 = pair[t].y - 8.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[t][r] = fmaf(-z8, tq.sum_q[r], s[t][0][r]) * pair[t].x;
+  }
 }
 // Hidden ones and those behind the sequence's end become -infinity.  (Row i sees the keys in front of first_hidden + its token.)
 __device__ __forceinline__ void hide(f32x4& x, int key, int len, int first_hidden, int shift, int row0, int lane) {
@@ -284,8 +302,7 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
       const bool masked = key0 + kWeightKeys > min(first_hidden + (row0 >> shift), len);
       f32x4 x[4];
       if (g != held) load_tile(g);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) x[t] = tile_logits16<D>(tq, k[t], pair[t]);
+      tile_logits16<D>(tq, k, pair, x);
       if (masked)
 #pragma unroll
         for (int t = 0; t < 4; ++t) hide(x[t], key0 + 16 * t + (lane & 15), len, first_hidden, shift, row0, lane);
@@ -463,9 +480,11 @@ __global__ __launch_bounds__(64 * kStepWaves, 4) void weight_step_kernel(PromptP
         f32x4 x[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          u32x4 k[D / 32];
-          const f32x2 pair = key_codes<D>(codes, bits, t, key0, len, lane, k);
-          x[t] = tile_logits16<D>(tq, k, pair);
+          u32x4 k[1][D / 32];
+          const f32x2 pair[1] = {key_codes<D>(codes, bits, t, key0, len, lane, k[0])};
+          f32x4 of[1];
+          tile_logits16<D>(tq, k, pair, of);
+          x[t] = of[0];
 #pragma unroll
           for (int r = 0; r < 4; ++r) x[t][r] *= tq.scale[r];
           if (masked) hide(x[t], key0 + 16 * t + (lane & 15), len, first_hidden, shift, row0, lane);
