@@ -240,28 +240,47 @@ __global__ __launch_bounds__(1024) void evict_digit_kernel(EvictParams p, Segmen
   for (int d = tid; d < kBins; d += 1024) ws.hist[(row * ws.segments + seg) * kBins + d] = bin_of(hist, d);
 }
 
+// f(key) for the m keys of a list, by a wavefront, eight loads in flight
+template <typename F>
+__device__ __forceinline__ void each_listed(const uint32_t* list, int m, int lane, F f) {
+  for (int i = lane; i < m; i += 64 * 8) {
+    uint32_t key[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) key[u] = list[min(i + 64 * u, m - 1)];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i + 64 * u < m) f(key[u]);
+  }
+}
+
 // first digit of the last key that is kept, from the segments' counts
 __device__ __forceinline__ void pick_first(const SegmentSpace& ws, int64_t row, int segments, int want, int tid, int lane, int* hist, int (&pick)[3]) {
-  for (int d = tid; d < kBins; d += 1024) {
-    int n = 0;
-#pragma unroll 4
-    for (int g = 0; g < segments; ++g) n += ws.hist[(row * ws.segments + g) * kBins + d];
-    hist[d * kCopies] = n;
+  // (two bins a thread, and sixteen segments' on their way at once: a load waits longer than it works)
+  const int2* const from = (const int2*)(ws.hist + row * ws.segments * kBins) + tid;
+  int2 n = make_int2(0, 0);
+  for (int g0 = 0; g0 < segments; g0 += 16) {
+    int2 v[16];
 #pragma unroll
-    for (int c = 1; c < kCopies; ++c) hist[d * kCopies + c] = 0;
+    for (int k = 0; k < 16; ++k) v[k] = from[(int64_t)min(g0 + k, segments - 1) * (kBins / 2)];
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (g0 + k < segments) { n.x += v[k].x; n.y += v[k].y; }
   }
+  static_assert(kBins == 2 * 1024 && kCopies == 4, "two bins a thread");
+  ((int4*)hist)[2 * tid] = make_int4(n.x, 0, 0, 0);
+  ((int4*)hist)[2 * tid + 1] = make_int4(n.y, 0, 0, 0);
   __syncthreads();
   if (tid < 64) pick_bin(hist, want, lane, pick);
   __syncthreads();
 }
 
-__global__ __launch_bounds__(1024) void evict_list_kernel(EvictParams p, SegmentSpace ws) {
+__global__ __launch_bounds__(1024, 8) void evict_list_kernel(EvictParams p, SegmentSpace ws) {
   const int b = blockIdx.z, h = blockIdx.y, seg = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int len = min(max(p.seq_lens[b], 0), p.bound), old = max(len - p.recent, 0);
   const int j0 = seg * kSegment, j1 = min(old, j0 + kSegment);
   if (len <= p.budget || j0 >= len) return;
   const int64_t row = (int64_t)b * p.n_kv_heads + h;
-  __shared__ int hist[kBins * kCopies];
+  __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];
   __shared__ int pick[3];
   __shared__ int count, above;
   if (tid == 0) count = above = 0;
@@ -275,7 +294,7 @@ __global__ __launch_bounds__(1024) void evict_list_kernel(EvictParams p, Segment
   if (tid == 0) ws.counts[row * ws.segments + seg] = make_int2(above, count);
 }
 
-__global__ __launch_bounds__(1024) void evict_write_kernel(EvictParams p, SegmentSpace ws) {
+__global__ __launch_bounds__(1024, 8) void evict_write_kernel(EvictParams p, SegmentSpace ws) {
   const int b = blockIdx.z, h = blockIdx.y, seg = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = min(max(p.seq_lens[b], 0), p.bound), old = max(len - p.recent, 0), n = min(len, p.budget);
   const int64_t row = (int64_t)b * p.n_kv_heads + h;
@@ -290,7 +309,7 @@ __global__ __launch_bounds__(1024) void evict_write_kernel(EvictParams p, Segmen
   }
   const int j0 = seg * kSegment, j1 = min(len, j0 + kSegment);
   if (len <= p.budget || j0 >= len) return;
-  __shared__ int hist[kBins * kCopies];
+  __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];
   __shared__ int pick[3];
   __shared__ int2 sums[16];
   __shared__ int before[2];
@@ -306,13 +325,9 @@ __global__ __launch_bounds__(1024) void evict_write_kernel(EvictParams p, Segmen
     __syncthreads();
     for (int g = wave; g < segments; g += 16) {              // (a wavefront a list)
       const int64_t at = row * ws.segments + g;
-      const int m = ws.counts[at].y;
-      const uint32_t* const list = ws.list + at * kSegment;
-#pragma unroll 4
-      for (int i = lane; i < m; i += 64) {
-        const uint32_t key = list[i];
+      each_listed(ws.list + at * kSegment, ws.counts[at].y, lane, [&](uint32_t key) {
         if (key >> above == prefix >> above) atomicAdd(&hist[((key >> shift) & (bins - 1)) * kCopies + lane % kCopies], 1);
-      }
+      });
     }
     __syncthreads();
     if (wave == 0) pick_bin(hist, want, lane, pick);
@@ -324,13 +339,11 @@ __global__ __launch_bounds__(1024) void evict_write_kernel(EvictParams p, Segmen
   for (int g = wave; g < seg; g += 16) {
     const int64_t at = row * ws.segments + g;
     const int2 c = ws.counts[at];
-    const uint32_t* const list = ws.list + at * kSegment;
     int above = 0, ties = 0;
-#pragma unroll 4
-    for (int i = lane; i < c.y; i += 64) {
-      above += list[i] > prefix;
-      ties += list[i] == prefix;
-    }
+    each_listed(ws.list + at * kSegment, c.y, lane, [&](uint32_t key) {
+      above += key > prefix;
+      ties += key == prefix;
+    });
     for (int d = 1; d < 64; d <<= 1) { above += __shfl_xor(above, d); ties += __shfl_xor(ties, d); }
     if (lane == 0) {
       // (positions from `old` on are kept; where a segment in front of this one reaches them its end does)
