@@ -81,19 +81,21 @@ struct Last {
   __device__ bool tie(int at, float f) const { return at < old && (nan ? f != f : f == score); }
 };
 
-// Kept positions of [j0, j1) by each of the block's 16 wavefronts: they count what they keep, then write it behind what the wavefronts in
+// Kept positions of those that each(f) calls f(position, score) with, ascending over the lanes and calls (from j1 on: none), by each of the
+// block's 16 wavefronts: they count what they keep, then write it behind what the wavefronts in
 // front of them keep, and the block behind `done` kept tokens with `tied` equals of the last among them.
-__device__ __forceinline__ void write_kept(const float* s, int j0, int j1, int wave, int lane, const Last& last, int want, int done, int tied,
+template <typename E>
+__device__ __forceinline__ void write_kept(E each, int j1, int wave, int lane, const Last& last, int want, int done, int tied,
                                            int2* sums, int32_t* kept, float* out) {
   int above = 0, ties = 0;
-  for_scores(s, j0, j1, lane, 64, [&](int at, float f) {
+  each([&](int at, float f) {
     above += __popcll(__ballot(at < j1 && last.above(at, f)));
     ties += __popcll(__ballot(at < j1 && last.tie(at, f)));
   });
   if (lane == 0) sums[wave] = make_int2(above, ties);
   __syncthreads();
   for (int w = 0; w < wave; ++w) { done += sums[w].x; tied += sums[w].y; }
-  for_scores(s, j0, j1, lane, 64, [&](int at, float f) {
+  each([&](int at, float f) {
     const bool over = at < j1 && last.above(at, f), tie = at < j1 && last.tie(at, f);
     const uint64_t om = __ballot(over), tm = __ballot(tie);
     if (om | tm) {
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(1024, 8) void evict_select_kernel(EvictParams p) {
   // `want` of the tokens whose key is `prefix` are kept, the lowest positions first
   const Last last(prefix, old);
   const int share = (len + 1023) / 1024 * 64, j0 = wave * share, j1 = min(len, j0 + share);
-  write_kept(s, j0, j1, wave, lane, last, want, 0, 0, sums, kept, out);
+  write_kept([&](auto f) { for_scores(s, j0, j1, lane, 64, f); }, j1, wave, lane, last, want, 0, 0, sums, kept, out);
 }
 
 // The same for few long rows, by a block for every 8192 positions in three launches: digits of the segments; candidates of the segments, whose
@@ -314,6 +316,11 @@ __global__ __launch_bounds__(1024, 8) void evict_write_kernel(EvictParams p, Seg
   __shared__ int2 sums[16];
   __shared__ int before[2];
   const int segments = (len + kSegment - 1) / kSegment;
+  constexpr int kMine = kSegment / 1024;         // of the lane, requested before the steps that they wait for
+  const int w0 = j0 + wave * (kSegment / 16);
+  float mine[kMine];
+#pragma unroll
+  for (int u = 0; u < kMine; ++u) mine[u] = s[min(w0 + 64 * u + lane, j1 - 1)];
   if (tid == 0) before[0] = before[1] = 0;
   pick_first(ws, row, segments, p.budget - p.recent, tid, lane, hist, pick);
   uint32_t prefix = (uint32_t)pick[0] << 21;
@@ -353,8 +360,10 @@ __global__ __launch_bounds__(1024, 8) void evict_write_kernel(EvictParams p, Seg
   }
   __syncthreads();
   const Last last(prefix, old);
-  const int share = kSegment / 16, w0 = j0 + wave * share;
-  write_kept(s, w0, min(j1, w0 + share), wave, lane, last, want, before[0], before[1], sums, kept, out);
+  write_kept([&](auto f) {
+#pragma unroll
+    for (int u = 0; u < kMine; ++u) f(w0 + 64 * u + lane, mine[u]);
+  }, j1, wave, lane, last, want, before[0], before[1], sums, kept, out);
 }
 
 // The kept tokens' codes and pairs, a thread for 16 bytes of K and of V of four tokens: where a token lies takes three loads one after the
