@@ -205,8 +205,8 @@ __global__ __launch_bounds__(1024, 8) void evict_select_kernel(EvictParams p) {
 }
 
 // The same for few long rows, by a block for every 8192 positions in three launches: digits of the segments; candidates of the segments, whose
-// first digit every block picks by itself from all segments' counts; the remaining digits, again by every block, and the segment's kept
-// positions.  (131072 tokens, 8 heads: 4.4, 10.6 and 16.6 us; one block a row took 120, bound by the instructions that a single compute unit
+// first digit every block picks by itself from all segments' counts; the remaining digits, by every block from all segments' candidates, and
+// the segment's kept positions.  (131072 tokens, 8 heads: 4.4, 10.6 and 16.6 us; one block a row took 120, bound by the instructions that a single compute unit
 // issues.)
 constexpr int kSegment = 8192;
 
@@ -214,11 +214,13 @@ struct SegmentSpace {
   int* hist;                // [row][segment][kBins]
   uint32_t* list;           // [row][segment][kSegment]
   int2* counts;             // [row][segment]: scores above the first digit of the last, candidates
+  int2* first;              // [row]: that digit, how many of it are wanted
   int segments;
   __host__ __device__ SegmentSpace(void* ws, int64_t rows, int segments) : segments(segments) {
     hist = (int*)ws;
     list = (uint32_t*)(hist + rows * segments * kBins);
     counts = (int2*)(list + rows * segments * kSegment);
+    first = counts + rows * segments;
   }
 };
 
@@ -287,6 +289,7 @@ __global__ __launch_bounds__(1024, 8) void evict_list_kernel(EvictParams p, Segm
   __shared__ int count, above;
   if (tid == 0) count = above = 0;
   pick_first(ws, row, (len + kSegment - 1) / kSegment, p.budget - p.recent, tid, lane, hist, pick);
+  if (seg == 0 && tid == 0) ws.first[row] = make_int2(pick[0], pick[1]);
   list_candidates(p.scores + row * p.score_stride, j0, j1, tid, lane, (uint32_t)pick[0] << 21, ws.list + (row * ws.segments + seg) * kSegment, &count);
   int mine = 0;                                  // scores of larger digits
   for (int d = tid; d < kBins; d += 1024)
@@ -322,9 +325,9 @@ __global__ __launch_bounds__(1024, 8) void evict_write_kernel(EvictParams p, Seg
 #pragma unroll
   for (int u = 0; u < kMine; ++u) mine[u] = s[min(w0 + 64 * u + lane, j1 - 1)];
   if (tid == 0) before[0] = before[1] = 0;
-  pick_first(ws, row, segments, p.budget - p.recent, tid, lane, hist, pick);
-  uint32_t prefix = (uint32_t)pick[0] << 21;
-  int want = pick[1];
+  const int2 first = ws.first[row];
+  uint32_t prefix = (uint32_t)first.x << 21;
+  int want = first.y;
   for (int digit = 1; digit < 3; ++digit) {
     const int shift = digit == 1 ? 10 : 0, bins = digit == 1 ? kBins : 1024, above = digit == 1 ? 21 : 10;
     __syncthreads();
@@ -411,7 +414,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
 static int evict_segments(int64_t rows, int64_t bound) { return rows < 128 && bound > 16384 ? (int)((bound + kSegment - 1) / kSegment) : 0; }
 size_t evict_bytes(int64_t rows, int64_t bound) {
   const size_t segments = evict_segments(rows, bound);
-  return segments * rows * (kBins * 4 + kSegment * 4 + 8);
+  return segments * rows * (kBins * 4 + kSegment * 4 + 8) + (segments ? rows * 8 : 0);
 }
 
 int launch_evict(const EvictParams& p, int B, int D, void* ws, hipStream_t st) {
