@@ -206,7 +206,7 @@ __global__ __launch_bounds__(1024, 8) void evict_select_kernel(EvictParams p) {
 
 // The same for few long rows, by a block for every 8192 positions in three launches: digits of the segments; candidates of the segments, whose
 // first digit every block picks by itself from all segments' counts; the remaining digits, by every block from all segments' candidates, and
-// the segment's kept positions.  (131072 tokens, 8 heads: 4.4, 10.6 and 16.6 us; one block a row took 120, bound by the instructions that a single compute unit
+// the segment's kept positions.  (131072 tokens, 8 heads: 4.6, 8.4 and 13.7 us; one block a row took 120, bound by the instructions that a single compute unit
 // issues.)
 constexpr int kSegment = 8192;
 
