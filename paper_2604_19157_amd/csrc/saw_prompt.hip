@@ -149,8 +149,8 @@ __device__ __forceinline__ void rescale(RowState<D>& st, float by) {
 
 // The queries of a lane column as B operand: channels of k-step ks, half h and place i have bits (ks, h, i), h at bit HALF_BIT.  Those for
 // the INT4 pages are rotated here, in registers, and become fp16 times 2^-e (prompt_query_kernel does the same for a learned rotation);
-// returns what turns a logit into log2 units.
-template <int D, int KV, int HALF_BIT>
+// returns what turns a logit into log2 units.  CODES: the eight channels of a word of codes in the order of `centred`.
+template <int D, int KV, int HALF_BIT, bool CODES = false>
 __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token, int head, int lane, u32x4 (&qf)[D / 16]) {
   const int half = lane >> 5;
   const bool ready = KV == kKvInt4 && p.dense_k;
@@ -159,7 +159,15 @@ __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token,
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const u32x4*)(src + (spread_channel<HALF_BIT>(8 * ks) | half << HALF_BIT));
   if constexpr (KV == kKvInt4) {
-    if (ready) return p.scale * p.query_scale[at];
+    if (ready) {
+      if (CODES)
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const u32x4 w = qf[ks];
+          qf[ks] = u32x4{(w.x & 0xffffu) | w.z << 16, w.x >> 16 | (w.z & 0xffff0000u), (w.y & 0xffffu) | w.w << 16, w.y >> 16 | (w.w & 0xffff0000u)};
+        }
+      return p.scale * p.query_scale[at];
+    }
     float x[D / 2];
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks)
@@ -184,7 +192,8 @@ __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token,
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) qf[ks][i] = MathF16::pack(x[8 * ks + 2 * i] * down, x[8 * ks + 2 * i + 1] * down);
+      for (int i = 0; i < 4; ++i)
+        qf[ks][i] = CODES ? MathF16::pack(x[8 * ks + i] * down, x[8 * ks + i + 4] * down) : MathF16::pack(x[8 * ks + 2 * i] * down, x[8 * ks + 2 * i + 1] * down);
     return p.scale * __uint_as_float((uint32_t)(127 + ex) << 23);
   }
   return p.scale;
@@ -199,7 +208,7 @@ __device__ __forceinline__ float2* partial_sums(const PromptParams& p) {
 
 // The end of a wavefront's 32 rows: outputs, or partial records [split][row][D] and [split][row] (maximum, sum) where the keys are split
 // or a learned rotation has to be undone.  scale: of the rows' logits; unit: of the output sums.
-template <int D, int KV, int HALF_BIT>
+template <int D, int KV, int HALF_BIT, bool CODES = false>
 __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile& rt, int w0, int last, int row, int h, int64_t token, int head,
                                             int k0, int len, int t0, int t1, const u32x4 (&qf)[D / 16], float scale, float unit, RowState<D>& st, int lane) {
   constexpr bool kInt4 = KV == kKvInt4;
@@ -232,7 +241,8 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
       // (channel c of row i is in register c's place of lane i or i + 32)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int c = lane + 64 * e, half = (c >> HALF_BIT) & 1, v = (c & ((1 << HALF_BIT) - 1)) | c >> (HALF_BIT + 1) << HALF_BIT;
+        const int c = lane + 64 * e, half = (c >> HALF_BIT) & 1, in = (c & ((1 << HALF_BIT) - 1)) | c >> (HALF_BIT + 1) << HALF_BIT;
+        const int v = CODES ? (in & ~7) | 2 * (in & 3) | ((in >> 2) & 1) : in;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
@@ -452,16 +462,19 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Few rows over the INT4 pages (draft tokens to verify, a decode step's queries): a block takes 32 rows, and its wavefronts share out the
 // keys, every fourth tile each, so that none waits for another until they join their states at the end.  Keys go from memory to operand
-// registers - a lane holds one half of one key's channels, which the queries' k-steps follow -, values through 64 rows of shared
-// memory of the wavefront's own for the transposing reads.
-//   Bound by the vector ALU, 1360 instructions for 64 keys, over half of them for the codes: 32 sequences of 5 tokens over 512 to 4096, 88
-// MB, 52 us and 6.7 for the merge.
+// registers as exact codes - a lane holds one half of one key's channels, which the queries' k-steps follow - and their scales and zero-points to
+// the logits, as in saw_weights.hip: half of the instructions of dequantised keys (16 tokens a sequence 79 -> 74 us); with 128 rows a
+// block, where codes are widened once for all, it would be more of them.  Values go through 64 rows of shared memory of the wavefront's own for
+// the transposing reads.
+//   Bound by the vector ALU, 1200 instructions for 64 keys, half of them for the codes: 32 sequences of 5 tokens over 512 to 4096, 88 MB, 49
+// us and 6.7 for the merge.
 template <int D>
 __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   constexpr int NW = 4, kRow = 2 * D, kTile = kTileKeys * kRow, kHalfBit = D == 128 ? 6 : 5, kWords = D / 16, kPieces = D / 32;
   static_assert(kTile == 64 * (D / 2) * 4, "a state fits the wavefront's tile");
   __shared__ __attribute__((aligned(1024))) char lds[NW][kTile];
   __shared__ float2 join[NW][64];
+  __shared__ __attribute__((aligned(16))) f32x2 pairs[NW][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % p.n_kv_heads;
   RowTile rt;
@@ -484,7 +497,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   char* const mine = lds[wave];
 
   u32x4 kc[2][kWords / 4], vc[kPieces];
-  f32x2 kpair[2], vpair[kPieces];
+  f32x2 kpair, vpair[kPieces];                                            // (of key `lane`; of the pieces' tokens)
   TilePages ids;
   auto request = [&] {
     ids.ready(p, h);
@@ -495,8 +508,8 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
       const u32x4* const src = (const u32x4*)(vector_codes<D>(p.k_codes, tile, key) + (lane >> 5) * (D / 4));
 #pragma unroll
       for (int i = 0; i < kWords / 4; ++i) kc[kb][i] = src[i];
-      kpair[kb] = *vector_pair(p.k_meta, tile, key);
     }
+    kpair = *vector_pair(p.k_meta, ids.tile_of(lane), lane);
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
       const int piece = 64 * j + lane, key = piece / kPieces;
@@ -511,7 +524,14 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     ids.fetch(pages, t0 + wave + NW, len);
   }
   u32x4 qf[D / 16];
-  const float scale = row_query<D, kKvInt4, kHalfBit>(p, token, head, lane, qf);
+  const float scale = row_query<D, kKvInt4, kHalfBit, true>(p, token, head, lane, qf);
+  float sum_q = 0.f;                                                      // of the row's channels as they are multiplied
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum_q += f16_to_f32(qf[ks][i] & 0xffffu) + f16_to_f32(qf[ks][i] >> 16);
+  sum_q = add_xor32(sum_q);
+  const CodeBits bits;
   RowState<D> st;
   st.m = -INFINITY; st.ref = 0.f; st.sum = 0.f;
 #pragma unroll
@@ -519,24 +539,10 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) st.o[t][r] = 0.f;
 
-  Unit keys, values;
+  Unit values;
   const int seen = max(sees_of(rt.row0), (t0 + wave) * kTileKeys + 1);
   for (int t = t0 + wave; t < t1; t += NW) {
     // (slots behind the end may hold anything)
-    float s[2], sz[2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      const bool there = t * kTileKeys + 32 * kb + (lane & 31) < len;
-      s[kb] = there ? kpair[kb].x : 0.f;
-      sz[kb] = there ? kpair[kb].x * kpair[kb].y : 0.f;
-    }
-    auto largest_key = [&](int end) {
-      float top = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-        if (t * kTileKeys + 32 * kb + (lane & 31) < end) top = fmaxf(top, largest_value(kpair[kb]));
-      return top;
-    };
     auto largest_of_values = [&](int end) {
       float top = 0.f;
 #pragma unroll
@@ -546,18 +552,28 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     };
     int by;
     const bool whole = (t + 1) * kTileKeys <= seen;
-    keys.fit(largest_key(len), t == t0 + wave, whole, by, [&] { return largest_key(seen); });
-    const float down = keys.down();
     if (values.fit(largest_of_values(len), t == t0 + wave, whole, by, [&] { return largest_of_values(seen); })) rescale<D>(st, power_of_two(-by));
     const float down_v = values.down();
+    // logits: s_j (q . (c_j - 8) - (z_j - 8) sum q), with the codes exact and each pair from shared memory where its key stands
+    pairs[wave][lane] = t * kTileKeys + lane < len ? f32x2{kpair.x, 8.f - kpair.y} : f32x2{0.f, 0.f};
     f32x16 x[2];
     u32x4 pf[4];
+    wave_sync();
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[kb][r] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) x[kb] = MathF16::mfma(widen_codes<MathF16>(kc[kb][ks / 4][ks % 4], s[kb] * down, sz[kb] * down), qf[ks], x[kb]);
+      for (int ks = 0; ks < D / 16; ++ks) x[kb] = MathF16::mfma(centred(kc[kb][ks / 4][ks % 4], bits), qf[ks], x[kb]);
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        const f32x4 two = *(const f32x4*)&pairs[wave][32 * kb + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 2)];
+        x[kb][r] = fmaf(two.y, sum_q, x[kb][r]) * two.x;
+        x[kb][r + 1] = fmaf(two.w, sum_q, x[kb][r + 1]) * two.z;
+      }
+      // (128 channels: or the compiler puts this off until the values are written, with all pairs in registers, and spills: 54 us become 87.  With
+      // 64 they fit: 36 us put off, 38 in place.)
+      if (D == 128) asm volatile("" : "+v"(x[kb]));
     }
     wave_sync();
 #pragma unroll
@@ -572,13 +588,13 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
       ids.fetch(pages, t + 2 * NW, len);
     }
     if ((t + 1) * kTileKeys > kfull) tile_mask(x, sees - t * kTileKeys, lane);
-    tile_weights<D, MathF16>(x, scale * keys.up(), st, pf);
+    tile_weights<D, MathF16>(x, scale, st, pf);
     tile_values<D, MathF16>(mine, pf, st, lane);
   }
   // the other wavefronts' states join the first's
   wave_sync();
   rescale<D>(st, values.up());
-  if (keys.lost || values.lost) st.o[0][0] = NAN;
+  if (values.lost) st.o[0][0] = NAN;
   if (wave > 0) {
 #pragma unroll
     for (int i = 0; i < D / 2; i += 4) *(f32x4*)(mine + i * 256 + 16 * lane) = f32x4{st.o[i / 16][i % 16], st.o[i / 16][i % 16 + 1], st.o[i / 16][i % 16 + 2], st.o[i / 16][i % 16 + 3]};
@@ -604,7 +620,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     }
   }
   st.m = m;
-  finish_rows<D, kKvInt4, kHalfBit>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, qf, scale, 1.f, st, lane);
+  finish_rows<D, kKvInt4, kHalfBit, true>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, qf, scale, 1.f, st, lane);
 }
 
 // Joins the partial records of a row: one wavefront a row, eight records on their way at once.  5120 rows in two splits 6.7 us, most of it

@@ -101,6 +101,21 @@ __device__ __forceinline__ const f32x2* vector_pair(const float* meta, uint32_t 
   return (const f32x2*)((const char*)meta + (uint64_t)tile * 128 + (uint32_t)(key & 15) * 8);
 }
 
+// codes - 8 of a word, in the order 0 4 1 5 2 6 3 7: 0x6400 + c is 1024 + c.  (The two constants in registers: with both as literals the
+// masking is two instructions.)
+struct CodeBits {
+  uint32_t mask, one;
+  __device__ __forceinline__ CodeBits() { asm("v_mov_b32 %0, 0xf000f\n\tv_mov_b32 %1, 0x64006400" : "=&v"(mask), "=v"(one)); }
+};
+__device__ __forceinline__ u32x4 centred(uint32_t w, CodeBits bits) {
+  u32x4 r;
+  const f16x2 off = {(_Float16)1032.f, (_Float16)1032.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, ((w >> (4 * i)) & bits.mask) | bits.one) - off);
+  return r;
+}
+
 // A tile of 64 keys in shared memory: rows of D 16-bit values in 16-byte chunks, the chunks of a row exchanged so that whatever a
 // read takes at once (256 bytes a clock) lies on different banks.  K: operand reads take one chunk of 16 rows.  V: transposing reads take 32
 // bytes of four rows for each 16 lanes.  Rows of 64 channels stand two to 256 bytes.  (Exchanges that keep only 128 bytes a clock apart:

@@ -156,21 +156,6 @@ struct KeyStream {
   }
 };
 
-// codes - 8 of a word, in the order 0 4 1 5 2 6 3 7: 0x6400 + c is 1024 + c.  (The two constants in registers: with both as literals the
-// masking is two instructions.)
-struct CodeBits {
-  uint32_t mask, one;
-  __device__ __forceinline__ CodeBits() { asm("v_mov_b32 %0, 0xf000f\n\tv_mov_b32 %1, 0x64006400" : "=&v"(mask), "=v"(one)); }
-};
-__device__ __forceinline__ u32x4 centred(uint32_t w, CodeBits bits) {
-  u32x4 r;
-  const f16x2 off = {(_Float16)1032.f, (_Float16)1032.f};
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, ((w >> (4 * i)) & bits.mask) | bits.one) - off);
-  return r;
-}
-
 // A row tile in a wavefront's registers.
 template <int D>
 struct TileQueries {
