@@ -677,23 +677,29 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int s
 
 // How a call is handed out: rows of a block, splits of the keys.
 //   * INT4 pages and at most 64 rows a sequence on average: blocks of 32 rows whose wavefronts share out the keys (32 sequences of 512 to 4096
-//     tokens, 32 query / 8 kv heads: 5 new tokens 54 us, 181 in blocks of 128 rows; 16 tokens 85, 24 tokens, in blocks of 128, 200);
+//     tokens, 32 query / 8 kv heads: 5 new tokens 54 us, 181 in blocks of 128 rows); at most 192 with 128 to 384 (sequence, kv head) pairs, where
+//     blocks of 128 rows are too few to be dealt out evenly (blocks of 32 and of 128 rows: 24 tokens, 16 sequences 70 us and 69, 24 94 and 106,
+//     32 113 and 126, 48 171 and 182; 32 x 48 160 and 171; 31 x 1 and one chunk of 700 104 and 165; but 8 x 24 51 and 43, 64 x 24 206 and 185,
+//     32 x 64 199 and 190);
 //   * 4096 rows a sequence and more, and a block for every compute unit: 256 rows, eight wavefronts, so that keys are brought in (and
 //     codes widened) half as often (8192 causal tokens 520 us, 544 in blocks of 128; 2048 tokens over 16384 in the pages 708 and 777; but 19
 //     packed prompts of 60 to 1437 tokens 181 and 178, four short ones 13.2 and 11.2);
 //   * 128 rows otherwise.
-// Keys are split while a call has fewer blocks than the chip holds, two for a compute unit (few rows: where it has under 900 of four
-// wavefronts that go their own ways; 640: 80 us instead of 59, 2560: 67), into parts of 256 keys at least.  A split where the
-// chip is full already costs its records: two sequences of 2000 tokens, 512 blocks, 88 us, in two splits 161.
+// Keys are split while a call has fewer blocks than the chip holds, two for a compute unit (a little more in blocks of 32 rows, whose
+// wavefronts go their own ways: two splits of 256 blocks 54 us, one 80, three 58), into parts of 256 keys at least.  Blocks are counted as those of
+// sequences of like length: the grid has one more for each sequence, of which many are empty (with those counted too, 8 x 24 tokens 56 us instead
+// of 43, 4 x 256 137 instead of 115).  A split where the chip is full already costs its records: two sequences of 2000 tokens, 512 blocks, 88 us,
+// in two splits 161.
 struct PromptPlan { int rows, splits; };
 constexpr int kMaxKeySplits = 64;
 static PromptPlan prompt_plan(bool int4, int D, int G, int Hkv, int64_t T, int B, int64_t max_k_len) {
   PromptPlan r = {128, 1};
   int64_t want = 512;
-  if (int4 && T * G <= 64 * (int64_t)B) { r.rows = 32; want = 900; }
+  const int64_t pairs = (int64_t)B * Hkv;
+  if (int4 && T * G <= (pairs >= 128 && pairs <= 384 ? 192 : 64) * (int64_t)B) { r.rows = 32; want = 560; }
   else if ((D == 128 || !int4) && T * G >= 4096 * (int64_t)B && row_tiles(T, G, 256, B) * Hkv >= 256) r.rows = 256;
-  const int64_t blocks = row_tiles(T, G, r.rows, B) * Hkv;
-  int64_t s = want / blocks, most = (max_k_len + 255) / 256;
+  const int64_t all = (int64_t)B * r.rows, blocks = B * ((T * G + all - 1) / all) * Hkv;             // of sequences of like length
+  int64_t s = want / (blocks < 1 ? 1 : blocks), most = (max_k_len + 255) / 256;
   if (r.rows == 256) s = 1;
   if (s > most) s = most;
   r.splits = s < 1 ? 1 : s > kMaxKeySplits ? kMaxKeySplits : (int)s;

@@ -130,6 +130,14 @@ def test_workspaces(saw):
     assert L.saw_evict_workspace_bytes(r, 1, 131072) > 0 and L.saw_evict_workspace_bytes(r, 4, 1000) == 0 and L.saw_evict_workspace_bytes(None, 1, 1000) == 0
 
 
+def test_workspaces_without_queries(saw):
+    L, r = saw.lib(), ctypes.byref(_cache(saw))
+    for B in (1, 7, 65535):
+        assert L.saw_prompt_workspace_bytes(128, 32, 8, 0, B, 1000) == 16
+        assert 0 < L.saw_paged_prompt_workspace_bytes(r, 32, 0, B, 1000) <= 64 and L.saw_attn_weights_workspace_bytes(r, 32, 0, B, 1000) > 0
+    assert L.saw_prompt_attn(*{**PROMPT, "T_q": 0}.values()) == 0
+
+
 @pytest.fixture(params=["native", "ctypes"])
 def marshal(request, saw):
     if request.param == "ctypes":
