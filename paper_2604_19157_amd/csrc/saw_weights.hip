@@ -239,8 +239,9 @@ __device__ __forceinline__ void row_allmax4(float (&v)[4]) { asm(ROW_ALL4("v_max
 __device__ __forceinline__ void row_allsum4(float (&v)[4]) { asm(ROW_ALL4("v_add_f32_dpp") : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3])); }
 
 // One pass over a chunk of the keys of a (sequence, kv head).  STATS: maximum and sum of each row of a group of row tiles over the
-// chunk; otherwise the weights of the chunk's keys over all rows.
-template <int D, bool STATS>
+// chunk; otherwise the weights of the chunk's keys over all rows.  The wavefronts of a block share out the chunk's keys, or, SHARE_ROWS, the row
+// tiles, and then add up their weights.
+template <int D, bool STATS, bool SHARE_ROWS>
 __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int64_t tiles, int chunk_keys) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % p.n_kv_heads, chunk = blockIdx.x / p.n_kv_heads, b = blockIdx.y;
@@ -256,6 +257,7 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
   const int k0 = chunk * chunk_keys, k1 = min(len, k0 + chunk_keys);
   if (STATS && g0 >= g1) return;
   __shared__ float2 stats[4][STATS ? kGroupTiles * kWeightRows : 1];
+  __shared__ float sums[4][STATS || !SHARE_ROWS ? 1 : kWeightKeys];
   if (STATS) {
     for (int r = lane; r < (g1 - g0) * kWeightRows; r += 64) stats[wave][r] = make_float2(-INFINITY, 0.f);
     wave_sync();
@@ -271,9 +273,11 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
   };
   KeyStream<D> keys;
   keys.pages = p.page_table + (int64_t)b * p.max_pages;
-  keys.end = k1; keys.stride = 4 * kWeightKeys; keys.len = len;
-  keys.start(p, h, k0 + kWeightKeys * wave, lane);
-  keys.each(k0 + kWeightKeys * wave, [&](int key0, KeyCodes<D>& codes) {
+  keys.end = k1; keys.stride = SHARE_ROWS ? kWeightKeys : 4 * kWeightKeys; keys.len = len;
+  constexpr int kTileStep = SHARE_ROWS ? 4 : 1;
+  const int start = SHARE_ROWS ? k0 : k0 + kWeightKeys * wave;
+  keys.start(p, h, start, lane);
+  keys.each(start, [&](int key0, KeyCodes<D>& codes) {
     u32x4 k[4][D / 32];
     f32x2 pair[4];
     float total[4] = {0.f, 0.f, 0.f, 0.f};
@@ -282,7 +286,7 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
     keys.next(p, h, key0, lane, codes);
     // the first row that sees a key of the step: key0 < first_hidden + token
     const int first_token = max(key0 - first_hidden + 1, 0);
-    for (int g = max(g0, (int)(((int64_t)first_token << shift) / kWeightRows)); g < g1; ++g) {
+    for (int g = max(g0, (int)(((int64_t)first_token << shift) / kWeightRows)) + (SHARE_ROWS ? wave : 0); g < g1; g += kTileStep) {
       const int row0 = g * kWeightRows;
       const bool masked = key0 + kWeightKeys > min(first_hidden + (row0 >> shift), len);
       f32x4 x[4];
@@ -296,7 +300,7 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
       for (int r = 0; r < 4; ++r) info[r] = tq.info[r];
       // (The next tile's queries arrive behind the exponentials: 32 tokens of 64 heads over 16000 keys 103 us, 111 without.  With 64
       // channels the registers for it cost a wavefront a SIMD: 86 us, 75 without.)
-      if (D == 128 && g + 1 < g1) load_tile(g + 1);
+      if (D == 128 && g + kTileStep < g1) load_tile(g + kTileStep);
       if constexpr (STATS) {
         float2* const mine = &stats[wave][(g - g0) * kWeightRows + 4 * (lane >> 4)];
         float top[4], sum[4], m[4], old[4];
@@ -346,7 +350,18 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
       for (int t = 0; t < 4; ++t) {
         const float w = add_xor32(add_xor16(total[t]));
         const int key = key0 + 16 * t + lane;
-        if (lane < 16 && key < len) p.scores[record + key] = (p.prev ? p.prev[record + key] : 0.f) + w;
+        if (SHARE_ROWS) {
+          if (lane < 16) sums[wave][16 * t + lane] = w;
+        } else if (lane < 16 && key < len) {
+          p.scores[record + key] = (p.prev ? p.prev[record + key] : 0.f) + w;
+        }
+      }
+      if (SHARE_ROWS) {                                                    // (all wavefronts are at the same keys)
+        __syncthreads();
+        const int key = key0 + lane;
+        if (wave == 0 && key < len)
+          p.scores[record + key] = (p.prev ? p.prev[record + key] : 0.f) + ((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
+        __syncthreads();
       }
     }
   });
@@ -577,28 +592,37 @@ __global__ __launch_bounds__(64 * kStepWaves, 4) void weight_step_kernel(PromptP
   }
 }
 
-static int weight_chunks(int Hkv, int B, int64_t bound) {
-  const int64_t items = (int64_t)B * Hkv;
+// How the passes are handed out: chunks of the keys, and what a block's wavefronts share out.  Its keys, 256 at a time, so that codes are turned
+// into operands once; its row tiles where a sequence has four and more and there are few blocks of 256 keys (sharing keys and rows: 10 x 131
+// tokens of 32 heads over 135 keys 89 us and 50, 24 x 60 over 74 89 and 61, 2 x 100 over 304 59 and 28, 1 x 185 over 3700 35 and 25; but 3 x
+// 200 of 64 heads over 3800, 480 blocks, 174 and 184, 8 x 210 over 15000 214 and 258).
+struct WeightPlan { int chunks, chunk_keys; bool share_rows; };
+static WeightPlan weight_plan(int G, int Hkv, int64_t T, int B, int64_t bound) {
+  const int64_t items = (int64_t)B * Hkv, tiles = T * G / ((int64_t)B * kWeightRows), wide = 4 * kWeightKeys;
+  const bool share_rows = tiles >= 4 && items * ((bound + wide - 1) / wide) <= 256;
+  const int64_t unit = share_rows ? kWeightKeys : wide, most = (bound + unit - 1) / unit;
   int64_t s = 2048 / items;
-  const int64_t most = (bound + 4 * kWeightKeys - 1) / (4 * kWeightKeys);
   if (s > most) s = most;
-  return s < 1 ? 1 : s > 256 ? 256 : (int)s;
+  if (s > 256) s = 256;
+  if (s < 1) s = 1;
+  return {(int)s, (int)(((bound + s - 1) / s + unit - 1) / unit * unit), share_rows};
 }
 
 size_t weights_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t bound) {
   const int64_t tiles = row_tiles(T, Hq / Hkv, kWeightRows, B);
-  return 16 + (size_t)tiles * Hkv * (2 * (D / 32) * 64 * 16 + kWeightRows * (sizeof(RowInfo) + (size_t)weight_chunks(Hkv, B, bound) * 8));
+  const WeightPlan plan = weight_plan(Hq / Hkv, Hkv, T, B, bound);
+  return 16 + (size_t)tiles * Hkv * (2 * (D / 32) * 64 * 16 + kWeightRows * (sizeof(RowInfo) + (size_t)plan.chunks * 8));
 }
 
-template <int D>
-static void launch_passes(const PromptParams& p, int64_t tiles, int chunks, int chunk_keys, hipStream_t st) {
-  const int groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles);
+template <int D, bool SHARE_ROWS>
+static void launch_passes(const PromptParams& p, int64_t tiles, const WeightPlan& plan, hipStream_t st) {
+  const int groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles), wide = p.n_kv_heads * plan.chunks;
   if (p.T_q) {
     weight_query_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(1024), 0, st>>>(p, tiles);
-    weight_pass_kernel<D, true><<<dim3(p.n_kv_heads * chunks, p.B, groups), dim3(256), 0, st>>>(p, tiles, chunk_keys);
-    weight_join_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(256), 0, st>>>(p, tiles, chunks);
+    weight_pass_kernel<D, true, SHARE_ROWS><<<dim3(wide, p.B, groups), dim3(256), 0, st>>>(p, tiles, plan.chunk_keys);
+    weight_join_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(256), 0, st>>>(p, tiles, plan.chunks);
   }
-  weight_pass_kernel<D, false><<<dim3(p.n_kv_heads * chunks, p.B), dim3(256), 0, st>>>(p, tiles, chunk_keys);
+  weight_pass_kernel<D, false, SHARE_ROWS><<<dim3(wide, p.B), dim3(256), 0, st>>>(p, tiles, plan.chunk_keys);
 }
 
 // One launch where a sequence has about one query: short contexts, whose four launches take longer than a block of one compute unit for each
@@ -614,18 +638,17 @@ static bool one_launch(const PromptParams& p) {
 
 int launch_weights(const PromptParams& p, int D, hipStream_t st) {
   const int64_t tiles = row_tiles(p.T_q, p.group, kWeightRows, p.B);
-  const int chunks = weight_chunks(p.n_kv_heads, p.B, p.bound), unit = 4 * kWeightKeys;
-  const int chunk_keys = (int)(((int64_t)(p.bound + chunks - 1) / chunks + unit - 1) / unit * unit);
+  const WeightPlan plan = weight_plan(p.group, p.n_kv_heads, p.T_q, p.B, p.bound);
   // (grids: widths below 2^32 threads, groups of tiles below 2^16)
-  if ((int64_t)p.n_kv_heads * chunks * 256 > 0xffffffffLL || (tiles + kGroupTiles - 1) / kGroupTiles > 65535) return SAW_EINVAL;
+  if ((int64_t)p.n_kv_heads * plan.chunks * 256 > 0xffffffffLL || (tiles + kGroupTiles - 1) / kGroupTiles > 65535) return SAW_EINVAL;
   if (one_launch(p)) {
     const dim3 grid(p.n_kv_heads, p.B);
     if (D == 128) weight_step_kernel<128><<<grid, dim3(64 * kStepWaves), 0, st>>>(p);
     else weight_step_kernel<64><<<grid, dim3(64 * kStepWaves), 0, st>>>(p);
     return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;
   }
-  if (D == 128) launch_passes<128>(p, tiles, chunks, chunk_keys, st);
-  else launch_passes<64>(p, tiles, chunks, chunk_keys, st);
+  if (D == 128) plan.share_rows ? launch_passes<128, true>(p, tiles, plan, st) : launch_passes<128, false>(p, tiles, plan, st);
+  else plan.share_rows ? launch_passes<64, true>(p, tiles, plan, st) : launch_passes<64, false>(p, tiles, plan, st);
   return hipGetLastError() == hipSuccess ? SAW_OK : SAW_ELAUNCH;
 }
 

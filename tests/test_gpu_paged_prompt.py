@@ -380,6 +380,18 @@ def test_long_contexts_split(saw, n, lens, G):
     pc.check(saw.paged_attn_weights(c.cache, *c.args, prev=torch.from_numpy(prev).cuda(), max_seq_len=max(lens)), want, tol)
 
 
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8)])
+@pytest.mark.parametrize("n,lens", [([70, 0, 33], [75, 9, 300]), ([200], [1900]), ([17, 150, 64, 1], [17, 131, 640, 5])], ids=str)
+def test_weights_of_many_queries_over_few_keys(saw, n, lens, d, G):
+    """Wavefronts share out the rows."""
+    c = Case(saw, n, lens, G=G, d=d, h=d, seed=7)
+    prev = np.random.default_rng(2).random((len(n), 2, max(lens) + 5)).astype(np.float32)
+    want, tol = _scores(c, prev)
+    got = saw.paged_attn_weights(c.cache, *c.args, prev=torch.from_numpy(prev).cuda(), max_seq_len=max(lens)).cpu()
+    for b, L in enumerate(lens):
+        pc.check(got[b, :, :L], want[b, :, :L], tol[b, :, :L], b)
+
+
 # ---- the calls together ----
 def test_pools_beyond_32_bits(saw):
     """Pages at the end of pools of 4.9 GiB of codes each: what they give at the front."""
