@@ -39,32 +39,37 @@ struct RowSource {
 // size, down to 2^-39 of the largest.
 __device__ __forceinline__ int query_exponent(float top) { return min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14; }
 
-// Queries under a learned rotation, whose 64 KiB a block of rows would read again: one wavefront a row.
+// Queries under a learned rotation, whose 64 KiB a block of rows would read again: a wavefront for NV rows, which read them once.
 //   ws: [rows][D] fp16 | [rows] float 2^e
-template <int D>
+template <int D, int NV>
 __global__ __launch_bounds__(256) void prompt_query_kernel(PromptParams p) {
   constexpr int E = D / 64;
-  __shared__ __attribute__((aligned(16))) float rows[4][128];
+  __shared__ __attribute__((aligned(16))) float rows[4][NV * 128];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n = p.T_q * p.n_q_heads, row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave;
-  if (row >= n) return;
-  const int64_t at = row / p.n_q_heads * p.q_stride + row % p.n_q_heads * D;
+  const int64_t n = p.T_q * p.n_q_heads, row0 = (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave) * NV;
+  if (row0 >= n) return;
   float* const x = rows[wave];
-  if (E == 1) x[lane + 64] = 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) x[lane + 64 * e] = load_elem(p.q, p.dtype, at + lane + 64 * e);
+  for (int v = 0; v < NV; ++v) {
+    const int64_t row = min(row0 + v, n - 1), at = row / p.n_q_heads * p.q_stride + row % p.n_q_heads * D;
+    if (E == 1) x[128 * v + lane + 64] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[128 * v + lane + 64 * e] = load_elem(p.q, p.dtype, at + lane + 64 * e);
+  }
   wave_sync();
-  rotate_row(p, x, D, lane);
-  float top = 0.f;
+  rotate_row<NV == 1 ? 16 : 8, NV>(p, x, D, lane);
+  for (int v = 0; v < NV && row0 + v < n; ++v) {
+    float top = 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[lane + 64 * e]));
-  top = max_xor32(max_xor16(row_allmax_positive(top)));
-  const int ex = query_exponent(top);
-  const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
-  uint16_t* const q = p.query + row * D;
+    for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[128 * v + lane + 64 * e]));
+    top = max_xor32(max_xor16(row_allmax_positive(top)));
+    const int ex = query_exponent(top);
+    const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+    uint16_t* const q = p.query + (row0 + v) * D;
 #pragma unroll
-  for (int e = 0; e < E; ++e) q[lane + 64 * e] = f32_to_f16(x[lane + 64 * e] * down);
-  if (lane == 0) p.query_scale[row] = __uint_as_float((uint32_t)(127 + ex) << 23);
+    for (int e = 0; e < E; ++e) q[lane + 64 * e] = f32_to_f16(x[128 * v + lane + 64 * e] * down);
+    if (lane == 0) p.query_scale[row0 + v] = __uint_as_float((uint32_t)(127 + ex) << 23);
+  }
 }
 
 // Keys and values of a tile on their way from the INT4 pages to shared memory: 16-byte pieces of 32 codes and the pairs of their tokens,
@@ -623,25 +628,20 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   finish_rows<D, kKvInt4, kHalfBit, true>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, qf, scale, 1.f, st, lane);
 }
 
-// Joins the partial records of a row: one wavefront a row, eight records on their way at once.  5120 rows in two splits 6.7 us, most of it
-// latency.
-template <int D, bool INT4>
-__global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int splits) {
+// The output of a row from its partial records; false: the row is no sequence's.
+template <int D>
+__device__ __forceinline__ bool merged_row(const PromptParams& p, int splits, int64_t row, int lane, float (&o)[D / 64]) {
   constexpr int E = D / 64;
-  __shared__ __attribute__((aligned(16))) float rotated[4][128];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t rows = p.T_q * p.n_q_heads, row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave;
-  if (row >= rows) return;
+  const int64_t rows = p.T_q * p.n_q_heads;
   const int64_t token = row / p.n_q_heads;
   const int b = last_not_above(p.B, token, lane, [&](int i) { return clamped_offset(p.cu_q, i, p.T_q); });
-  if (b < 0 || token >= clamped_offset(p.cu_q, b + 1, p.T_q)) return;
+  if (b < 0 || token >= clamped_offset(p.cu_q, b + 1, p.T_q)) return false;
   const float2* const ml = (const float2*)(p.ws + (int64_t)splits * rows * D);
   float2 mine = make_float2(-INFINITY, 0.f);                              // (a split a lane: kMaxKeySplits of them)
   if (lane < splits) mine = ml[lane * rows + row];
   const float m = max_xor32(max_xor16(row_allmax(mine.x)));
   const float weight = fast_exp2(mine.x - (m == -INFINITY ? 0.f : m));
   const float den = add_xor32(add_xor16(row_allsum(weight * mine.y)));
-  float o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
   constexpr int kAhead = 8;                                               // records on their way at once
@@ -661,18 +661,42 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int s
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = den == 0.f ? 0.f : o[e] / den;
-  if (INT4 && (p.rot_v || p.dense_v)) {
-    float* const x = rotated[wave];
-    if (E == 1) x[lane + 64] = 0.f;
+  return true;
+}
+
+// Joins the partial records of a row: one wavefront a row, eight records on their way at once.  5120 rows in two splits 6.7 us, most of it
+// latency.  (NV rows under a learned rotation, whose 64 KiB they read once.)
+template <int D, bool INT4, int NV>
+__global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int splits) {
+  constexpr int E = D / 64;
+  __shared__ __attribute__((aligned(16))) float rotated[4][INT4 ? NV * 128 : 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t rows = p.T_q * p.n_q_heads, row0 = (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave) * NV;
+  if (row0 >= rows) return;
+  const bool turn = INT4 && (p.rot_v || p.dense_v);
+  uint32_t whose = 0;                                                     // rows of a sequence
+  float o[NV][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[E * lane + e] = o[e];
+  for (int v = 0; v < NV; ++v) {
+    if (row0 + v < rows && merged_row<D>(p, splits, row0 + v, lane, o[v])) whose |= 1u << v;
+    if (turn) {
+      float* const x = rotated[wave] + 128 * v;
+      if (E == 1) x[lane + 64] = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[E * lane + e] = whose >> v & 1 ? o[v][e] : 0.f;
+    }
+  }
+  if (!whose) return;
+  if (turn) {
     wave_sync();
-    unrotate_row(p, x, D, lane);
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = x[E * lane + e];
+    unrotate_row<NV == 1 ? 16 : 8, NV>(p, rotated[wave], D, lane);
   }
 #pragma unroll
-  for (int e = 0; e < E; ++e) store_elem(p.out, p.dtype, row * D + E * lane + e, o[e]);
+  for (int v = 0; v < NV; ++v)
+    if (whose >> v & 1)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        store_elem(p.out, p.dtype, (row0 + v) * D + E * lane + e, turn ? rotated[wave][128 * v + E * lane + e] : o[v][e]);
 }
 
 // How a call is handed out: rows of a block, splits of the keys.
@@ -707,19 +731,37 @@ static PromptPlan prompt_plan(bool int4, int D, int G, int Hkv, int64_t T, int B
 }
 static size_t record_bytes(int D, int64_t rows, int splits) { return (size_t)rows * splits * (D + 2) * 4; }
 
+// Rows of a wavefront where a learned rotation has to be read: four from 8192 on (32 sequences of 8 new tokens, 32 heads, level; of 16 145 us in
+// ones, 126 in eights, 114 in fours; of 64 465, 330 and 323; 2048 tokens over 16384 1003, 874 and 865).
+constexpr int kTurnedAtOnce = 4;
+static bool turn_many(const PromptParams& p) { return p.T_q * p.n_q_heads >= 8192; }
+// Blocks of four wavefronts for `rows` rows, NV a wavefront.  (A grid's width is counted in threads, in 32 bits.)
+static dim3 row_grid(int64_t rows, int NV) {
+  const int64_t blocks = (rows + 4 * NV - 1) / (4 * NV);
+  const unsigned wide = (unsigned)(blocks < 1 << 22 ? blocks : 1 << 22);
+  return dim3(wide, (unsigned)((blocks + wide - 1) / wide));
+}
+
 template <int D, int KV>
 static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream_t st) {
-  const int64_t quads = (p.T_q * p.n_q_heads + 3) / 4;                   // (a grid's width is counted in threads, in 32 bits)
-  const unsigned wide = (unsigned)(quads < 1 << 22 ? quads : 1 << 22);
-  const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads), plan.splits), by_row(wide, (unsigned)((quads + wide - 1) / wide)), block(256);
+  const int64_t rows = p.T_q * p.n_q_heads;
+  const dim3 grid((unsigned)(row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads), plan.splits), block(256);
   if constexpr (KV == kKvInt4 && D == kDenseD)
-    if (p.dense_k) prompt_query_kernel<D><<<by_row, block, 0, st>>>(p);
+    if (p.dense_k) {
+      if (turn_many(p)) prompt_query_kernel<D, kTurnedAtOnce><<<row_grid(rows, kTurnedAtOnce), block, 0, st>>>(p);
+      else prompt_query_kernel<D, 1><<<row_grid(rows, 1), block, 0, st>>>(p);
+    }
   if (plan.rows == 128) prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
   if constexpr (KV == kKvInt4)
     if (plan.rows == 32) few_rows_kernel<D><<<grid, block, 0, st>>>(p);
   if constexpr (D == 128 || KV != kKvInt4)
     if (plan.rows == 256) prompt_kernel<D, KV, 8><<<grid, dim3(512), 0, st>>>(p);
-  if (plan.splits > 1 || (KV == kKvInt4 && p.dense_v)) prompt_merge_kernel<D, KV == kKvInt4><<<by_row, block, 0, st>>>(p, plan.splits);
+  if constexpr (KV == kKvInt4 && D == kDenseD)
+    if (p.dense_v && turn_many(p)) {
+      prompt_merge_kernel<D, true, kTurnedAtOnce><<<row_grid(rows, kTurnedAtOnce), block, 0, st>>>(p, plan.splits);
+      return;
+    }
+  if (plan.splits > 1 || (KV == kKvInt4 && p.dense_v)) prompt_merge_kernel<D, KV == kKvInt4, 1><<<row_grid(rows, 1), block, 0, st>>>(p, plan.splits);
 }
 
 int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {

@@ -132,6 +132,18 @@ def test_rotations(saw, options, dtype):
     pc.check(saw.paged_prompt_attn(c.cache, *c.args), want, tol)
 
 
+@pytest.mark.parametrize("options", [dict(h=128, signs=True), dict(h=1), dict(h=64, mask=1), dict(h=16, mask=2)], ids=str)
+def test_many_rows_under_a_learned_rotation(saw, options):
+    """Several rows at once, the last ones and those of no sequence among them."""
+    c = Case(saw, [700, 0, 401], [760, 5, 430], seed=13, dense=True, **options)
+    want, tol = c.attention()
+    q = torch.cat([c.args[0], pc.rand((5, 8, 128), 2, BF).cuda()])
+    out = torch.full_like(q, 7.0)
+    saw.paged_prompt_attn(c.cache, q, *c.args[1:], out=out)
+    pc.check(out[:1101], want, tol)
+    assert bool((out[1101:] == 7).all())
+
+
 def test_a_long_chunk(saw):
     """Blocks of 256 rows."""
     c = Case(saw, [1024], [1100], Hkv=16, G=4, seed=8)
