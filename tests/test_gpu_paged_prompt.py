@@ -404,6 +404,15 @@ def test_weights_of_many_queries_over_few_keys(saw, n, lens, d, G):
         pc.check(got[b, :, :L], want[b, :, :L], tol[b, :, :L], b)
 
 
+def test_weights_of_many_queries_over_one_long_sequence(saw):
+    """A single head: wavefronts that share out the rows go over several steps of keys."""
+    c = Case(saw, [90], [20000], Hkv=1, G=8, seed=9)
+    prev = np.zeros((1, 1, 20000), np.float32)
+    want, tol = _scores(c, prev)
+    got = saw.paged_attn_weights(c.cache, *c.args, prev=torch.from_numpy(prev).cuda(), max_seq_len=20000)
+    pc.check(got, want, tol)
+
+
 # ---- the calls together ----
 def test_pools_beyond_32_bits(saw):
     """Pages at the end of pools of 4.9 GiB of codes each: what they give at the front."""
