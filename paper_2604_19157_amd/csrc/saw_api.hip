@@ -856,7 +856,7 @@ int saw_evict_pages(const saw_cache_t* c, const float* scores, int64_t score_str
   const int64_t cap = (int64_t)max_pages_per_seq * c->page_size;
   if (cap > 0x7fffffffLL || max_seq_len > cap || (max_seq_len <= 0 ? cap : max_seq_len) > kMaxTokens) return SAW_EINVAL;
   const int32_t bound = max_seq_len <= 0 ? (int32_t)cap : max_seq_len;
-  if (budget < 1 || recent < 0 || recent > budget || (int64_t)dst_pages_per_seq * c->page_size < budget) return SAW_EINVAL;
+  if (budget < 1 || budget > kMaxTokens || recent < 0 || recent > budget || (int64_t)dst_pages_per_seq * c->page_size < budget) return SAW_EINVAL;
   if (score_stride < bound || (scores_out && score_out_stride < budget)) return SAW_EINVAL;
   if (!c->k_codes || !c->v_codes || !c->k_meta || !c->v_meta || !scores || !page_table || !seq_lens || !dst_table || !new_lens || !kept)
     return SAW_ENULL;

@@ -308,8 +308,8 @@ __global__ __launch_bounds__(1024, 8) void evict_write_kernel(EvictParams p, Seg
   float* const out = p.scores_out ? p.scores_out + row * p.score_out_stride : nullptr;
   if (h == 0 && seg == 0 && tid == 0) p.new_lens[b] = n;
   // (every block a part of what lies behind the kept tokens, or of a sequence that is kept whole)
-  for (int i = (len <= p.budget ? 0 : n) + seg * 1024 + tid; i < p.budget; i += 1024 * (int)gridDim.x) {
-    kept[i] = i < n ? i : -1;
+  for (int64_t i = (len <= p.budget ? 0 : n) + seg * 1024 + tid; i < p.budget; i += 1024 * (int)gridDim.x) {      // (a step may pass 2^31)
+    kept[i] = i < n ? (int32_t)i : -1;
     if (out) out[i] = i < n ? s[i] : 0.f;
   }
   const int j0 = seg * kSegment, j1 = min(len, j0 + kSegment);

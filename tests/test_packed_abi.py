@@ -116,6 +116,14 @@ def test_evict_refuses_caches(saw, change, code):
     assert saw.lib().saw_evict_pages(*{**EVICT, "cache": ctypes.byref(c)}.values()) == code
 
 
+@pytest.mark.parametrize("budget,code", [((1 << 31) - 1, EINVAL), (0x7fff0001, EINVAL)])
+def test_budgets_beyond_the_counters_are_refused(saw, budget, code):
+    """Positions and kept tokens are counted in 32 bits in steps of a block, as lengths are."""
+    c = _cache(saw)
+    wide = dict(budget=budget, dst_pages=1 << 27, score_out_stride=1 << 32)
+    assert saw.lib().saw_evict_pages(*{**EVICT, "cache": ctypes.byref(c), **wide}.values()) == code
+
+
 def test_workspaces(saw):
     L, c = saw.lib(), _cache(saw)
     r = ctypes.byref(c)
