@@ -49,6 +49,7 @@ class Held {                                                 // references kept 
     v_.push_back(o);
     return o;
   }
+  const std::vector<PyObject*>& all() const { return v_; }
 };
 
 class Unlocked {                                             // the interpreter lock is another thread's meanwhile
@@ -307,6 +308,11 @@ void on_this_gpu(const T&... t) {
   const auto device = c10::hip::getCurrentHIPStream().device_index();
   check(((t.get_device() == device) && ...), "every tensor is on the current device");
 }
+// ... and so are the cache's pools and its learned rotation.
+void pools_on_this_gpu(const Held& held) {
+  for (PyObject* o : held.all())
+    if (o != Py_None) on_this_gpu(tensor(o));
+}
 int32_t in_int32(PyObject* o) {
   const long long v = PyLong_AsLongLong(o);
   if (v == -1 && PyErr_Occurred()) throw Raised();
@@ -370,6 +376,7 @@ PyObject* paged_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float scale = as_float(a[6]);
     check(ws.is_contiguous(), "the workspace is contiguous");
     on_this_gpu(q, cq, pt, lens, out, ws);
+    pools_on_this_gpu(held);
     return run(present(&saw_paged_prompt_attn), &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
                (int32_t)pt.size(1), sl, bound, scale, out.data_ptr(), ws.data_ptr(), (size_t)ws.nbytes(), stream());
   });
@@ -397,6 +404,7 @@ PyObject* attn_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float scale = as_float(a[8]);
     check(ws.is_contiguous(), "the workspace is contiguous");
     on_this_gpu(q, cq, pt, lens, scores, ws);
+    pools_on_this_gpu(held);
     if (prev) on_this_gpu(tensor(a[5]));
     return run(present(&saw_paged_attn_weights), &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
                (int32_t)pt.size(1), sl, bound, scale, prev, to, stride, ws.data_ptr(), (size_t)ws.nbytes(), stream());
@@ -420,6 +428,7 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t *const sl = offsets(lens, B, "seq_lens is a contiguous int32 vector"), *const table = table_of(pt, B), *const to = table_of(dst, B);
     int32_t* const nl = (int32_t*)offsets(now, B, "new_lens is a contiguous int32 vector of seq_lens' length");
     on_this_gpu(scores, pt, lens, dst, now, kept);
+    pools_on_this_gpu(held);
     if (out) on_this_gpu(tensor(a[10]));
     void* ws = nullptr;
     size_t ws_bytes = 0;

@@ -92,6 +92,10 @@ def _on_this_gpu(*tensors):
     assert all(t.get_device() == torch.cuda.current_device() for t in tensors), "every tensor is on the current device"
 
 
+def _pools(cache):
+    return [t for t in (cache.k_codes, cache.v_codes, cache.k_meta, cache.v_meta, cache.dense_rot) if t is not None]
+
+
 def _heads_dense(t):
     return t.dim() == 3 and (t.shape[2] <= 1 or t.stride(2) == 1) and (t.shape[1] <= 1 or t.stride(1) == t.shape[2])
 
@@ -136,7 +140,7 @@ def paged_prompt(cache, q, cu_q, page_table, seq_lens, max_seq_len, sm_scale, ou
     _counts(max_seq_len)
     assert _heads_dense(q) and q.shape[2] == cache.head_dim and _like(out, q)
     assert _vector(cu_q, B + 1) and _vector(seq_lens, B) and _table(page_table, B) and workspace.is_contiguous()
-    _on_this_gpu(q, cu_q, page_table, seq_lens, out, workspace)
+    _on_this_gpu(q, cu_q, page_table, seq_lens, out, workspace, *_pools(cache))
     st = cache.struct()
     return b.lib().saw_paged_prompt_attn(ctypes.byref(st), b._ptr(q), b._DT[q.dtype], q.shape[0], _token_stride(q), q.shape[1], b._ptr(cu_q),
                                          B, b._ptr(page_table), page_table.shape[1], b._ptr(seq_lens), max_seq_len, float(sm_scale),
@@ -149,7 +153,7 @@ def attn_weights(cache, q, cu_q, page_table, seq_lens, prev, scores, max_seq_len
     assert _heads_dense(q) and q.shape[2] == cache.head_dim and _record(scores, B, cache.n_kv_heads)
     assert prev is None or (_record(prev, B, cache.n_kv_heads) and prev.shape == scores.shape)
     assert _vector(cu_q, B + 1) and _vector(seq_lens, B) and _table(page_table, B) and workspace.is_contiguous()
-    _on_this_gpu(q, cu_q, page_table, seq_lens, scores, workspace, *([] if prev is None else [prev]))
+    _on_this_gpu(q, cu_q, page_table, seq_lens, scores, workspace, *([] if prev is None else [prev]), *_pools(cache))
     st = cache.struct()
     return b.lib().saw_paged_attn_weights(ctypes.byref(st), b._ptr(q), b._DT[q.dtype], q.shape[0], _token_stride(q), q.shape[1],
                                           b._ptr(cu_q), B, b._ptr(page_table), page_table.shape[1], b._ptr(seq_lens), max_seq_len,
@@ -163,7 +167,7 @@ def evict(cache, scores, page_table, seq_lens, dst_table, budget, recent, max_se
     assert _record(scores, B, cache.n_kv_heads) and (scores_out is None or _record(scores_out, B, cache.n_kv_heads))
     assert kept.dtype == torch.int32 and kept.is_contiguous() and kept.shape == (B, cache.n_kv_heads, budget)
     assert _vector(seq_lens, B) and _vector(new_lens, B) and _table(page_table, B) and _table(dst_table, B)
-    _on_this_gpu(scores, page_table, seq_lens, dst_table, new_lens, kept, *(x for x in (scores_out, workspace) if x is not None))
+    _on_this_gpu(scores, page_table, seq_lens, dst_table, new_lens, kept, *(x for x in (scores_out, workspace) if x is not None), *_pools(cache))
     assert workspace is None or workspace.is_contiguous()
     st = cache.struct()
     return b.lib().saw_evict_pages(ctypes.byref(st), b._ptr(scores), scores.shape[2], b._ptr(page_table), page_table.shape[1],

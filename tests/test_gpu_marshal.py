@@ -33,3 +33,23 @@ def test_native_and_ctypes_make_the_same_calls(monkeypatch, T):
         got.append(out + [t for c in caches for t in (c.k_codes, c.v_codes, c.k_meta, c.v_meta)])
     for i, (a, b) in enumerate(zip(*got)):
         assert a.dtype == b.dtype and torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("pool", ["k_codes", "v_codes", "k_meta", "v_meta", "dense_rot"])
+def test_pools_of_another_device_are_refused(pool, native):
+    """The calls of packed queries and eviction take no cache of which a part lies elsewhere than the other tensors."""
+    from paper_2604_19157_amd import binding as saw
+    from paper_2604_19157_amd import marshal_ctypes
+    saw.lib()
+    m = saw._marshal() if native else marshal_ctypes
+    cache = saw.Cache(8, 2, 128, 128, dense=torch.eye(128))
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    q, ws = torch.zeros((6, 4, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    cu, lens, pt, rec = i32(3), i32(2), i32(2, 4), torch.zeros((2, 2, 64), device="cuda")
+    setattr(cache, pool, getattr(cache, pool).cpu())
+    for call, args in ((m.paged_prompt, (cache, q, cu, pt, lens, 0, 0.0, torch.zeros_like(q), ws)),
+                       (m.attn_weights, (cache, q, cu, pt, lens, None, rec, 0, 0.0, ws)),
+                       (m.evict, (cache, rec, pt, lens, i32(2, 2), 20, 0, 0, i32(2), i32(2, 2, 20), None, None))):
+        with pytest.raises(AssertionError, match="GPU"):
+            call(*args)
