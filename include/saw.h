@@ -450,7 +450,7 @@ int saw_paged_attn_weights(const saw_cache_t* cache, const void* q, int32_t dtyp
  *               that other sequences share stay valid.  A token whose source or destination page id is outside [0, num_pages) is not
  *               copied; slots from min(seq_lens[b], budget) on are left as they were.
  *   budget, recent   1 <= budget <= 2^31 - 2^16, 0 <= recent <= budget
- *   new_lens    device, [B] int32: min(seq_lens[b], budget)
+ *   new_lens    device, [B] int32: min(seq_lens[b], budget).  May be seq_lens itself (lengths are replaced in place).
  *   kept        device, [B][n_kv_heads][budget] int32: the old positions of the kept tokens, ascending; -1 from new_lens[b] on
  *   scores_out  device, [B][n_kv_heads][score_out_stride >= budget] float32 or NULL: the kept tokens' scores, 0 from new_lens[b] to
  *               budget; must not overlap `scores`.

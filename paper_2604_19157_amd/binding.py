@@ -389,7 +389,8 @@ def evict_workspace_bytes(cache: Cache, n_seqs, max_seq_len) -> int:
 def evict_pages(cache: Cache, scores, page_table, seq_lens, dst_table, budget, recent=0, max_seq_len=0, new_lens=None, kept=None,
                 scores_out=None, workspace=None):
     """saw_evict_pages: keeps ``budget`` tokens of every (sequence, kv head) by ``scores [B][Hkv][n]`` fp32, the last ``recent`` among them,
-    and copies them to the pages of ``dst_table``; returns ``(new_lens [B], kept [B][Hkv][budget], scores_out [B][Hkv][>= budget])``."""
+    and copies them to the pages of ``dst_table``; returns ``(new_lens [B], kept [B][Hkv][budget], scores_out [B][Hkv][>= budget])``.  new_lens may
+    be seq_lens itself."""
     B, dev = seq_lens.numel(), scores.device
     if new_lens is None:
         new_lens = torch.empty(B, dtype=torch.int32, device=dev)

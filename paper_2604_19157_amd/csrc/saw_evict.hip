@@ -146,7 +146,6 @@ __global__ __launch_bounds__(1024, 8) void evict_select_kernel(EvictParams p) {
   int32_t* const kept = p.kept + row * p.budget;
   float* const out = p.scores_out ? p.scores_out + row * p.score_out_stride : nullptr;
   const int n = min(len, p.budget), old = max(len - p.recent, 0);
-  if (h == 0 && tid == 0) p.new_lens[b] = n;
   for (int i = n + tid; i < p.budget; i += 1024) {
     kept[i] = -1;
     if (out) out[i] = 0.f;
@@ -306,7 +305,6 @@ __global__ __launch_bounds__(1024, 8) void evict_write_kernel(EvictParams p, Seg
   const float* const s = p.scores + row * p.score_stride;
   int32_t* const kept = p.kept + row * p.budget;
   float* const out = p.scores_out ? p.scores_out + row * p.score_out_stride : nullptr;
-  if (h == 0 && seg == 0 && tid == 0) p.new_lens[b] = n;
   // (every block a part of what lies behind the kept tokens, or of a sequence that is kept whole)
   for (int64_t i = (len <= p.budget ? 0 : n) + seg * 1024 + tid; i < p.budget; i += 1024 * (int)gridDim.x) {      // (a step may pass 2^31)
     kept[i] = i < n ? (int32_t)i : -1;
@@ -378,6 +376,8 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
   const int t0 = blockIdx.x * (kEach * kStep) + threadIdx.x / LPV, part = threadIdx.x % LPV;
   const int b = blockIdx.z, h = blockIdx.y;
   const int n = min(min(max(p.seq_lens[b], 0), p.bound), p.budget);
+  // (new_lens may be seq_lens itself: the kernels before this one need the whole length; n is the same before and after the write)
+  if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) p.new_lens[b] = n;
   if (t0 >= n) return;
   const int32_t* const kept = p.kept + ((int64_t)b * p.n_kv_heads + h) * p.budget;
   int j[kEach], from[kEach], to[kEach];

@@ -118,6 +118,14 @@ def test_long_rows(saw, lens, budget, recent, kind):
     c.check(c.run(saw))
 
 
+@pytest.mark.parametrize("lens,budget", [([3000, 700, 90], 600), ([3000] * 300, 100), ([40000, 17000], 5000)], ids=["few", "many", "long"])
+def test_lengths_replaced_in_place(saw, lens, budget):
+    """new_lens is seq_lens: every head selects from the old length, whenever its block starts."""
+    c = Case(saw, lens, budget, 10, Hkv=4)
+    c.check(c.run(saw, new_lens=c.args[2]))
+    assert c.args[2].tolist() == [min(x, budget) for x in lens]
+
+
 def test_rows_further_apart_than_needed(saw):
     c = Case(saw, [300, 200], 100, 10, width=517)
     out = torch.full((2, 2, 333), 8.0, device="cuda")
