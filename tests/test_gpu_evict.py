@@ -126,6 +126,28 @@ def test_lengths_replaced_in_place(saw, lens, budget):
     assert c.args[2].tolist() == [min(x, budget) for x in lens]
 
 
+@pytest.mark.parametrize("lens,Hkv", [([12000, 16384, 8193, 8192], 2), ([17000] + [30] * 64, 2)], ids=["middle", "many rows"])
+@pytest.mark.parametrize("kind", ["random", "few", "constant", "nan", "all nan", "low digits"])
+def test_many_scores_of_like_size_in_one_block(saw, lens, Hkv, kind):
+    """Rows that a single block selects from, of which more scores share the first digit than its list holds: they are all read again."""
+    rng = np.random.default_rng(9)
+    s = rng.random((len(lens), Hkv, max(lens))).astype(np.float32)
+    if kind == "few":
+        s = rng.integers(1, 3, s.shape).astype(np.float32) / 8 + 1
+    elif kind == "constant":
+        s[:] = 0.25
+    elif kind == "nan":
+        s[rng.random(s.shape) < 0.9] = np.nan
+    elif kind == "all nan":
+        s[:] = np.nan
+    elif kind == "low digits":                        # one in the first 11 bits of the key, many in the next and the last
+        s = (1 + s / 16).astype(np.float32)
+    for budget, recent in ((5000, 700), (1, 0), (8000, 8000)):
+        c = Case(saw, lens, budget, recent, Hkv=Hkv, scores=s)
+        assert saw.evict_workspace_bytes(c.cache, len(lens), max(lens)) == 0
+        c.check(c.run(saw))
+
+
 def test_rows_further_apart_than_needed(saw):
     c = Case(saw, [300, 200], 100, 10, width=517)
     out = torch.full((2, 2, 333), 8.0, device="cuda")
