@@ -384,7 +384,8 @@ int saw_flatten_dequant(const saw_cache_t* cache, const int32_t* page_table,
  *   workspace   device scratch of at least saw_prompt_workspace_bytes(...) bytes, 16-byte aligned; contents are overwritten;
  *               concurrent calls need separate workspaces.
  * Logits, their maxima and sums and the output sums are fp32; the weights enter the product with V in dtype's precision
- * (half a step: 2^-8 for bf16, 2^-11 for fp16, as the output's own).  A masked key counts for nothing whatever it
+ * (half a step: 2^-8 for bf16, 2^-11 for fp16, as the output's own; fp16 weights of less than 2^-21 of the row's largest are off
+ * by 2^-32 of that one at most).  A masked key counts for nothing whatever it
  * and its value hold (NaN and infinities too).  A row whose logits are all -infinity gets zeros.
  * T_q == 0 is a no-op.  head_dim 64 or 128; n_q_heads / n_kv_heads in {1, 2, 4, 8}; B <= 65535; T_k and T_q n_q_heads up to 2^31 - 2^16
  * (here and in the calls below, as bounds of lengths).
@@ -406,8 +407,8 @@ int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, 
  *   out         device, dense [T][n_q_heads][head_dim] of dtype, 16-byte aligned; rows of no sequence are left as they were.
  *   workspace   at least saw_paged_prompt_workspace_bytes(...) bytes, 16-byte aligned, one per call in flight.
  * Rotated queries and dequantised keys enter their product as fp16 times powers of two (a query's of its row, keys' of the
- * sequence), weights and dequantised values theirs as fp16 too: half a step each, 2^-11, and 2^-19 of the largest value that a row
- * meets, whatever the size of those that it does not see; everything between and all sums are fp32.  Page ids of visible tokens outside
+ * sequence), weights and dequantised values theirs as fp16 too: half a step each, 2^-11, at least 2^-32 of the row's largest weight and
+ * 2^-19 of the largest value that a row meets, whatever the size of those that it does not see; everything between and all sums are fp32.  Page ids of visible tokens outside
  * [0, num_pages) are read as page 0.  Alignment of the pools as for the decode calls.  T == 0 is a no-op.
  */
 size_t saw_paged_prompt_workspace_bytes(const saw_cache_t* cache, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len);

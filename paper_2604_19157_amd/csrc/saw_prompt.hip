@@ -36,7 +36,7 @@ struct RowSource {
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // A rotated query becomes fp16 times 2^-e with the row's largest channel in [2^14, 2^15): relative rounding 2^-11 whatever the row's
-// size, down to 2^-39 of the largest.
+// size down to 2^-28 of the largest channel, smaller ones are off by 2^-39 of it.
 __device__ __forceinline__ int query_exponent(float top) { return min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14; }
 
 // Queries under a learned rotation, whose 64 KiB a block of rows would read again: a wavefront for NV rows, which read them once.
@@ -204,14 +204,14 @@ __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token,
   return p.scale;
 }
 
-// This split's (maximum, sum) of every row, behind the records of all splits.
+// This split's (reference, sum) of every row, behind the records of all splits: log2 of what sum and record are relative to.
 template <int D>
 __device__ __forceinline__ float2* partial_sums(const PromptParams& p) {
   const int64_t rows = p.T_q * p.n_q_heads;
   return (float2*)(p.ws + (int64_t)gridDim.y * rows * D) + (int64_t)blockIdx.y * rows;
 }
 
-// The end of a wavefront's 32 rows: outputs, or partial records [split][row][D] and [split][row] (maximum, sum) where the keys are split
+// The end of a wavefront's 32 rows: outputs, or partial records [split][row][D] and [split][row] (reference, sum) where the keys are split
 // or a learned rotation has to be undone.  scale: of the rows' logits; unit: of the output sums.
 template <int D, int KV, int HALF_BIT, bool CODES = false>
 __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile& rt, int w0, int last, int row, int h, int64_t token, int head,
@@ -297,7 +297,7 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
   }
   if (split) {
     if (row > last) return;
-    if (lane < 32) ml[at] = make_float2(st.m, sum);
+    if (lane < 32) ml[at] = make_float2(st.m - std::conditional<KV == kKvBf16, MathBf16, MathF16>::type::kRaise, sum);
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll

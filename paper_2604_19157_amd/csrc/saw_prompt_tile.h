@@ -57,13 +57,18 @@ __device__ __forceinline__ bool find_row_tile(const PromptParams& p, int64_t til
 inline int64_t row_tiles(int64_t T, int G, int R, int B) { return T * G / R + B; }
 
 // Operand types of the two products: bits of K / V, the matrix instruction, and the rounding of a pair of weights (nearest even).
+//   kRaise: weights are relative to 2^(m - kRaise), m the row's maximum so far, up to 2^8 behind (tile_weights).  fp16 ones so go up to 2^15 and are
+// off by half a step, 2^-11, down to 2^-21 of the largest weight; below by 2^-32 of the largest at most (relative to the maximum itself, by
+// 2^-25: a strong token and 131072 others of 2^-25 of its weight each would lose their 0.4 % of the row).  bf16 has fp32's exponents.
 struct MathBf16 {
+  static constexpr float kRaise = 0.f;
   static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2)); }
 };
 struct MathF16 {
+  static constexpr float kRaise = 7.f;
   static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
@@ -134,7 +139,7 @@ __device__ __forceinline__ int v_place(int row, int chunk) {
 template <int D>
 struct RowState {
   f32x16 o[D / 32];       // O^T: channel 32 t + 8 (r / 4) + 4 (lane / 32) + r % 4 of query lane % 32, relative to 2^ref
-  float m, ref, sum;      // maximum that the state refers to (log2 units, -inf: none yet; ref: 0 then); this half's sum of weights
+  float m, ref, sum;      // maximum that the state refers to (log2 units, -inf: none yet; ref: m - kRaise, 0 then); this half's sum of weights
 };
 
 // S^T of one tile against the queries in qf.  The two halves of the keys alternate, so that a product does not wait for the sum of the one
@@ -187,10 +192,9 @@ __device__ __forceinline__ void tile_weights(f32x16 (&s)[2], float scale, RowSta
   top = max_xor32(top) * scale;
   if (__any(top > st.m + 8.f)) {
     const float m = fmaxf(st.m, top);
-    const float ref = m == -INFINITY ? 0.f : m;
-    const float alpha = fast_exp2(st.m - ref);
+    const float alpha = fast_exp2(st.m - (m == -INFINITY ? 0.f : m));
     st.m = m;
-    st.ref = ref;
+    st.ref = m == -INFINITY ? 0.f : m - M2::kRaise;
     st.sum *= alpha;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)

@@ -283,6 +283,38 @@ def test_captured_and_replayed(saw):
         assert torch.equal(out, got[0]) and torch.equal(scores, got[1])
 
 
+def _same_pages(saw, B, n, L, d, dtype, sink, tail):
+    """B sequences of the same L tokens: the first has logit `sink` and value 0, the others logit 0 and the value `tail` in every channel."""
+    Hkv, pages = 8, (L + 15) // 16
+    cache = saw.Cache(pages, Hkv, d, 1)
+    cache.k_codes.fill_(0x88)
+    cache.v_codes.fill_(0xff)
+    cache.k_codes[0, :, 0, 0] = 0x8f                 # channel 0 of the first token: 7 scales
+    cache.v_codes[0, :, 0] = 0x88
+    for pool, scale in ((cache.k_meta, sink / 7), (cache.v_meta, tail / 7)):
+        pool[..., 0], pool[..., 1] = scale, 8
+    q = torch.zeros((B * n, Hkv * 4, d), dtype=dtype, device="cuda")
+    q[..., 0] = 1
+    pt = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(B, 1)
+    cu = torch.arange(0, B * n + 1, n, dtype=torch.int32, device="cuda")
+    return cache, q, cu, pt, torch.full((B,), L, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("B,n", [(70, 1), (70, 20), (1, 3), (1, 20), (16, 520)])
+def test_many_small_weights(saw, B, n, d, dtype):
+    """One token of nearly all the weight and no value, 20000 of 2^-25.2 of its weight each: the output is what they give.  Off by the roundings of
+    output, weight and value and by 2^-32 of the largest weight for each token (logits are exact: 17.5, 0)."""
+    L, sink, tail = 20000, 17.5, 3.5
+    got = saw.paged_prompt_attn(*_same_pages(saw, B, n, L, d, dtype, sink, tail), sm_scale=1.0).double().cpu().numpy()
+    seen = np.tile(np.arange(L - n, L), B).astype(np.float64)[:, None, None]           # tokens of the tail that a query sees
+    small = np.exp(-sink)
+    want = tail * seen * small / (1 + seen * small)
+    tol = want * (pc.U[dtype] + 2.0 ** -10 + 2.0 ** -18 + L * 2.0 ** -22) * 1.01 + tail * L * 2.0 ** -32
+    assert (np.abs(got - want) <= tol).all(), np.abs(got / want - 1).max()
+
+
 # ---- accumulated weights ----
 def _scores(c, prev):
     """(scores, bound): a weight is off by at most w (exp(2 e) - 1 + 2^-20 + n 2^-22); then sums of as many terms as there are rows, in fp32."""

@@ -214,3 +214,24 @@ def test_many_sequences(saw):
     rng = np.random.default_rng(3)
     n = rng.integers(0, 9, 300).tolist()
     _run(saw, n, [x + int(e) for x, e in zip(n, rng.integers(0, 40, 300))], 1, 4, 64, BF)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("B,n,L,d", [(300, 1, 4000, 64), (2, 1, 4000, 128), (300, 40, 2000, 128), (1, 6000, 6000, 64)])
+def test_many_small_weights(saw, B, n, L, d, dtype):
+    """One key of nearly all the weight and no value, thousands of 2^-25.2 of its weight each: the output is what they give.  Off by the roundings of
+    output and weight and, fp16, by 2^-32 of the largest weight for each key (logits are exact: 17.5, 0)."""
+    sink, tail = 17.5, 4.0
+    q, k = torch.zeros((B * n, 8, d), dtype=dtype, device="cuda"), torch.zeros((B * L, 1, d), dtype=dtype, device="cuda")
+    v = torch.full_like(k, tail)
+    q[..., 0] = 1
+    k[::L, :, 0] = sink
+    v[::L] = 0
+    cu_q, cu_k = (torch.arange(0, B * x + 1, x, dtype=torch.int32, device="cuda") for x in (n, L))
+    got = saw.prompt_attn(q, k, v, cu_q, cu_k, sm_scale=1.0).double().cpu().numpy()
+    seen = np.tile(np.arange(L - n, L), B).astype(np.float64)[:, None, None]
+    small = np.exp(-sink)
+    want = tail * seen * small / (1 + seen * small)
+    # (fp16 outputs below 2^-14: half of fp16's smallest step)
+    tol = want * (2 * pc.U[dtype] + 2.0 ** -18 + L * 2.0 ** -22) * 1.01 + tail * L * 2.0 ** -32 + (2.0 ** -25 if dtype == FP else 0)
+    assert (np.abs(got - want) <= tol).all(), np.nanmax(np.abs(got - want) / tol)
