@@ -17,10 +17,11 @@ __device__ __forceinline__ float f16_to_f32(uint32_t u16) {
   c.u = (uint16_t)u16;
   return (float)c.h;
 }
+// (conversion instructions, which keep every NaN a NaN: adding half a step to the bits turns one with all of them set into zero)
 __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
-  uint32_t u = __float_as_uint(f);
-  u += 0x7fffu + ((u >> 16) & 1u);
-  return (uint16_t)(u >> 16);
+  union { uint16_t u; __bf16 h; } c;
+  c.h = (__bf16)f;
+  return c.u;
 }
 __device__ __forceinline__ uint16_t f32_to_f16(float f) {
   union { uint16_t u; _Float16 h; } c;

@@ -315,6 +315,18 @@ def test_many_small_weights(saw, B, n, d, dtype):
     assert (np.abs(got - want) <= tol).all(), np.abs(got / want - 1).max()
 
 
+@pytest.mark.parametrize("n,lens", [([3], [40]), ([1], [3000]), ([60], [100]), ([1], [200])], ids=str)
+@pytest.mark.parametrize("options", [dict(h=1), dict(h=128), dict(h=1, dense=True)], ids=str)
+def test_every_kind_of_nan_shows(saw, n, lens, options):
+    """Also the one with all bits set, which memory that was never written may hold."""
+    for pool in ("k_meta", "v_meta"):
+        c = Case(saw, n, lens, **options)
+        getattr(c.cache, pool)[c.pt[0, 0], :, 3].view(torch.int32).fill_(-1)
+        assert bool(torch.isnan(saw.paged_prompt_attn(c.cache, *c.args)).all())
+        if n == [1]:
+            assert bool(torch.isnan(saw.paged_decode_attn(c.cache, c.args[0], c.args[2].clamp(max=c.cache.num_pages - 1), c.args[3], out_dtype=BF)).all())
+
+
 # ---- accumulated weights ----
 def _scores(c, prev):
     """(scores, bound): a weight is off by at most w (exp(2 e) - 1 + 2^-20 + n 2^-22); then sums of as many terms as there are rows, in fp32."""
