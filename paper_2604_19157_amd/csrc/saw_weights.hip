@@ -334,9 +334,10 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
 #pragma unroll
           for (int r = 0; r < 4; ++r)
             if (mi[r].y != mi[r].y) {
+              const int end = min(len, first_hidden + ((row0 + 4 * (lane >> 4) + r) >> shift));
 #pragma unroll
               for (int t = 0; t < 4; ++t)
-                if (x[t][r] != -INFINITY) total[t] = mi[r].y;
+                if (key0 + 16 * t + (lane & 15) < end) total[t] = mi[r].y;
               mi[r].y = 0.f;
             }
 #pragma unroll
@@ -573,13 +574,16 @@ __global__ __launch_bounds__(64 * kStepWaves, 4) void weight_step_kernel(PromptP
       }
     } else {
       first();
+      int end[4];                                                          // positions that the rows see, also those whose logit is -infinity
+#pragma unroll
+      for (int r = 0; r < 4; ++r) end[r] = min(len, first_hidden + ((row0 + 4 * (lane >> 4) + r) >> shift));
       steps([&](int key0, const f32x4 (&x)[4]) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           float w = 0.f;
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (4 * (lane >> 4) + r < here && x[t][r] != -INFINITY)
+            if (4 * (lane >> 4) + r < here && key0 + 16 * t + (lane & 15) < end[r])
               w = fmaf(fast_exp2(x[t][r] - info[4 * (lane >> 4) + r].m), info[4 * (lane >> 4) + r].inv, w);
           w = add_xor32(add_xor16(w));
           const int key = key0 + 16 * t + lane;

@@ -426,6 +426,22 @@ def test_weights_of_a_query_that_is_no_number(saw, bad, lens):
     pc.check(got[1:], want[1:], tol[1:])
 
 
+@pytest.mark.parametrize("lens", [[60, 30], [5000, 30], [60] + [30] * 40, [5000] + [30] * 40], ids=len)
+def test_weights_of_a_row_that_is_no_number_beside_an_infinite_key(saw, lens):
+    """A token whose logit is -infinity is a token that the row sees: its weight is no number either."""
+    n = [2] + [0] * (len(lens) - 1)
+    c = Case(saw, n, lens, Hkv=8, h=1, seed=5)
+    c.args[0].fill_(1)
+    at = [lens[0] - 3, 1]                             # in the last tile, and in front
+    for j in at:
+        c.cache.k_codes[c.pt[0, j // 16], :, j % 16] = 0
+        c.cache.k_meta[c.pt[0, j // 16], :, j % 16] = torch.tensor([float("inf"), 8.0], device="cuda")
+    j = lens[0] - 4
+    c.cache.k_meta[c.pt[0, j // 16], :, j % 16] = float("nan")
+    got = saw.paged_attn_weights(c.cache, *c.args, max_seq_len=max(lens))
+    assert bool(torch.isnan(got[0, :, :lens[0]]).all())
+
+
 @pytest.mark.parametrize("n,lens,G", [([1, 1], [5000, 9000], 4), ([1], [20000], 8), ([2, 33], [7000, 3001], 2), ([1] * 40, list(range(100, 1300, 30)), 4)], ids=str)
 def test_long_contexts_split(saw, n, lens, G):
     c = Case(saw, n, lens, G=G, seed=2)
