@@ -327,8 +327,9 @@ def flatten_dequant(cache: Cache, page_table, seq, pos_begin, pos_end, unrotate=
 
 
 def prompt_workspace_bytes(q, k, n_seqs, max_k_len=0) -> int:
-    """Scratch of prompt_attn for q ``[T_q][Hq][d]`` and k ``[T_k][Hkv][d]`` in ``n_seqs`` sequences."""
-    return int(lib().saw_prompt_workspace_bytes(q.shape[2], q.shape[1], k.shape[1], q.shape[0], n_seqs, max_k_len or k.shape[0]))
+    """Scratch of prompt_attn for q ``[T_q][Hq][d]`` and k ``[T_k][Hkv][d]`` in ``n_seqs`` sequences, with prompt_attn's bound (<= 0: T_k)."""
+    bound = min(max_k_len, k.shape[0]) if max_k_len > 0 else k.shape[0]
+    return int(lib().saw_prompt_workspace_bytes(q.shape[2], q.shape[1], k.shape[1], q.shape[0], n_seqs, bound))
 
 
 def prompt_attn(q, k, v, cu_q, cu_k=None, max_k_len=0, causal=True, sm_scale=0.0, out=None, workspace=None):

@@ -138,6 +138,16 @@ def test_workspaces(saw):
     assert L.saw_evict_workspace_bytes(r, 1, 131072) > 0 and L.saw_evict_workspace_bytes(r, 4, 1000) == 0 and L.saw_evict_workspace_bytes(None, 1, 1000) == 0
 
 
+def test_the_binding_sizes_scratch_for_every_bound_that_the_call_takes(saw):
+    """<= 0 stands for all keys; a bound above their number, whatever its size, for their number."""
+    q, k = torch.zeros(3, 8, 128, dtype=torch.bfloat16), torch.zeros(5000, 2, 128, dtype=torch.bfloat16)
+    need = saw.prompt_workspace_bytes(q, k, 1, 5000)
+    assert need > 16
+    for bound in (0, -1, -(1 << 40), 5001, 1 << 31, 1 << 40):
+        assert saw.prompt_workspace_bytes(q, k, 1, bound) == need
+    assert saw.prompt_workspace_bytes(q, k, 1, 400) < need
+
+
 def test_workspaces_without_queries(saw):
     L, r = saw.lib(), ctypes.byref(_cache(saw))
     for B in (1, 7, 65535):
