@@ -382,7 +382,7 @@ int saw_flatten_dequant(const saw_cache_t* cache, const int32_t* page_table,
  *   out         device, dense [T_q][n_q_heads][head_dim] of dtype, 16-byte aligned; must not overlap the inputs.  Rows of no
  *               sequence (from cu_q[B] on, or in front of cu_q[0]) are left as they were.
  *   workspace   device scratch of at least saw_prompt_workspace_bytes(...) bytes, 16-byte aligned; contents are overwritten;
- *               concurrent calls need separate workspaces.
+ *               concurrent calls need separate workspaces.  (Calls of few rows split their keys and need more than large ones.)
  * Logits, their maxima and sums and the output sums are fp32; the weights enter the product with V in dtype's precision
  * (half a step: 2^-8 for bf16, 2^-11 for fp16, as the output's own; fp16 weights of less than 2^-21 of the row's largest are off
  * by 2^-32 of that one at most).  A masked key counts for nothing whatever it
@@ -405,7 +405,8 @@ int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, 
  *   seq_lens    device, [B] int32: tokens in the cache, the new ones included.  Query i sees positions 0 .. seq_lens[b] - n_b + i;
  *               one that sees nothing gets zeros.  Lengths are clamped to max_seq_len (<= 0: max_pages_per_seq * page_size).
  *   out         device, dense [T][n_q_heads][head_dim] of dtype, 16-byte aligned; rows of no sequence are left as they were.
- *   workspace   at least saw_paged_prompt_workspace_bytes(...) bytes, 16-byte aligned, one per call in flight.
+ *   workspace   at least saw_paged_prompt_workspace_bytes(...) bytes, 16-byte aligned, one per call in flight: partial
+ *               records where keys are split, which calls of few rows need more of than large ones, and the rows of a learned rotation.
  * Rotated queries and dequantised keys enter their product as fp16 times powers of two (a query's of its row, keys' of the
  * sequence), weights and dequantised values theirs as fp16 too: half a step each, 2^-11, at least 2^-32 of the row's largest weight and
  * 2^-19 of the largest value that a row meets, whatever the size of those that it does not see; everything between and all sums are fp32.  Page ids of visible tokens outside

@@ -294,7 +294,7 @@ int launch_weights(const PromptParams&, int D, hipStream_t);
 int launch_evict(const EvictParams&, int B, int D, void* ws, hipStream_t);
 size_t evict_bytes(int64_t rows, int64_t bound);
 size_t prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len);
-size_t paged_prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len);
+size_t paged_prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len, bool dense_k, bool dense_v);
 size_t weights_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len);
 
 static bool group_ok(int n_q_heads, int n_kv_heads) {
@@ -803,7 +803,8 @@ int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, 
 
 size_t saw_paged_prompt_workspace_bytes(const saw_cache_t* c, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len) {
   if (!c || !shape_ok(c) || !group_ok(n_q_heads, c->n_kv_heads) || !tokens_ok(T, B) || !rows_ok(T, n_q_heads) || max_seq_len < 1 || max_seq_len > kMaxTokens) return 0;
-  return paged_prompt_bytes(c->head_dim, n_q_heads, c->n_kv_heads, T, B, max_seq_len);
+  return paged_prompt_bytes(c->head_dim, n_q_heads, c->n_kv_heads, T, B, max_seq_len, c->dense_rot && (c->rotate_mask & SAW_ROT_K),
+                            c->dense_rot && (c->rotate_mask & SAW_ROT_V));
 }
 
 int saw_paged_prompt_attn(const saw_cache_t* c, const void* q, int32_t dtype, int64_t T, int64_t q_stride, int32_t n_q_heads,
@@ -817,7 +818,7 @@ int saw_paged_prompt_attn(const saw_cache_t* c, const void* q, int32_t dtype, in
   if (T == 0) return SAW_OK;
   if (!out) return SAW_ENULL;
   if (!aligned16(out)) return SAW_EINVAL;
-  if (workspace_bytes < paged_prompt_bytes(c->head_dim, n_q_heads, c->n_kv_heads, T, B, p.bound)) return SAW_EWORKSPACE;
+  if (workspace_bytes < paged_prompt_bytes(c->head_dim, n_q_heads, c->n_kv_heads, T, B, p.bound, p.dense_k, p.dense_v)) return SAW_EWORKSPACE;
   p.out = out;
   return launch_prompt(p, c->head_dim, true, (hipStream_t)stream);
 }

@@ -730,6 +730,8 @@ static PromptPlan prompt_plan(bool int4, int D, int G, int Hkv, int64_t T, int B
   return r;
 }
 static size_t record_bytes(int D, int64_t rows, int splits) { return (size_t)rows * splits * (D + 2) * 4; }
+// Rows leave records where their keys are split, or for a learned rotation to be undone by the merge.
+static bool keeps_records(const PromptPlan& plan, bool dense_v) { return plan.splits > 1 || dense_v; }
 
 // Rows of a wavefront where a learned rotation has to be read: four from 8192 on (32 sequences of 8 new tokens, 32 heads, level; of 16 145 us in
 // ones, 126 in eights, 114 in fours; of 64 465, 330 and 323; 2048 tokens over 16384 1003, 874 and 865).
@@ -761,7 +763,7 @@ static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream
       prompt_merge_kernel<D, true, kTurnedAtOnce><<<row_grid(rows, kTurnedAtOnce), block, 0, st>>>(p, plan.splits);
       return;
     }
-  if (plan.splits > 1 || (KV == kKvInt4 && p.dense_v)) prompt_merge_kernel<D, KV == kKvInt4, 1><<<row_grid(rows, 1), block, 0, st>>>(p, plan.splits);
+  if (keeps_records(plan, KV == kKvInt4 && p.dense_v)) prompt_merge_kernel<D, KV == kKvInt4, 1><<<row_grid(rows, 1), block, 0, st>>>(p, plan.splits);
 }
 
 int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
@@ -769,8 +771,8 @@ int launch_prompt(PromptParams p, int D, bool int4, hipStream_t st) {
   const PromptPlan plan = prompt_plan(int4, D, p.group, p.n_kv_heads, p.T_q, p.B, p.bound);
   if (row_tiles(p.T_q, p.group, plan.rows, p.B) * p.n_kv_heads * (plan.rows == 256 ? 512 : 256) > 0xffffffffLL) return SAW_EINVAL;
   if (int4) {
-    // (behind the records: rows of D + 2 floats)
-    p.query_scale = p.ws + ((D + 2) * rows * plan.splits + 3) / 4 * 4;
+    // (behind the records, if there are any: rows of D + 2 floats)
+    p.query_scale = p.ws + (keeps_records(plan, p.dense_v) ? ((D + 2) * rows * plan.splits + 3) / 4 * 4 : 0);
     p.query = (uint16_t*)(p.query_scale + (rows + 3) / 4 * 4);
     if (D == 128) launch_rows<128, kKvInt4>(p, plan, st);
     else launch_rows<64, kKvInt4>(p, plan, st);
@@ -788,10 +790,10 @@ size_t prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len)
   const PromptPlan plan = prompt_plan(false, D, Hq / Hkv, Hkv, T, B, max_k_len);
   return 16 + (plan.splits > 1 ? record_bytes(D, T * Hq, plan.splits) : 0);
 }
-size_t paged_prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len) {
+size_t paged_prompt_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t max_k_len, bool dense_k, bool dense_v) {
   const PromptPlan plan = prompt_plan(true, D, Hq / Hkv, Hkv, T, B, max_k_len);
   const int64_t rows = T * Hq;
-  return 32 + record_bytes(D, rows, plan.splits) + (size_t)(rows + 3) / 4 * 16 + (size_t)rows * D * 2;
+  return 32 + (keeps_records(plan, dense_v) ? record_bytes(D, rows, plan.splits) : 0) + (dense_k ? (size_t)(rows + 3) / 4 * 16 + (size_t)rows * D * 2 : 0);
 }
 
 }  // namespace saw

@@ -327,6 +327,23 @@ def test_every_kind_of_nan_shows(saw, n, lens, options):
             assert bool(torch.isnan(saw.paged_decode_attn(c.cache, c.args[0], c.args[2].clamp(max=c.cache.num_pages - 1), c.args[3], out_dtype=BF)).all())
 
 
+@pytest.mark.parametrize("n,lens", [([7, 1], [60, 3000]), ([150], [400]), ([1300, 3], [1300, 900])], ids=str)
+@pytest.mark.parametrize("options", [dict(h=128), dict(h=128, dense=True), dict(h=64, dense=True, mask=1), dict(h=64, dense=True, mask=2)], ids=str)
+def test_scratch_of_the_size_asked_for(saw, options, n, lens):
+    """Nothing behind it is written, and nothing of what it held counts."""
+    c = Case(saw, n, lens, seed=21, **options)
+    q = c.args[0]
+    need = saw.paged_prompt_workspace_bytes(c.cache, q, len(n), c.pt.shape[1] * 16)
+    got = []
+    for fill in (0, 0xff):
+        ws = torch.full((need + 4096,), fill, dtype=torch.uint8, device="cuda")
+        got.append(saw.paged_prompt_attn(c.cache, *c.args, workspace=ws[:need]))
+        assert bool((ws[need:] == fill).all())
+    assert torch.equal(*got)
+    want, tol = c.attention()
+    pc.check(got[0], want, tol)
+
+
 # ---- accumulated weights ----
 def _scores(c, prev):
     """(scores, bound): a weight is off by at most w (exp(2 e) - 1 + 2^-20 + n 2^-22); then sums of as many terms as there are rows, in fp32."""

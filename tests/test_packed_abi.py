@@ -148,6 +148,19 @@ def test_the_binding_sizes_scratch_for_every_bound_that_the_call_takes(saw):
     assert saw.prompt_workspace_bytes(q, k, 1, 400) < need
 
 
+def test_scratch_is_asked_for_where_it_is_used(saw):
+    """Records of split keys or for a learned rotation of V, rotated queries for one of K; nothing of rows otherwise."""
+    L = saw.lib()
+    rows, record, query = 2048 * 32, 130 * 4, 128 * 2 + 4
+    for kw, each in ((dict(), 0), (dict(dense_rot=A), record + query), (dict(dense_rot=A, rotate_mask=1), query), (dict(dense_rot=A, rotate_mask=2), record),
+                     (dict(dense_rot=A, rotate_mask=0), 0)):
+        need = L.saw_paged_prompt_workspace_bytes(ctypes.byref(_cache(saw, **kw)), 32, 2048, 1, 18432)
+        assert rows * each < need <= rows * each + 64, kw
+    r = ctypes.byref(_cache(saw))
+    assert L.saw_paged_prompt_workspace_bytes(r, 32, 160, 32, 4096) >= 2 * 160 * 32 * record       # (few rows: split)
+    assert L.saw_paged_prompt_attn(*{**PAGED, "cache": r, "T": 2048, "B": 1, "max_pages": 1152, "workspace_bytes": 31}.values()) == EWORKSPACE
+
+
 def test_workspaces_without_queries(saw):
     L, r = saw.lib(), ctypes.byref(_cache(saw))
     for B in (1, 7, 65535):
