@@ -386,7 +386,9 @@ int saw_flatten_dequant(const saw_cache_t* cache, const int32_t* page_table,
  * Logits, their maxima and sums and the output sums are fp32; the weights enter the product with V in dtype's precision
  * (half a step: 2^-8 for bf16, 2^-11 for fp16, as the output's own; fp16 weights of less than 2^-21 of the row's largest are off
  * by 2^-32 of that one at most).  A masked key counts for nothing whatever it
- * and its value hold (NaN and infinities too).  A row whose logits are all -infinity gets zeros.
+ * and its value hold (NaN and infinities too).  A row whose logits are all -infinity gets zeros, one with a logit of NaN or +infinity (also by
+ * overflow of fp32) NaN.  An infinite value makes its channel infinite in the rows that see it; values of both infinities, or NaN, make it
+ * NaN.  A call that meets such values takes a few times as long.
  * T_q == 0 is a no-op.  head_dim 64 or 128; n_q_heads / n_kv_heads in {1, 2, 4, 8}; B <= 65535; T_k and T_q n_q_heads up to 2^31 - 2^16
  * (here and in the calls below, as bounds of lengths).
  */
@@ -409,8 +411,9 @@ int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, 
  *               records where keys are split, which calls of few rows need more of than large ones, and the rows of a learned rotation.
  * Rotated queries and dequantised keys enter their product as fp16 times powers of two (a query's of its row, keys' of the
  * sequence), weights and dequantised values theirs as fp16 too: half a step each, 2^-11, at least 2^-32 of the row's largest weight and
- * 2^-19 of the largest value that a row meets, whatever the size of those that it does not see; everything between and all sums are fp32.  Page ids of visible tokens outside
- * [0, num_pages) are read as page 0.  Alignment of the pools as for the decode calls.  T == 0 is a no-op.
+ * 2^-19 of the largest value that a row meets, whatever the size of those that it does not see; everything between and all sums are
+ * fp32.  What is no number shows as above, values in the space that they are stored in.  Page ids of visible tokens outside [0, num_pages)
+ * are read as page 0.  Alignment of the pools as for the decode calls.  T == 0 is a no-op.
  */
 size_t saw_paged_prompt_workspace_bytes(const saw_cache_t* cache, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len);
 int saw_paged_prompt_attn(const saw_cache_t* cache, const void* q, int32_t dtype, int64_t T, int64_t q_stride, int32_t n_q_heads,

@@ -9,15 +9,19 @@ namespace saw {
 
 enum { kKvBf16, kKvF16, kKvInt4 };
 
-// Channels of one vector that a lane holds: lane, lane + 64.
+// Channels of one vector that a lane holds: lane, lane + 64.  page: of position j, INT4 (eight positions from a multiple of eight on share theirs).
 template <int D, int KV>
 struct RowSource {
   const PromptParams& p;
   int b, h, k0, lane;
-  __device__ void load(bool value, int j, float (&x)[D / 64]) const {
+  __device__ int page_of(int j) const {
+    if constexpr (KV != kKvInt4) return 0;
+    const int page = p.page_table[(int64_t)b * p.max_pages + (j >> 4)];
+    return page < 0 || page >= p.num_pages ? 0 : page;
+  }
+  __device__ f32x2 value_pair_of(int page, int j) const { return *(const f32x2*)(p.v_meta + 2 * (((int64_t)page * p.n_kv_heads + h) * 16 + (j & 15))); }
+  __device__ void load(bool value, int page, int j, float (&x)[D / 64]) const {
     if constexpr (KV == kKvInt4) {
-      int page = p.page_table[(int64_t)b * p.max_pages + (j >> 4)];
-      if (page < 0 || page >= p.num_pages) page = 0;
       const int64_t vec = ((int64_t)page * p.n_kv_heads + h) * 16 + (j & 15);
       const float* const m = (value ? p.v_meta : p.k_meta) + 2 * vec;
       const uint8_t* const c = (value ? p.v_codes : p.k_codes) + vec * (D / 2);
@@ -38,6 +42,10 @@ struct RowSource {
 // A rotated query becomes fp16 times 2^-e with the row's largest channel in [2^14, 2^15): relative rounding 2^-11 whatever the row's
 // size down to 2^-28 of the largest channel, smaller ones are off by 2^-39 of it.
 __device__ __forceinline__ int query_exponent(float top) { return min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14; }
+
+// What logits are multiplied by is no less (products of fp16 are below 2^37, so that they stay as good as zero): zero times a masked logit
+// would be no number.
+constexpr float kLeastScale = 0x1p-126f;
 
 // Queries under a learned rotation, whose 64 KiB a block of rows would read again: a wavefront for NV rows, which read them once.
 //   ws: [rows][D] fp16 | [rows] float 2^e
@@ -106,10 +114,38 @@ __device__ __forceinline__ void put_piece(char* tile, int row, int piece, u32x4 
   }
 }
 
-// The largest that a token's values can be, from its pair alone; zero if that is no number (it shows in the result by itself).
+// The largest that a token's values can be, from its pair alone; infinity if that is no number.
 __device__ __forceinline__ float largest_value(f32x2 pair) {
   const float sz = pair.x * pair.y, most = fmaxf(fabsf(sz), fabsf(fmaf(15.f, pair.x, -sz)));
-  return most < INFINITY ? most : 0.f;
+  return most < INFINITY ? most : INFINITY;
+}
+// Sums of values with a larger unit are looked at once more when they have it: below it fp32 holds 2^15 (tile_weights) times 2^15 times 2^31 tokens.
+constexpr float kLargeUnit = 0x1p60f;
+
+// 16-bit numbers of a word that are none become zero.
+template <typename M>
+__device__ __forceinline__ uint32_t numbers_only(uint32_t w) {
+  constexpr uint32_t kExponent = std::is_same<M, MathBf16>::value ? 0x7f80 : 0x7c00;
+  return ((w & kExponent) == kExponent ? 0 : w & 0xffffu) | (((w >> 16) & kExponent) == kExponent ? 0 : w & 0xffff0000u);
+}
+
+template <int D>
+__device__ __forceinline__ void clear(RowState<D>& st) {
+  st.m = -INFINITY; st.ref = 0.f; st.sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st.o[t][r] = 0.f;
+}
+// some output sum of the lane's row is no number
+template <int D>
+__device__ __forceinline__ bool no_sum(const RowState<D>& st) {
+  float odd = 0.f;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) odd = fmaf(st.o[t][r], 0.f, odd);
+  return odd != odd;
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
@@ -122,18 +158,21 @@ __device__ __forceinline__ float wave_max(float x) {
 // largest so far.  (A power for every tile by itself would be a maximum over all lanes for each: 2048 tokens over 16384 760 us, ragged
 // fp16 chunks 174.)
 //   Rows need not see the key that sets the unit.  `floor` is no more than the largest that any row met (of keys that all of the
-// wavefront's rows see); where the unit is set by one 2^12 times as large the sums are given up, and finish_rows takes the rows again key
-// by key.
+// wavefront's rows see); where the unit is set by one 2^12 times as large the sums are given up, and finish_rows takes the rows again.
+//   Tokens that are no numbers do not count.
 struct Unit {
   int e = 0;
   float limit = 0.f, floor = 0.f;
   bool lost = false;
+  __device__ __forceinline__ bool passed(float mine, bool first) const { return first || __any(mine >= limit); }
   // mine: the largest of the lane's keys; all_see: of those that every row sees, `whole`: all of the tile.  true: raised by 2^by
   template <typename F>
   __device__ __forceinline__ bool fit(float mine, bool first, bool whole, int& by, F all_see) {
-    if (!first && !__any(mine >= limit)) return false;
-    const float top = wave_max(mine);
-    floor = whole ? top : fmaxf(floor, wave_max(all_see()));
+    if (!passed(mine, first)) return false;
+    auto number = [](float x) { return x < INFINITY ? x : 0.f; };
+    const float top = wave_max(number(mine));
+    if (!first && top < limit) return false;
+    floor = whole ? top : fmaxf(floor, wave_max(number(all_see())));
     lost = lost || top > 4096.f * floor;
     const int to = max((int)(__float_as_uint(top) >> 23) - 127, -100) - 6;
     by = min(to - e, 126);
@@ -171,7 +210,7 @@ __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token,
           const u32x4 w = qf[ks];
           qf[ks] = u32x4{(w.x & 0xffffu) | w.z << 16, w.x >> 16 | (w.z & 0xffff0000u), (w.y & 0xffffu) | w.w << 16, w.y >> 16 | (w.w & 0xffff0000u)};
         }
-      return p.scale * p.query_scale[at];
+      return fmaxf(p.scale * p.query_scale[at], kLeastScale);
     }
     float x[D / 2];
 #pragma unroll
@@ -199,7 +238,7 @@ __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token,
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         qf[ks][i] = CODES ? MathF16::pack(x[8 * ks + i] * down, x[8 * ks + i + 4] * down) : MathF16::pack(x[8 * ks + 2 * i] * down, x[8 * ks + 2 * i + 1] * down);
-    return p.scale * __uint_as_float((uint32_t)(127 + ex) << 23);
+    return fmaxf(p.scale * __uint_as_float((uint32_t)(127 + ex) << 23), kLeastScale);
   }
   return p.scale;
 }
@@ -211,34 +250,132 @@ __device__ __forceinline__ float2* partial_sums(const PromptParams& p) {
   return (float2*)(p.ws + (int64_t)gridDim.y * rows * D) + (int64_t)blockIdx.y * rows;
 }
 
+// The first positions of [j0, j1), j0 a multiple of eight, whose value is NaN, +infinity, -infinity in the lane's channels, and, INT4, of a token whose
+// value is a number there and not in all its channels.
+template <int D, int KV>
+__device__ __forceinline__ void first_odd_values(const RowSource<D, KV>& src, int j0, int j1, int (&first)[3][D / 64], int& mixed) {
+  constexpr int E = D / 64, kAhead = 8;                                   // values on their way at once
+  mixed = INT32_MAX;
+#pragma unroll
+  for (int e = 0; e < E; ++e) first[0][e] = first[1][e] = first[2][e] = INT32_MAX;
+  for (int j = j0; j < j1; j += kAhead) {
+    float v[kAhead][E];
+    const int page = src.page_of(j);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) src.load(true, page, min(j + u, j1 - 1), v[u]);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int at = min(j + u, j1 - 1);
+      bool none = true;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (v[u][e] != v[u][e]) first[0][e] = min(first[0][e], at);
+        if (v[u][e] == INFINITY) first[1][e] = min(first[1][e], at);
+        if (v[u][e] == -INFINITY) first[2][e] = min(first[2][e], at);
+        none = none && !(fabsf(v[u][e]) < INFINITY);
+      }
+      if constexpr (KV == kKvInt4)
+        if (!none && largest_value(src.value_pair_of(page, at)) == INFINITY) mixed = min(mixed, at);
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) mixed = min(mixed, __shfl_xor(mixed, d));
+}
+
+// A channel's sum, given the first positions of odd values and how many positions its row sees
+__device__ __forceinline__ float odd_sum(int nan, int pos, int neg, int sees, float o) {
+  return min(nan, max(pos, neg)) < sees ? NAN : pos < sees ? INFINITY : neg < sees ? -INFINITY : o;
+}
+
+// Values that are no numbers.  A masked key's weight is zero, and one that is seen may be rounded to zero, but zero times infinity is no number.
+// So they are left out, and the first positions of those that were (one reading of the values) say which sums are infinite or none:
+//   * tokens in the INT4 pages, whose pairs tell, right away.  What is no number even then - sums of finite values that overflow, tokens that have
+//     numbers in some channels only - and sums that lost their precision (Unit) are rows that are taken again, eight keys at a time over
+//     the keys that each sees.
+//   * 16-bit values, which no instruction looks at on their way, once a sum ended as none: the wavefront goes over its keys again.
+
+// ... with keys and values from memory to operand registers.  (bf16: weights up to 1, with which fewer sums of large values overflow.)
+struct LowBf16 : MathBf16 { static constexpr float kRaise = -8.f; };
+template <int D, typename M>
+__device__ __forceinline__ void rows_of_numbers(const PromptParams& p, int h, int k0, int len, int t0, int t1, int sees, int wend,
+                                                const u32x4 (&qf)[D / 16], float scale, RowState<D>& st, int lane) {
+  const int half = lane >> 5, in = lane & 31;
+  const uint16_t* const k = (const uint16_t*)p.k + (int64_t)k0 * p.k_stride + (int64_t)h * D + 8 * half;
+  const uint16_t* const v = (const uint16_t*)p.v + (int64_t)k0 * p.v_stride + (int64_t)h * D + in;
+  clear(st);
+  for (int t = t0; t < t1 && t * kTileKeys < wend; ++t) {
+    f32x16 s[2];
+    u32x4 pf[4];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int64_t key = min(t * kTileKeys + 32 * kb + in, len - 1);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) s[kb] = M::mfma(*(const u32x4*)(k + key * p.k_stride + 16 * ks), qf[ks], s[kb]);
+    }
+    tile_mask(s, sees - t * kTileKeys, lane);
+    tile_weights<D, typename std::conditional<std::is_same<M, MathBf16>::value, LowBf16, M>::type>(s, scale, st, pf);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const uint16_t* at[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) at[i] = v + (int64_t)min(t * kTileKeys + 16 * ks + 4 * half + (i & 3) + 8 * (i >> 2), len - 1) * p.v_stride;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = numbers_only<M>((uint32_t)at[2 * i][32 * c] | (uint32_t)at[2 * i + 1][32 * c] << 16);
+        st.o[c] = M::mfma(w, pf[ks], st.o[c]);
+      }
+    }
+  }
+}
+
 // The end of a wavefront's 32 rows: outputs, or partial records [split][row][D] and [split][row] (reference, sum) where the keys are split
-// or a learned rotation has to be undone.  scale: of the rows' logits; unit: of the output sums.
+// or a learned rotation has to be undone.  scale: of the rows' logits; sees: keys that the lane's row sees, wend: the last row; odd: values were
+// left out (INT4); lost: the sums are not precise enough.
 template <int D, int KV, int HALF_BIT, bool CODES = false>
 __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile& rt, int w0, int last, int row, int h, int64_t token, int head,
-                                            int k0, int len, int t0, int t1, const u32x4 (&qf)[D / 16], float scale, float unit, RowState<D>& st, int lane) {
+                                            int k0, int len, int t0, int t1, int sees, int wend, bool odd, bool lost, const u32x4 (&qf)[D / 16], float scale,
+                                            RowState<D>& st, int lane) {
   constexpr bool kInt4 = KV == kKvInt4;
   const int shift = __builtin_ctz(p.group);
-  const float sum = add_xor32(st.sum);
+  float sum = add_xor32(st.sum);
   const int64_t at = token * p.n_q_heads + head;
-  // Values that are no numbers: a masked key's weight is zero, but zero times infinity is not.  Rows of a wavefront that ended with one
-  // are taken again, key by key, over the keys that each sees.
-  float odd = 0.f;
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) odd = fmaf(st.o[t][r], 0.f, odd);
   const bool split = gridDim.y > 1 || (kInt4 && p.dense_v);
   const int64_t rows = p.T_q * p.n_q_heads;
   float* const records = p.ws + (int64_t)blockIdx.y * rows * D;
   float2* const ml = partial_sums<D>(p);
-  if (__any(odd != odd)) {
-    constexpr int E = D / 64;
+  uint32_t again = 0;                                                     // rows that are taken again
+  if constexpr (!kInt4) odd = __any(row <= last && no_sum<D>(st));
+  if (w0 <= last && (odd || lost)) {
+    constexpr int E = D / 64, kAhead = 8;                                 // keys at once
+    using M = typename std::conditional<KV == kKvBf16, MathBf16, MathF16>::type;
+    if constexpr (!kInt4) {
+      rows_of_numbers<D, M>(p, h, k0, len, t0, t1, sees, wend, qf, scale, st, lane);
+      sum = add_xor32(st.sum);
+    }
     const RowSource<D, KV> src = {p, rt.b, h, k0, lane};
-    for (int i = 0; i < 32 && w0 + i <= last; ++i) {
-      const int tok_i = (w0 + i) >> shift;
+    int first[3][E], mixed;
+    first_odd_values(src, t0 * kTileKeys, min(wend, t1 * kTileKeys), first, mixed);
+    bool redo = lost || mixed < sees;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int from = (32 * t + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) & 63;
+        const int nan = __shfl(first[0][t / 2], from), pos = __shfl(first[1][t / 2], from), neg = __shfl(first[2][t / 2], from);
+        redo = redo || !(fabsf(st.o[t][r]) < INFINITY);
+        st.o[t][r] = sum == sum ? odd_sum(nan, pos, neg, sees, st.o[t][r]) : NAN;       // (a logit is none: nor is anything of the row)
+      }
+    const uint64_t which = __ballot(kInt4 && redo && row <= last && sum == sum);
+    again = __builtin_amdgcn_readfirstlane((uint32_t)which | (uint32_t)(which >> 32));
+    if constexpr (kInt4) for (uint32_t left = again; left; left &= left - 1) {
+      const int i = __builtin_ctz(left), tok_i = (w0 + i) >> shift;
       const int64_t mine = (int64_t)(rt.begin + tok_i) * p.n_q_heads + h * p.group + ((w0 + i) & (p.group - 1));
-      const int sees = p.causal ? max(min(len, len - rt.n + tok_i + 1), 0) : len;
-      const int end = min(sees, t1 * kTileKeys);
+      const int sees_i = max(min(len, len - rt.n + tok_i + 1), 0);
+      const int end = min(sees_i, t1 * kTileKeys);
       const float row_scale = __shfl(scale, i);
       float q[E], acc[E], m = -INFINITY, den = 0.f;
 #pragma unroll
@@ -253,23 +390,40 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
             const uint32_t w = __shfl((int)qf[ks][d], i + 32 * half), x = v & 1 ? w >> 16 : w & 0xffffu;
-            if (v >> 1 == 4 * ks + d) q[e] = (KV == kKvBf16 ? bf16_to_f32(x) : f16_to_f32(x)) * row_scale;
+            if (v >> 1 == 4 * ks + d) q[e] = f16_to_f32(x) * row_scale;
           }
       }
-      for (int j = t0 * kTileKeys; j < end; ++j) {
-        float k[E], v[E], x = 0.f;
-        src.load(false, j, k);
-        src.load(true, j, v);
+      for (int j = t0 * kTileKeys; j < end; j += kAhead) {
+        float kv[kAhead][E], x[kAhead], top = m;
+        const int page = src.page_of(j);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
-        x = add_xor32(add_xor16(row_allsum(x)));
-        const float top = fmaxf(m, x), ref = top == -INFINITY ? 0.f : top;
-        const float alpha = fast_exp2(m - ref), w = fast_exp2(x - ref);
+        for (int u = 0; u < kAhead; ++u) src.load(false, page, min(j + u, end - 1), kv[u]);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          x[u] = 0.f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[u] = fmaf(q[e], kv[u][e], x[u]);
+          x[u] = add_xor32(add_xor16(row_allsum(x[u])));
+          if (j + u < end) top = fmaxf(top, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) src.load(true, page, min(j + u, end - 1), kv[u]);
+        const float ref = top == -INFINITY ? 0.f : top, alpha = fast_exp2(m - ref);
         m = top;
-        den = fmaf(den, alpha, w);
+        den *= alpha;
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(acc[e], alpha, w * v[e]);
+        for (int e = 0; e < E; ++e) acc[e] *= alpha;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          if (j + u < end) {
+            const float w = fast_exp2(x[u] - ref);
+            den += w;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(w, kv[u][e], acc[e]);
+          }
       }
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = odd_sum(first[0][e], first[1][e], first[2][e], sees_i, acc[e]);
       if (split) {
 #pragma unroll
         for (int e = 0; e < E; ++e) records[mine * D + lane + 64 * e] = acc[e];
@@ -278,7 +432,7 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
         float x[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = den == 0.f ? 0.f : acc[e] / den;
-        if (kInt4 && p.rot_v) {                                          // (lane + 64 e: bits 0 to 5 across the lanes, the last in the lane)
+        if (p.rot_v) {                                                   // (lane + 64 e: bits 0 to 5 across the lanes, the last in the lane)
           for (int st = 1; st < p.had_block && st < 64; st <<= 1)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -293,28 +447,28 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
         for (int e = 0; e < E; ++e) store_elem(p.out, p.dtype, mine * D + lane + 64 * e, x[e]);
       }
     }
-    return;
   }
+  const bool done = row > last || (again >> (lane & 31) & 1);
   if (split) {
-    if (row > last) return;
-    if (lane < 32) ml[at] = make_float2(st.m - std::conditional<KV == kKvBf16, MathBf16, MathF16>::type::kRaise, sum);
+    if (done) return;
+    if (lane < 32) ml[at] = make_float2(st.m == -INFINITY ? st.m : st.ref, sum);
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
-        *(f32x4*)(records + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) = f32x4{st.o[t][r] * unit, st.o[t][r + 1] * unit, st.o[t][r + 2] * unit, st.o[t][r + 3] * unit};
+        *(f32x4*)(records + at * D + 32 * t + 2 * r + 4 * (lane >> 5)) = f32x4{st.o[t][r], st.o[t][r + 1], st.o[t][r + 2], st.o[t][r + 3]};
     return;
   }
   float inv = sum == 0.f ? 0.f : 1.f / sum;
   float x[D / 2];
 #pragma unroll
-  for (int i = 0; i < D / 2; ++i) x[i] = kInt4 ? st.o[i / 16][i % 16] * unit : st.o[i / 16][i % 16];
+  for (int i = 0; i < D / 2; ++i) x[i] = st.o[i / 16][i % 16];
   if (kInt4 && p.rot_v) {
     fwht_rows<D, 2>(x, p.had_block, lane);                               // (accumulators: the half is bit 2 of the channel)
     if (p.has_signs) sign_rows<D, 2>(x, p.signs, lane);
     inv *= had_norm(p.had_block);
   }
-  if (row > last) return;
+  if (done) return;
 #pragma unroll
   for (int i = 0; i < D / 2; i += 4) {
     const bool bf16 = kInt4 ? p.dtype == SAW_BF16 : KV == kKvBf16;
@@ -366,13 +520,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
   u32x4 qf[D / 16];
   const float scale = row_query<D, KV, 3>(p, token, head, lane, qf);
   RowState<D> st;
-  st.m = -INFINITY; st.ref = 0.f; st.sum = 0.f;
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) st.o[t][r] = 0.f;
+  clear(st);
 
-  Unit keys, values;                                                      // (INT4)
+  bool odd = false;                                                       // (INT4) values that are no numbers were met
+  Unit keys, values;
   auto products = [&](int buf, int t, float tile_scale) {
     if (t * kTileKeys >= wend) return;
     f32x16 s[2];
@@ -425,12 +576,20 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
       if (t * kTileKeys + lane >= len) c.key_pair = c.value_pair = f32x2{0.f, 0.f};
     };
     const int seen = max(sees_of(w0), t0 * kTileKeys + 1);                   // keys in front of it are seen by every row that sees any
-    auto put = [&](int buf, const Pieces& c, int t) {                        // returns what the tile's logits are to be multiplied by
+    auto put = [&](int buf, Pieces& c, int t) {                              // returns what the tile's logits are to be multiplied by
       const bool whole = (t + 1) * kTileKeys <= seen, mine = t * kTileKeys + lane < seen;
       const float key = largest_value(c.key_pair), value = largest_value(c.value_pair);
       int by;
       keys.fit(key, t == t0, whole, by, [&] { return mine ? key : 0.f; });
-      if (values.fit(value, t == t0, whole, by, [&] { return mine ? value : 0.f; })) rescale<D>(st, power_of_two(-by));
+      if (values.passed(value, t == t0)) {
+        if (__any(value == INFINITY)) {
+          odd = true;
+#pragma unroll
+          for (int j = 0; j < Pieces::kEach; ++j)
+            if (j * threads + (int)threadIdx.x >= Pieces::kPieces / 2 && largest_value(c.pair[j]) == INFINITY) c.pair[j] = f32x2{0.f, 0.f};
+        }
+        if (values.fit(value, t == t0, whole, by, [&] { return mine ? value : 0.f; })) rescale<D>(st, power_of_two(-by));
+      }
       const float down = keys.down(), down_v = values.down();
 #pragma unroll
       for (int j = 0; j < Pieces::kEach; ++j) {
@@ -456,12 +615,13 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
         request(t + 1, c);
         ids.fetch(pages, t + 2, len);
       }
-      products(buf, t, scale * tile_scale);
+      products(buf, t, fmaxf(scale * tile_scale, kLeastScale));
       if (t + 1 < t1) tile_scale = put(buf ^ 1, c, t + 1);
     }
+    rescale<D>(st, values.up());
+    if (values.up() > kLargeUnit) odd = odd || __any(row <= last && no_sum<D>(st));
   }
-  if (keys.lost || values.lost) st.o[0][0] = NAN;
-  finish_rows<D, KV, 3>(p, rt, w0, last, row, h, token, head, k0, len, t0, t1, qf, scale, kInt4 ? values.up() : 1.f, st, lane);
+  finish_rows<D, KV, 3>(p, rt, w0, last, row, h, token, head, k0, len, t0, t1, sees, wend, odd, keys.lost || values.lost, qf, scale, st, lane);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
@@ -538,12 +698,9 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   sum_q = add_xor32(sum_q);
   const CodeBits bits;
   RowState<D> st;
-  st.m = -INFINITY; st.ref = 0.f; st.sum = 0.f;
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) st.o[t][r] = 0.f;
+  clear(st);
 
+  bool odd = false;                                                       // values that are no numbers were met
   Unit values;
   const int seen = max(sees_of(rt.row0), (t0 + wave) * kTileKeys + 1);
   for (int t = t0 + wave; t < t1; t += NW) {
@@ -557,7 +714,16 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     };
     int by;
     const bool whole = (t + 1) * kTileKeys <= seen;
-    if (values.fit(largest_of_values(len), t == t0 + wave, whole, by, [&] { return largest_of_values(seen); })) rescale<D>(st, power_of_two(-by));
+    const float top = largest_of_values(len);
+    if (values.passed(top, t == t0 + wave)) {
+      if (__any(top == INFINITY)) {
+        odd = true;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
+          if (largest_value(vpair[j]) == INFINITY) vpair[j] = f32x2{0.f, 0.f};
+      }
+      if (values.fit(largest_of_values(len), t == t0 + wave, whole, by, [&] { return largest_of_values(seen); })) rescale<D>(st, power_of_two(-by));
+    }
     const float down_v = values.down();
     // logits: s_j (q . (c_j - 8) - (z_j - 8) sum q), with the codes exact and each pair from shared memory where its key stands
     pairs[wave][lane] = t * kTileKeys + lane < len ? f32x2{kpair.x, 8.f - kpair.y} : f32x2{0.f, 0.f};
@@ -599,7 +765,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   // the other wavefronts' states join the first's
   wave_sync();
   rescale<D>(st, values.up());
-  if (values.lost) st.o[0][0] = NAN;
+  if (lane == 0) pairs[wave][0] = f32x2{odd || values.up() > kLargeUnit ? 1.f : 0.f, values.lost ? 1.f : 0.f};
   if (wave > 0) {
 #pragma unroll
     for (int i = 0; i < D / 2; i += 4) *(f32x4*)(mine + i * 256 + 16 * lane) = f32x4{st.o[i / 16][i % 16], st.o[i / 16][i % 16 + 1], st.o[i / 16][i % 16 + 2], st.o[i / 16][i % 16 + 3]};
@@ -625,7 +791,12 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     }
   }
   st.m = m;
-  finish_rows<D, kKvInt4, kHalfBit, true>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, qf, scale, 1.f, st, lane);
+  st.ref = m == -INFINITY ? 0.f : m - MathF16::kRaise;
+  float look = 0.f, lost = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) { look += pairs[w][0].x; lost += pairs[w][0].y; }
+  finish_rows<D, kKvInt4, kHalfBit, true>(p, rt, rt.row0, last, row, h, token, head, 0, len, t0, t1, sees, kend, look != 0.f, lost != 0.f, qf, scale, st,
+                                          lane);
 }
 
 // The output of a row from its partial records; false: the row is no sequence's.

@@ -75,3 +75,33 @@ def check(got, want, tol, what=""):
     err = np.abs(got.double().cpu().numpy() - want)
     bad = ~(err <= tol)
     assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, first {np.argwhere(bad)[0]}, {err[bad].max():.3g} against {tol[bad][err[bad].argmax()]:.3g}"
+
+
+def check_odd(got, want, tol, odd, cu_q, cu_k, causal, G, what=""):
+    """A channel is NaN where its row sees a NaN or infinities of both signs, infinite where it sees one, and what the finite values give elsewhere.
+    odd [T_k][Hkv][d]: the values in float64."""
+    got = got.double().cpu().numpy()
+    for b in range(len(cu_q) - 1):
+        n, L = cu_q[b + 1] - cu_q[b], cu_k[b + 1] - cu_k[b]
+        x = odd[cu_k[b]:cu_k[b + 1]]
+        for i in range(n):
+            seen = x[:max(L - n + i + 1, 0) if causal else L]
+            nan, pos, neg = (f(seen).any(0).repeat(G, 0) for f in (np.isnan, np.isposinf, np.isneginf))
+            o = got[cu_q[b] + i]
+            assert np.isnan(o[nan | (pos & neg)]).all(), (what, b, i)
+            assert np.isposinf(o[pos & ~neg & ~nan]).all() and np.isneginf(o[neg & ~pos & ~nan]).all(), (what, b, i)
+            fine = ~(nan | pos | neg)
+            assert (np.abs(o - want[cu_q[b] + i])[fine] <= tol[cu_q[b] + i][fine]).all(), (what, b, i)
+
+
+def milliseconds(f):
+    """The best of four calls."""
+    best = []
+    for _ in range(4):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f()
+        b.record()
+        torch.cuda.synchronize()
+        best.append(a.elapsed_time(b))
+    return min(best)

@@ -344,6 +344,58 @@ def test_scratch_of_the_size_asked_for(saw, options, n, lens):
     pc.check(got[0], want, tol)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8)])
+@pytest.mark.parametrize("n,lens", [([3, 5], [50, 900]), ([40, 150], [50, 160]), ([1], [6000]), ([100], [3000])], ids=str)
+def test_values_that_are_no_numbers_show_where_they_are_seen(saw, n, lens, d, G, dtype):
+    """Scales that are NaN or infinite: without a rotation a code above the zero-point is +infinity, one below -infinity, one at it NaN."""
+    c = Case(saw, n, lens, d=d, G=G, h=1, dtype=dtype, seed=17)
+    want, tol = c.attention()
+    for seed, count in ((1, 1), (2, 2), (3, 12)):
+        rng = np.random.default_rng(seed)
+        ref = c.ref["v_meta"].copy()
+        rest = c.ref["v_meta"].copy()
+        for _ in range(count):
+            b = rng.integers(len(n))
+            at, g = rng.integers(max(0, lens[b] - 2 * n[b] - 20), lens[b]), rng.integers(2)
+            ref[c.pt[b, at // 16], g, at % 16, 0] = rng.choice([np.nan, np.inf, -np.inf])
+            rest[c.pt[b, at // 16], g, at % 16, 0] = 0
+        keep = c.ref["v_meta"]
+        c.ref["v_meta"] = rest
+        want, tol = c.attention()
+        c.ref["v_meta"] = ref
+        with np.errstate(invalid="ignore"):
+            values = np.concatenate([O._gather(c.ref, "v", c.pt[b], 0, L) for b, L in enumerate(lens)])
+        c.ref["v_meta"] = keep
+        c.cache.v_meta.copy_(torch.from_numpy(ref).reshape(c.cache.v_meta.shape))
+        got = saw.paged_prompt_attn(c.cache, *c.args)
+        pc.check_odd(got, want, tol, values, c.cu, pc.offsets(lens), True, G, count)
+
+
+@pytest.mark.parametrize("n", [3, 80])
+@pytest.mark.parametrize("size", [1.0, 1e-30])
+def test_queries_of_zeros(saw, n, size):
+    """A padded batch's: every token that they see weighs the same, however small the keys are."""
+    c = Case(saw, [n], [300], h=1, seed=3)
+    c.q.zero_()
+    c.args[0].zero_()
+    c.cache.k_meta[..., 0] *= size
+    c.ref["k_meta"][..., 0] *= np.float32(size)
+    want, tol = c.attention()
+    pc.check(saw.paged_prompt_attn(c.cache, *c.args), want, tol)
+
+
+@pytest.mark.parametrize("n", [8, 512])
+def test_a_value_that_is_no_number_does_not_take_the_call_apart(saw, n):
+    c = Case(saw, [n], [8192], Hkv=8, G=4, seed=3)
+    ws, out = torch.empty(1 << 27, dtype=torch.uint8, device="cuda"), torch.empty_like(c.args[0])
+    call = lambda: saw.paged_prompt_attn(c.cache, *c.args, out=out, workspace=ws)  # noqa: E731
+    clean = pc.milliseconds(call)
+    c.cache.v_meta[c.pt[0, 0], :, 0] = float("nan")
+    odd = pc.milliseconds(call)
+    assert odd < 20 * clean + 1
+
+
 # ---- accumulated weights ----
 def _scores(c, prev):
     """(scores, bound): a weight is off by at most w (exp(2 e) - 1 + 2^-20 + n 2^-22); then sums of as many terms as there are rows, in fp32."""

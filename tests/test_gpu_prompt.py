@@ -235,3 +235,86 @@ def test_many_small_weights(saw, B, n, L, d, dtype):
     # (fp16 outputs below 2^-14: half of fp16's smallest step)
     tol = want * (2 * pc.U[dtype] + 2.0 ** -18 + L * 2.0 ** -22) * 1.01 + tail * L * 2.0 ** -32 + (2.0 ** -25 if dtype == FP else 0)
     assert (np.abs(got - want) <= tol).all(), np.nanmax(np.abs(got - want) / tol)
+
+
+def _odd_values(v, seed, count):
+    """v with `count` elements that are no numbers, and what is left of it with zeros there."""
+    g = torch.Generator().manual_seed(seed)
+    at = torch.randint(v.numel(), (count,), generator=g)
+    odd = v.clone()
+    odd.view(-1)[at] = torch.tensor([float("nan"), float("inf"), -float("inf")], dtype=v.dtype)[torch.randint(3, (count,), generator=g)]
+    return odd, torch.where(torch.isfinite(odd), odd, torch.zeros_like(odd))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8), (128, 1)])
+@pytest.mark.parametrize("n_q,n_k,causal", [([20, 150, 33], [20, 150, 33], True), ([300], [300], True), ([3, 70], [2500, 90], True), ([40, 9], [200, 70], False)], ids=str)
+def test_values_that_are_no_numbers_show_where_they_are_seen(saw, n_q, n_k, causal, d, G, dtype):
+    cu_q, cu_k = pc.offsets(n_q), pc.offsets(n_k)
+    q, k, v = pc.rand((cu_q[-1], 2 * G, d), 1, dtype), pc.rand((cu_k[-1], 2, d), 2, dtype), pc.rand((cu_k[-1], 2, d), 3, dtype)
+    for count in (1, 40, 2000):
+        odd, rest = _odd_values(v, count, count)
+        got = saw.prompt_attn(q.cuda(), k.cuda(), odd.cuda(), torch.from_numpy(cu_q).cuda(), torch.from_numpy(cu_k).cuda(), causal=causal)
+        want, tol = pc.prompt_reference(q, k, rest, cu_q, cu_k, causal)
+        pc.check_odd(got, want, tol, odd.double().numpy(), cu_q, cu_k, causal, G, count)
+
+
+def test_an_infinite_value_of_hardly_any_weight(saw):
+    """Its channel is infinite whatever the weight is rounded to."""
+    q, k = torch.ones((8, 2, 64), dtype=FP).cuda(), torch.zeros((100, 1, 64), dtype=FP).cuda()
+    v = pc.rand((100, 1, 64), 3, FP).cuda()
+    k[7, :, 0] = 300
+    v[50, :, 9], v[51, :, 10] = float("inf"), -float("inf")
+    out = saw.prompt_attn(q, k, v, torch.tensor([0, 8], dtype=torch.int32).cuda(), torch.tensor([0, 100], dtype=torch.int32).cuda(), sm_scale=1.0)
+    assert bool((out[..., 9] == float("inf")).all()) and bool((out[..., 10] == -float("inf")).all())
+    rest = [c for c in range(64) if c not in (9, 10)]
+    assert torch.equal(out[..., rest], v[7, 0, rest].expand(8, 2, 62))
+
+
+def test_rows_that_see_a_key_that_is_no_number(saw):
+    """Rows that see a key of NaN, or one whose logit is +infinity, are NaN; a logit of -infinity has no weight; the other rows are what they were."""
+    n, G, d = [20, 150, 33], 2, 64
+    cu = pc.offsets(n)
+    for dtype in (BF, FP):
+        q, k, v = pc.rand((203, 2 * G, d), 1, dtype), pc.rand((203, 2, d), 2, dtype), pc.rand((203, 2, d), 3, dtype)
+        q[..., 0] = q[..., 0].abs() + 0.5
+        want, tol = pc.prompt_reference(q, k, v, cu, cu, True)
+        for at in (60, 120, 169):                     # of the second sequence
+            # without the key: the sequence's rows behind it over the other keys (the first of these rows sees one key less than its successor)
+            rest = [20 + i for i in range(150) if 20 + i != at]
+            less, less_tol = pc.prompt_reference(q[at:170], k[rest], v[rest], [0, 170 - at], [0, 149], True)
+            for bad in (float("nan"), float("inf"), -float("inf")):
+                k2 = k.clone()
+                k2[at, :, 0] = bad
+                got = saw.prompt_attn(q.cuda(), k2.cuda(), v.cuda(), torch.from_numpy(cu).cuda())
+                pc.check(got[:at], want[:at], tol[:at], (at, bad))
+                pc.check(got[170:], want[170:], tol[170:], (at, bad))
+                if bad == -float("inf"):
+                    pc.check(got[at:170], less, less_tol, at)
+                else:
+                    assert bool(torch.isnan(got[at:170]).all()), (at, bad)
+
+
+def test_sums_of_large_values_that_do_not_overflow(saw):
+    """Values of 1e36: weights 2^7.5 of the first tile's would carry a sum past fp32's range on its way."""
+    q, k = torch.zeros((2, 4, 64), dtype=BF), torch.zeros((130, 2, 64), dtype=BF)
+    v = (pc.rand((130, 2, 64), 3, BF).float().sign() * 1e36).to(BF)
+    q[..., 0] = 1
+    k[64:, :, 0] = 5.1875
+    cu_q, cu_k = pc.offsets([2]), pc.offsets([130])
+    got = saw.prompt_attn(q.cuda(), k.cuda(), v.cuda(), torch.from_numpy(cu_q).cuda(), torch.from_numpy(cu_k).cuda(), sm_scale=1.0)
+    want, tol = pc.prompt_reference(q, k, v, cu_q, cu_k, True, 1.0)
+    pc.check(got, want, tol)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_value_that_is_no_number_does_not_take_the_call_apart(saw, bad):
+    """Seen by every row of a head, it costs a few readings of the values, not a pass key by key."""
+    n = 2048
+    q, k, v = pc.rand((n, 32, 128), 1, BF).cuda(), pc.rand((n, 8, 128), 2, BF).cuda(), pc.rand((n, 8, 128), 3, BF).cuda()
+    cu, ws, out = torch.tensor([0, n], dtype=torch.int32).cuda(), torch.empty(1 << 26, dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+    call = lambda: saw.prompt_attn(q, k, v, cu, out=out, workspace=ws)  # noqa: E731
+    clean = pc.milliseconds(call)
+    v[0, :, 5] = bad
+    odd = pc.milliseconds(call)
+    assert odd < 20 * clean + 1
