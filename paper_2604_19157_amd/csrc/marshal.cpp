@@ -290,6 +290,17 @@ PyObject* kv16_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (weak: beside a library that lacks these entry points the module still loads and serves the calls above)
+#pragma weak saw_prompt_attn
+#pragma weak saw_paged_prompt_attn
+#pragma weak saw_paged_attn_weights
+#pragma weak saw_evict_pages
+template <typename F>
+F present(F f) {
+  check(f != nullptr, "the library beside this module lacks the call");
+  return f;
+}
+
 // Every tensor of the calls below is on the GPU whose stream takes the call: an address of another device or of the host would fault there.
 template <typename... T>
 void on_this_gpu(const T&... t) {
@@ -343,7 +354,7 @@ PyObject* prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float scale = as_float(a[7]);
     check(ws.is_contiguous(), "the workspace is contiguous");
     on_this_gpu(q, k, v, cq, ck, out, ws);
-    return run(saw_prompt_attn, q.data_ptr(), k.data_ptr(), v.data_ptr(), type, (int32_t)q.size(2), (int32_t)q.size(1), (int32_t)k.size(1),
+    return run(present(&saw_prompt_attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), type, (int32_t)q.size(2), (int32_t)q.size(1), (int32_t)k.size(1),
                q.size(0), k.size(0), token_stride(q), token_stride(k), token_stride(v), oq, ok, (int32_t)(cq.numel() - 1), bound, causal, scale,
                out.data_ptr(), ws.data_ptr(), (size_t)ws.nbytes(), stream());
   });
@@ -366,7 +377,7 @@ PyObject* paged_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     check(ws.is_contiguous(), "the workspace is contiguous");
     on_this_gpu(q, cq, pt, lens, out, ws);
     pools_on_this_gpu(held);
-    return run(saw_paged_prompt_attn, &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
+    return run(present(&saw_paged_prompt_attn), &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
                (int32_t)pt.size(1), sl, bound, scale, out.data_ptr(), ws.data_ptr(), (size_t)ws.nbytes(), stream());
   });
 }
@@ -395,7 +406,7 @@ PyObject* attn_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
     on_this_gpu(q, cq, pt, lens, scores, ws);
     pools_on_this_gpu(held);
     if (prev) on_this_gpu(tensor(a[5]));
-    return run(saw_paged_attn_weights, &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
+    return run(present(&saw_paged_attn_weights), &c, q.data_ptr(), type, q.size(0), token_stride(q), (int32_t)q.size(1), oq, (int32_t)B, table,
                (int32_t)pt.size(1), sl, bound, scale, prev, to, stride, ws.data_ptr(), (size_t)ws.nbytes(), stream());
   });
 }
@@ -428,7 +439,7 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
       ws = w.data_ptr();
       ws_bytes = (size_t)w.nbytes();
     }
-    return run(saw_evict_pages, &c, from, stride, table, (int32_t)pt.size(1), sl, (int32_t)B, bound, budget, recent, to, (int32_t)dst.size(1), nl,
+    return run(present(&saw_evict_pages), &c, from, stride, table, (int32_t)pt.size(1), sl, (int32_t)B, bound, budget, recent, to, (int32_t)dst.size(1), nl,
                (int32_t*)kept.data_ptr(), out, out_stride, ws, ws_bytes, stream());
   });
 }
