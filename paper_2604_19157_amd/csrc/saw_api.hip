@@ -322,7 +322,7 @@ static int paged_args(const saw_cache_t* c, const void* q, int dtype, int64_t T,
   if (!group_ok(Hq, c->n_kv_heads) || !tokens_ok(T, B) || max_pages < 1) return SAW_EINVAL;
   const int64_t cap = (int64_t)max_pages * c->page_size;
   if (cap > 0x7fffffffLL || max_seq_len > cap || (max_seq_len <= 0 ? cap : max_seq_len) > kMaxTokens || !rows_ok(T, Hq)) return SAW_EINVAL;
-  if (!isfinite(sm_scale)) return SAW_EINVAL;
+  if (!isfinite(sm_scale) || !isfinite(log2_scale(sm_scale, c->head_dim))) return SAW_EINVAL;
   if (q_stride < (int64_t)Hq * c->head_dim || (q_stride & 7)) return SAW_EINVAL;
   if (!c->k_codes || !c->k_meta || (values && (!c->v_codes || !c->v_meta)) || !cu_q || !pt || !seq_lens || (T && (!q || !ws))) return SAW_ENULL;
   if (!aligned16(q) || !aligned16(ws) || !aligned16(c->k_codes) || !aligned16(c->k_meta) || !aligned4(cu_q) || !aligned4(pt) || !aligned4(seq_lens))
@@ -786,7 +786,7 @@ int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, 
                     size_t workspace_bytes, saw_stream_t stream) {
   if (dtype != SAW_F16 && dtype != SAW_BF16) return SAW_EINVAL;
   if ((head_dim != 64 && head_dim != 128) || !group_ok(n_q_heads, n_kv_heads) || !tokens_ok(T_q, B) || !tokens_ok(T_k, B) || !rows_ok(T_q, n_q_heads)) return SAW_EINVAL;
-  if (!isfinite(sm_scale)) return SAW_EINVAL;
+  if (!isfinite(sm_scale) || !isfinite(log2_scale(sm_scale, head_dim))) return SAW_EINVAL;
   const int64_t kv = (int64_t)n_kv_heads * head_dim;
   if (q_stride < (int64_t)n_q_heads * head_dim || k_stride < kv || v_stride < kv || ((q_stride | k_stride | v_stride) & 7)) return SAW_EINVAL;
   if (T_q == 0) return SAW_OK;

@@ -78,6 +78,15 @@ def test_weights_refusals(saw, change, code):
     assert saw.lib().saw_paged_attn_weights(*{**WEIGHTS, "cache": ctypes.byref(c), **change}.values()) == code
 
 
+@pytest.mark.parametrize("scale", [3e38, -math.inf, math.inf, math.nan])
+def test_logit_scales_beyond_fp32_are_refused(saw, scale):
+    """Logits are taken in log2 units: the scale times log2(e) has to be a number, or a logit of zero would be none."""
+    r = ctypes.byref(_cache(saw))
+    assert saw.lib().saw_prompt_attn(*{**PROMPT, "sm_scale": scale}.values()) == EINVAL
+    assert saw.lib().saw_paged_prompt_attn(*{**PAGED, "cache": r, "sm_scale": scale}.values()) == EINVAL
+    assert saw.lib().saw_paged_attn_weights(*{**WEIGHTS, "cache": r, "sm_scale": scale}.values()) == EINVAL
+
+
 def test_grids_beyond_32_bits_are_refused(saw):
     """Launches are counted in 32 bits of threads, and the weights' groups of rows in 16."""
     wide = dict(n_kv_heads=1024, n_q_heads=1024, T_q=1, q_stride=1024 * 128, k_stride=1024 * 128, v_stride=1024 * 128, B=65535)
