@@ -283,6 +283,10 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
     float total[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < 4; ++t) pair[t] = key_codes<D>(codes, bits, t, key0, len, lane, k[t]);
+    // (rows behind the last are zeros, and zero times an infinite scale is no number)
+    bool odd_scale = false;
+    if (!STATS && rows % kWeightRows)
+      odd_scale = __any(!(fmaxf(fmaxf(fabsf(pair[0].x), fabsf(pair[1].x)), fmaxf(fabsf(pair[2].x), fabsf(pair[3].x))) < INFINITY));
     keys.next(p, h, key0, lane, codes);
     // the first row that sees a key of the step: key0 < first_hidden + token
     const int first_token = max(key0 - first_hidden + 1, 0);
@@ -295,6 +299,12 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
       if (masked)
 #pragma unroll
         for (int t = 0; t < 4; ++t) hide(x[t], key0 + 16 * t + (lane & 15), len, first_hidden, shift, row0, lane);
+      if (odd_scale && g == all - 1)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (row0 + 4 * (lane >> 4) + r >= rows) x[t][r] = -INFINITY;
       f32x4 info[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) info[r] = tq.info[r];

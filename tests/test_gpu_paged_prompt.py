@@ -511,6 +511,24 @@ def test_weights_of_a_row_that_is_no_number_beside_an_infinite_key(saw, lens):
     assert bool(torch.isnan(got[0, :, :lens[0]]).all())
 
 
+@pytest.mark.parametrize("n", [1, 2, 7])
+@pytest.mark.parametrize("lens", [[60, 30], [5000, 30], [60] + [30] * 40, [5000] + [30] * 40], ids=len)
+def test_weights_of_a_key_of_minus_infinity(saw, lens, n):
+    """Its logits have no weight; the other positions get what they get without it."""
+    c = Case(saw, [n] + [0] * (len(lens) - 1), lens, Hkv=8, h=1, seed=5)
+    c.args[0].fill_(1)
+    c.q.fill_(1)
+    for j in (0, 17, lens[0] - n):                   # seen by every query
+        where = c.pt[0, j // 16], slice(None), j % 16
+        c.cache.k_codes[where] = 0
+        c.cache.k_meta[where] = torch.tensor([float("inf"), 8.0], device="cuda")
+        c.ref["k_codes"][where] = 0
+        c.ref["k_meta"][where] = (1e4, 8.0)           # a weight of zero
+    want, tol = _scores(c, np.zeros((len(lens), 8, max(lens)), np.float32))
+    got = saw.paged_attn_weights(c.cache, *c.args, max_seq_len=max(lens))
+    pc.check(got[0, :, :lens[0]], want[0, :, :lens[0]], tol[0, :, :lens[0]])
+
+
 @pytest.mark.parametrize("n,lens,G", [([1, 1], [5000, 9000], 4), ([1], [20000], 8), ([2, 33], [7000, 3001], 2), ([1] * 40, list(range(100, 1300, 30)), 4)], ids=str)
 def test_long_contexts_split(saw, n, lens, G):
     c = Case(saw, n, lens, G=G, seed=2)
