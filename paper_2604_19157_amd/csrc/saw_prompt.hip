@@ -726,7 +726,8 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     }
     const float down_v = values.down();
     // logits: s_j (q . (c_j - 8) - (z_j - 8) sum q), with the codes exact and each pair from shared memory where its key stands
-    pairs[wave][lane] = t * kTileKeys + lane < len ? f32x2{kpair.x, 8.f - kpair.y} : f32x2{0.f, 0.f};
+    // (a key that is no number has no logit: its sum of codes would hide that)
+    pairs[wave][lane] = t * kTileKeys + lane < len ? f32x2{largest_value(kpair) < INFINITY ? kpair.x : NAN, 8.f - kpair.y} : f32x2{0.f, 0.f};
     f32x16 x[2];
     u32x4 pf[4];
     wave_sync();

@@ -372,6 +372,24 @@ def test_values_that_are_no_numbers_show_where_they_are_seen(saw, n, lens, d, G,
         pc.check_odd(got, want, tol, values, c.cu, pc.offsets(lens), True, G, count)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("n,lens", [([3, 1], [50, 900]), ([40, 150], [50, 160]), ([1], [6000])], ids=str)
+@pytest.mark.parametrize("pair", [(np.inf, 8.0), (-np.inf, 3.0), (np.nan, 8.0), (0.1, np.inf)], ids=str)
+def test_keys_that_are_no_numbers_show_where_they_are_seen(saw, pair, n, lens, dtype):
+    """A key of infinities of both signs, as queries of both signs meet them, has no logit: the rows that see it are NaN, the others what they were."""
+    c = Case(saw, n, lens, dtype=dtype, seed=19)
+    want, tol = c.attention()
+    for back in (1, n[0] // 2 + 1):
+        at = lens[0] - back                           # seen by the last `back` queries of the first sequence
+        keep = c.cache.k_meta.clone()
+        c.cache.k_meta[c.pt[0, at // 16], :, at % 16] = torch.tensor(pair, device="cuda")
+        got = saw.paged_prompt_attn(c.cache, *c.args)
+        c.cache.k_meta.copy_(keep)
+        assert bool(torch.isnan(got[n[0] - back:n[0]]).all())
+        pc.check(got[:n[0] - back], want[:n[0] - back], tol[:n[0] - back])
+        pc.check(got[n[0]:], want[n[0]:], tol[n[0]:])
+
+
 @pytest.mark.parametrize("n", [3, 80])
 @pytest.mark.parametrize("size", [1.0, 1e-30])
 def test_queries_of_zeros(saw, n, size):
