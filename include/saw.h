@@ -409,8 +409,9 @@ int saw_prompt_attn(const void* q, const void* k, const void* v, int32_t dtype, 
  *   out         device, dense [T][n_q_heads][head_dim] of dtype, 16-byte aligned; rows of no sequence are left as they were.
  *   workspace   at least saw_paged_prompt_workspace_bytes(...) bytes, 16-byte aligned, one per call in flight: partial
  *               records where keys are split, which calls of few rows need more of than large ones, and the rows of a learned rotation.
- * Rotated queries and dequantised keys enter their product as fp16 times powers of two (a query's of its row, keys' of the
- * sequence), weights and dequantised values theirs as fp16 too: half a step each, 2^-11, at least 2^-32 of the row's largest weight and
+ * Rotated queries enter their product as fp16 times a power of two of their row, dequantised keys as fp16 times one of the sequence where
+ * outputs are bf16; with fp16 outputs keys are exact, and queries of calls with few rows a sequence two fp16 limbs.  Weights and
+ * dequantised values enter theirs as fp16 too: half a step each, 2^-11, at least 2^-32 of the row's largest weight and
  * 2^-19 of the largest value that a row meets, whatever the size of those that it does not see; everything between and all sums are
  * fp32.  What is no number shows as above, values in the space that they are stored in.  Page ids of visible tokens outside [0, num_pages)
  * are read as page 0.  Alignment of the pools as for the decode calls.  T == 0 is a no-op.

@@ -7,7 +7,9 @@
 
 namespace saw {
 
-enum { kKvBf16, kKvF16, kKvInt4 };
+// kKvCodes: the INT4 pages, keys as exact codes and their scales on the logits.
+enum { kKvBf16, kKvF16, kKvInt4, kKvCodes };
+constexpr bool int4_pages(int kv) { return kv >= kKvInt4; }
 
 // Channels of one vector that a lane holds: lane, lane + 64.  page: of position j, INT4 (eight positions from a multiple of eight on share theirs).
 template <int D, int KV>
@@ -15,13 +17,13 @@ struct RowSource {
   const PromptParams& p;
   int b, h, k0, lane;
   __device__ int page_of(int j) const {
-    if constexpr (KV != kKvInt4) return 0;
+    if constexpr (!int4_pages(KV)) return 0;
     const int page = p.page_table[(int64_t)b * p.max_pages + (j >> 4)];
     return page < 0 || page >= p.num_pages ? 0 : page;
   }
   __device__ f32x2 value_pair_of(int page, int j) const { return *(const f32x2*)(p.v_meta + 2 * (((int64_t)page * p.n_kv_heads + h) * 16 + (j & 15))); }
   __device__ void load(bool value, int page, int j, float (&x)[D / 64]) const {
-    if constexpr (KV == kKvInt4) {
+    if constexpr (int4_pages(KV)) {
       const int64_t vec = ((int64_t)page * p.n_kv_heads + h) * 16 + (j & 15);
       const float* const m = (value ? p.v_meta : p.k_meta) + 2 * vec;
       const uint8_t* const c = (value ? p.v_codes : p.k_codes) + vec * (D / 2);
@@ -104,14 +106,33 @@ __device__ __forceinline__ u32x4 widen_codes(uint32_t w, float s, float sz) {
   x.w = M::pack(fmaf((float)(even >> 24), s, -sz), fmaf((float)(odd >> 24), s, -sz));
   return x;
 }
-// ... of 32 codes to four places of a row
-template <typename M, int D, bool VALUE>
+// ... of 32 codes to four places of a row; EXACT: the codes as they are, minus 8
+template <typename M, int D, bool VALUE, bool EXACT = false>
 __device__ __forceinline__ void put_piece(char* tile, int row, int piece, u32x4 w, float s, float sz) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int chunk = 4 * piece + i;
-    *(u32x4*)(tile + row * (2 * D) + 16 * (VALUE ? v_place<D>(row, chunk) : k_place<D>(row, chunk))) = widen_codes<M>(w[i], s, sz);
+    *(u32x4*)(tile + row * (2 * D) + 16 * (VALUE ? v_place<D>(row, chunk) : k_place<D>(row, chunk))) = EXACT ? centred(w[i], CodeBits()) : widen_codes<M>(w[i], s, sz);
   }
+}
+// Products of a row's query and codes minus 8 become logits, s_j (q . (c_j - 8) - (z_j - 8) sum q); pairs: code_pair of the tile's keys.
+__device__ __forceinline__ void code_logits(f32x16& x, const f32x2* pairs, int kb, float sum_q, int lane) {
+#pragma unroll
+  for (int r = 0; r < 16; r += 2) {
+    const f32x4 two = *(const f32x4*)&pairs[32 * kb + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 2)];
+    x[r] = fmaf(two.y, sum_q, x[r]) * two.x;
+    x[r + 1] = fmaf(two.w, sum_q, x[r + 1]) * two.z;
+  }
+}
+// Sum of a row's channels as they are multiplied.
+template <int D>
+__device__ __forceinline__ float channel_sum(const u32x4 (&qf)[D / 16]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += f16_to_f32(qf[ks][i] & 0xffffu) + f16_to_f32(qf[ks][i] >> 16);
+  return add_xor32(sum);
 }
 
 // The largest that a token's values can be, from its pair alone; infinity if that is no number.
@@ -119,6 +140,9 @@ __device__ __forceinline__ float largest_value(f32x2 pair) {
   const float sz = pair.x * pair.y, most = fmaxf(fabsf(sz), fabsf(fmaf(15.f, pair.x, -sz)));
   return most < INFINITY ? most : INFINITY;
 }
+// What code_logits needs of a key's pair.  (A key that is no number has no logit: its sum of codes would hide that.)
+__device__ __forceinline__ f32x2 code_pair(f32x2 pair) { return f32x2{largest_value(pair) < INFINITY ? pair.x : NAN, 8.f - pair.y}; }
+
 // Sums of values with a larger unit are looked at once more when they have it: below it fp32 holds 2^15 (tile_weights) times 2^15 times 2^31 tokens.
 constexpr float kLargeUnit = 0x1p60f;
 
@@ -194,15 +218,15 @@ __device__ __forceinline__ void rescale(RowState<D>& st, float by) {
 // The queries of a lane column as B operand: channels of k-step ks, half h and place i have bits (ks, h, i), h at bit HALF_BIT.  Those for
 // the INT4 pages are rotated here, in registers, and become fp16 times 2^-e (prompt_query_kernel does the same for a learned rotation);
 // returns what turns a logit into log2 units.  CODES: the eight channels of a word of codes in the order of `centred`.
-template <int D, int KV, int HALF_BIT, bool CODES = false>
-__device__ __forceinline__ float row_query(const PromptParams& p, int64_t token, int head, int lane, u32x4 (&qf)[D / 16]) {
+template <int D, int KV, int HALF_BIT, bool CODES = false, typename F>
+__device__ __forceinline__ float row_query(const PromptParams& p, int64_t token, int head, int lane, u32x4 (&qf)[D / 16], F second) {
   const int half = lane >> 5;
-  const bool ready = KV == kKvInt4 && p.dense_k;
+  const bool ready = int4_pages(KV) && p.dense_k;
   const int64_t at = token * p.n_q_heads + head;
   const uint16_t* const src = ready ? p.query + at * D : (const uint16_t*)p.q + token * p.q_stride + (int64_t)head * D;
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const u32x4*)(src + (spread_channel<HALF_BIT>(8 * ks) | half << HALF_BIT));
-  if constexpr (KV == kKvInt4) {
+  if constexpr (int4_pages(KV)) {
     if (ready) {
       if (CODES)
 #pragma unroll
@@ -210,6 +234,8 @@ __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token,
           const u32x4 w = qf[ks];
           qf[ks] = u32x4{(w.x & 0xffffu) | w.z << 16, w.x >> 16 | (w.z & 0xffff0000u), (w.y & 0xffffu) | w.w << 16, w.y >> 16 | (w.w & 0xffff0000u)};
         }
+#pragma unroll
+      for (int i = 0; i < D / 4; ++i) second(i / 4, i % 4, f16_to_f32(qf[i / 4][i % 4] & 0xffffu), f16_to_f32(qf[i / 4][i % 4] >> 16));
       return fmaxf(p.scale * p.query_scale[at], kLeastScale);
     }
     float x[D / 2];
@@ -237,7 +263,11 @@ __device__ __forceinline__ float row_query(const PromptParams& p, int64_t token,
     for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        qf[ks][i] = CODES ? MathF16::pack(x[8 * ks + i] * down, x[8 * ks + i + 4] * down) : MathF16::pack(x[8 * ks + 2 * i] * down, x[8 * ks + 2 * i + 1] * down);
+{
+        const float a = x[8 * ks + (CODES ? i : 2 * i)] * down, b = x[8 * ks + (CODES ? i + 4 : 2 * i + 1)] * down;
+        qf[ks][i] = MathF16::pack(a, b);
+        second(ks, i, a, b);
+      }
     return fmaxf(p.scale * __uint_as_float((uint32_t)(127 + ex) << 23), kLeastScale);
   }
   return p.scale;
@@ -274,7 +304,7 @@ __device__ __forceinline__ void first_odd_values(const RowSource<D, KV>& src, in
         if (v[u][e] == -INFINITY) first[2][e] = min(first[2][e], at);
         none = none && !(fabsf(v[u][e]) < INFINITY);
       }
-      if constexpr (KV == kKvInt4)
+      if constexpr (int4_pages(KV))
         if (!none && largest_value(src.value_pair_of(page, at)) == INFINITY) mixed = min(mixed, at);
     }
   }
@@ -339,7 +369,7 @@ template <int D, int KV, int HALF_BIT, bool CODES = false>
 __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile& rt, int w0, int last, int row, int h, int64_t token, int head,
                                             int k0, int len, int t0, int t1, int sees, int wend, bool odd, bool lost, const u32x4 (&qf)[D / 16], float scale,
                                             RowState<D>& st, int lane) {
-  constexpr bool kInt4 = KV == kKvInt4;
+  constexpr bool kInt4 = int4_pages(KV);
   const int shift = __builtin_ctz(p.group);
   float sum = add_xor32(st.sum);
   const int64_t at = token * p.n_q_heads + head;
@@ -483,19 +513,22 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
 // one barrier a tile.  Keys and values of 16 bits come from memory straight into the buffer (each transfer has a whole tile's
 // products to arrive in).  Those of the INT4 pages are requested a tile ahead into registers and written behind the tile's products:
 // as fp16 times powers of two (Unit), each once per block and not once per row.
-//   Roundings: weights to the type of the values, whose half step the output has anyway; over the pages query, keys, weights and
-// values to fp16 (an output is off by 1.4e-3 in fp16 and 2.0e-3 in bf16, 1.6e-3 of it bf16's own, where keys have channels 20
-// times as large as others; two limbs of the query as in saw_weights.hip would be half as much matrix work again).
+//   Roundings: weights to the type of the values, whose half step the output has anyway; over the pages queries, weights and values to
+// fp16, and keys too where outputs are bf16 (off by 2.0e-3 with four channels of the keys 20 times as large as the others, 1.6e-3 of it bf16's
+// own).  With fp16 outputs keys stay exact codes and their scales and zero-points meet the logits (kKvCodes): 5.3e-4 instead of 1.2e-3, of which
+// fp16's own is 2.1e-4, for 32 multiplications and 32 additions a tile more (2048 tokens over 16384 755 us instead of 714, ragged chunks of 64
+// channels 176 and 162).  Two limbs of the query as in saw_weights.hip would be half as much matrix work again.
 //   Bound by the matrix cores at the clock that they leave, with the exponentials behind them: 8192 causal tokens, 32 query and 8 kv heads
 // of 128 channels, 515 us, 1.07 PFLOP/s (a library product of 8192^3 1.27); 64 channels, where a logit has half the products, 0.87; 2048
 // tokens over 16384 in the pages 700 us, 0.83, with 200 M instructions of the vector ALU, 0.3 of them for the codes.
 template <int D, int KV, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
+__global__ __launch_bounds__(64 * NW, D == 64 && KV == kKvCodes ? 3 : 2) void prompt_kernel(PromptParams p) {
   constexpr int R = 32 * NW, kRow = 2 * D, kTile = kTileKeys * kRow, kInstr = kTile / 1024, kRpi = 1024 / kRow;
-  constexpr bool kInt4 = KV == kKvInt4;
+  constexpr bool kInt4 = int4_pages(KV), kCodes = KV == kKvCodes;
   using M1 = typename std::conditional<KV == kKvBf16, MathBf16, MathF16>::type;      // queries and keys, weights and values
   using M2 = M1;
   __shared__ __attribute__((aligned(1024))) char lds[2][2][kTile];       // [buffer][K, V]
+  __shared__ __attribute__((aligned(16))) f32x2 pairs[kCodes ? 2 : 1][kCodes ? kTileKeys : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % p.n_kv_heads;
   // (the last tiles of a causal sequence have the most keys and start first)
@@ -518,17 +551,21 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
   const int64_t token = rt.begin + (min(row, last) >> shift);
   const int head = h * p.group + (row & (p.group - 1));
   u32x4 qf[D / 16];
-  const float scale = row_query<D, KV, 3>(p, token, head, lane, qf);
+  const float scale = row_query<D, KV, 3, kCodes>(p, token, head, lane, qf, [](int, int, float, float) {});
   RowState<D> st;
   clear(st);
 
   bool odd = false;                                                       // (INT4) values that are no numbers were met
   Unit keys, values;
+  const float sum_q = kCodes ? channel_sum<D>(qf) : 0.f;
   auto products = [&](int buf, int t, float tile_scale) {
     if (t * kTileKeys >= wend) return;
     f32x16 s[2];
     u32x4 pf[4];
     tile_logits<D, M1>(lds[buf][0], qf, s, lane);
+    if constexpr (kCodes)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) code_logits(s[kb], pairs[buf], kb, sum_q, lane);
     if ((t + 1) * kTileKeys > wfull) tile_mask(s, sees - t * kTileKeys, lane);
     tile_weights<D, M2>(s, tile_scale, st, pf);
     tile_values<D, M2>(lds[buf][1], pf, st, lane);
@@ -580,7 +617,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
       const bool whole = (t + 1) * kTileKeys <= seen, mine = t * kTileKeys + lane < seen;
       const float key = largest_value(c.key_pair), value = largest_value(c.value_pair);
       int by;
-      keys.fit(key, t == t0, whole, by, [&] { return mine ? key : 0.f; });
+      if constexpr (!kCodes) keys.fit(key, t == t0, whole, by, [&] { return mine ? key : 0.f; });
+      else if (wave == 0) pairs[buf][lane] = code_pair(c.key_pair);
       if (values.passed(value, t == t0)) {
         if (__any(value == INFINITY)) {
           odd = true;
@@ -596,9 +634,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
         const int piece = j * threads + threadIdx.x, value = piece >= Pieces::kPieces / 2, i = value ? piece - Pieces::kPieces / 2 : piece;
         const float s = c.pair[j].x, sz = s * c.pair[j].y;
         if (value) put_piece<M2, D, true>(lds[buf][1], i / (D / 32), i % (D / 32), c.codes[j], s * down_v, sz * down_v);
-        else put_piece<M1, D, false>(lds[buf][0], i / (D / 32), i % (D / 32), c.codes[j], s * down, sz * down);
+        else put_piece<M1, D, false, kCodes>(lds[buf][0], i / (D / 32), i % (D / 32), c.codes[j], s * down, sz * down);
       }
-      return keys.up();
+      return kCodes ? 1.f : keys.up();
     };
     Pieces c;
     float tile_scale = 1.f;
@@ -621,7 +659,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
     rescale<D>(st, values.up());
     if (values.up() > kLargeUnit) odd = odd || __any(row <= last && no_sum<D>(st));
   }
-  finish_rows<D, KV, 3>(p, rt, w0, last, row, h, token, head, k0, len, t0, t1, sees, wend, odd, keys.lost || values.lost, qf, scale, st, lane);
+  finish_rows<D, KV, 3, kCodes>(p, rt, w0, last, row, h, token, head, k0, len, t0, t1, sees, wend, odd, keys.lost || values.lost, qf, scale, st, lane);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
@@ -633,11 +671,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptParams p) {
 // the transposing reads.
 //   Bound by the vector ALU, 1200 instructions for 64 keys, half of them for the codes: 32 sequences of 5 tokens over 512 to 4096, 88 MB, 49
 // us and 6.7 for the merge.
-template <int D>
+//   LIMBS, for fp16 outputs: the query is two limbs, the second read from shared memory for every 32 keys (but for a learned rotation's, which come as
+// one): off by 3.2e-4 instead of 5.2e-4, 32 x 5 tokens 57 us instead of 53.3.  bf16's own half step hides that: 1.7e-3 either way.
+template <int D, bool LIMBS>
 __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   constexpr int NW = 4, kRow = 2 * D, kTile = kTileKeys * kRow, kHalfBit = D == 128 ? 6 : 5, kWords = D / 16, kPieces = D / 32;
   static_assert(kTile == 64 * (D / 2) * 4, "a state fits the wavefront's tile");
   __shared__ __attribute__((aligned(1024))) char lds[NW][kTile];
+  __shared__ u32x4 limbs[LIMBS ? D / 16 : 1][64];
   __shared__ float2 join[NW][64];
   __shared__ __attribute__((aligned(16))) f32x2 pairs[NW][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -664,7 +705,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
   u32x4 kc[2][kWords / 4], vc[kPieces];
   f32x2 kpair, vpair[kPieces];                                            // (of key `lane`; of the pieces' tokens)
   TilePages ids;
-  auto request = [&] {
+  auto request = [&]() __attribute__((always_inline)) {
     ids.ready(p, h);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -689,13 +730,16 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     ids.fetch(pages, t0 + wave + NW, len);
   }
   u32x4 qf[D / 16];
-  const float scale = row_query<D, kKvInt4, kHalfBit, true>(p, token, head, lane, qf);
-  float sum_q = 0.f;                                                      // of the row's channels as they are multiplied
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sum_q += f16_to_f32(qf[ks][i] & 0xffffu) + f16_to_f32(qf[ks][i] >> 16);
-  sum_q = add_xor32(sum_q);
+  float sum_lo = 0.f;
+  const float scale = row_query<D, kKvInt4, kHalfBit, true>(p, token, head, lane, qf, [&](int ks, int i, float a, float b) {
+    if constexpr (LIMBS) {
+      const uint32_t lo = MathF16::pack(a - f16_to_f32(qf[ks][i] & 0xffffu), b - f16_to_f32(qf[ks][i] >> 16));
+      sum_lo += f16_to_f32(lo & 0xffffu) + f16_to_f32(lo >> 16);
+      if (ks % NW == wave) limbs[ks][lane][i] = lo;
+    }
+  });
+  const float sum_q = channel_sum<D>(qf) + add_xor32(sum_lo);
+  if (LIMBS) lds_barrier();
   const CodeBits bits;
   RowState<D> st;
   clear(st);
@@ -726,8 +770,7 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     }
     const float down_v = values.down();
     // logits: s_j (q . (c_j - 8) - (z_j - 8) sum q), with the codes exact and each pair from shared memory where its key stands
-    // (a key that is no number has no logit: its sum of codes would hide that)
-    pairs[wave][lane] = t * kTileKeys + lane < len ? f32x2{largest_value(kpair) < INFINITY ? kpair.x : NAN, 8.f - kpair.y} : f32x2{0.f, 0.f};
+    pairs[wave][lane] = t * kTileKeys + lane < len ? code_pair(kpair) : f32x2{0.f, 0.f};
     f32x16 x[2];
     u32x4 pf[4];
     wave_sync();
@@ -735,14 +778,14 @@ __global__ __launch_bounds__(256, 2) void few_rows_kernel(PromptParams p) {
     for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[kb][r] = 0.f;
+      if (LIMBS) asm volatile("" ::: "memory");                              // (or the limbs would be kept in registers after all)
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) x[kb] = MathF16::mfma(centred(kc[kb][ks / 4][ks % 4], bits), qf[ks], x[kb]);
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const f32x4 two = *(const f32x4*)&pairs[wave][32 * kb + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 2)];
-        x[kb][r] = fmaf(two.y, sum_q, x[kb][r]) * two.x;
-        x[kb][r + 1] = fmaf(two.w, sum_q, x[kb][r + 1]) * two.z;
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const u32x4 k = centred(kc[kb][ks / 4][ks % 4], bits);
+        if constexpr (LIMBS) x[kb] = MathF16::mfma(k, limbs[ks][lane], x[kb]);
+        x[kb] = MathF16::mfma(k, qf[ks], x[kb]);
       }
+      code_logits(x[kb], pairs[wave], kb, sum_q, lane);
       // (128 channels: or the compiler puts this off until the values are written, with all pairs in registers, and spills: 54 us become 87.  With
       // 64 they fit: 36 us put off, 38 in place.)
       if (D == 128) asm volatile("" : "+v"(x[kb]));
@@ -925,11 +968,20 @@ static void launch_rows(const PromptParams& p, const PromptPlan& plan, hipStream
       if (turn_many(p)) prompt_query_kernel<D, kTurnedAtOnce><<<row_grid(rows, kTurnedAtOnce), block, 0, st>>>(p);
       else prompt_query_kernel<D, 1><<<row_grid(rows, 1), block, 0, st>>>(p);
     }
-  if (plan.rows == 128) prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
+  if (plan.rows == 128) {
+    if (KV == kKvInt4 && p.dtype == SAW_F16) prompt_kernel<D, KV == kKvInt4 ? kKvCodes : KV, 4><<<grid, block, 0, st>>>(p);
+    else prompt_kernel<D, KV, 4><<<grid, block, 0, st>>>(p);
+  }
   if constexpr (KV == kKvInt4)
-    if (plan.rows == 32) few_rows_kernel<D><<<grid, block, 0, st>>>(p);
+    if (plan.rows == 32) {
+      if (p.dtype == SAW_F16) few_rows_kernel<D, true><<<grid, block, 0, st>>>(p);
+      else few_rows_kernel<D, false><<<grid, block, 0, st>>>(p);
+    }
   if constexpr (D == 128 || KV != kKvInt4)
-    if (plan.rows == 256) prompt_kernel<D, KV, 8><<<grid, dim3(512), 0, st>>>(p);
+    if (plan.rows == 256) {
+      if (KV == kKvInt4 && p.dtype == SAW_F16) prompt_kernel<D, KV == kKvInt4 ? kKvCodes : KV, 8><<<grid, dim3(512), 0, st>>>(p);
+      else prompt_kernel<D, KV, 8><<<grid, dim3(512), 0, st>>>(p);
+    }
   if constexpr (KV == kKvInt4 && D == kDenseD)
     if (p.dense_v && turn_many(p)) {
       prompt_merge_kernel<D, true, kTurnedAtOnce><<<row_grid(rows, kTurnedAtOnce), block, 0, st>>>(p, plan.splits);

@@ -120,6 +120,35 @@ def test_attention_over_ordinary_codes(saw, d, h, dtype, n, lens):
     assert off < pc.U[dtype] + 1.5 * 2.0 ** -11 * max(1.0, np.abs(want).max() / np.abs(want).mean()) ** 0.5
 
 
+def _half(x):
+    """x as fp16 times a power of two for each row of the last axis: no number is subnormal that is not far below the largest."""
+    top = np.abs(x).max(-1, keepdims=True)
+    unit = 2.0 ** np.floor(np.log2(np.where(top > 0, top, 1)) - 14)
+    return (x / unit).astype(np.float16).astype(np.float64) * unit
+
+
+@pytest.mark.parametrize("d,h", [(128, 128), (64, 16), (128, 1)])
+@pytest.mark.parametrize("n,lens,limbs", [([1, 5], [200, 333], True), ([150], [400], False), ([1], [3000], True)], ids=str)
+def test_fp16_outputs_are_off_by_the_roundings_that_they_are_said_to_have(saw, n, lens, limbs, d, h):
+    """Logits of a standard deviation of several units: no more than weights and values, and the queries of long chunks, as fp16 give in 64 bits.  (Norms of thousands of numbers, which vary by a few hundredths; 1.25 is not reached by chance.)"""
+    c = Case(saw, n, lens, d=d, h=h, dtype=FP, seed=31, offsets=False)
+    c.q.mul_(3)
+    c.args[0].mul_(3)
+    want, stated = np.zeros(c.q.shape), np.zeros(c.q.shape)
+    for b, L in enumerate(lens):
+        rows = slice(c.cu[b], c.cu[b + 1])
+        q = O.rotate(c.q[rows].double().numpy(), h)
+        k, v = (O._gather(c.ref, x, c.pt[b], 0, L) for x in "kv")
+        for j in range(c.q.shape[1]):
+            for out, qj, vj, half in ((want, q[:, j], v[:, j // 4], False), (stated, q[:, j] if limbs else _half(q[:, j]), _half(v[:, j // 4].ravel()).reshape(L, d), True)):
+                w = pc.weights64(qj, k[:, j // 4], pc.visible(n[b], L), d ** -0.5)[0]
+                o = O.unrotate((_half(w) if half else w) @ vj, h)
+                out[rows, j] = o.astype(np.float16) if half else o
+    got = saw.paged_prompt_attn(c.cache, *c.args).double().cpu().numpy()
+    off, said = (np.linalg.norm(x - want) / np.linalg.norm(want) for x in (got, stated))
+    assert off < 1.25 * said, (off, said)
+
+
 OPTIONS = [dict(h=1), dict(h=16), dict(h=32, mask=1), dict(h=64, mask=2), dict(h=128, signs=True), dict(h=128, dense=True),
            dict(h=1, dense=True), dict(h=64, dense=True, signs=True, mask=1), dict(d=64, h=16), dict(d=64, h=64, signs=True), dict(d=64, h=1)]
 
