@@ -258,6 +258,41 @@ def test_the_size_of_tokens_that_are_not_seen_counts_for_nothing(saw, n, lens, s
         pool.copy_(keep)
 
 
+@pytest.mark.parametrize("size", [1e-30, 1e4, 1e30])
+@pytest.mark.parametrize("d,h", [(128, 1), (128, 128), (64, 16)])
+@pytest.mark.parametrize("n,lens", [([40, 3], [330, 21]), ([5, 3], [330, 700]), ([300], [300])], ids=str)
+def test_the_size_of_tokens_that_are_not_seen_counts_for_nothing_in_fp16(saw, n, lens, d, h, size):
+    c = Case(saw, n, lens, d=d, h=h, dtype=FP, signs=h > 1)
+    want, tol = c.attention()
+    first = int(c.cu[1]) // 2
+    at = lens[0] - n[0] + first
+    for pool in (c.cache.k_meta, c.cache.v_meta):
+        keep = pool.clone()
+        pool[c.pt[0, at // 16], :, at % 16, 0] = size
+        got = saw.paged_prompt_attn(c.cache, *c.args)
+        pc.check(got[:first], want[:first], tol[:first])
+        pc.check(got[n[0]:], want[n[0]:], tol[n[0]:])
+        pool.copy_(keep)
+
+
+@pytest.mark.parametrize("n,lens", [([3], [50]), ([40], [330]), ([1], [5000])], ids=str)
+def test_tokens_that_are_numbers_in_some_channels(saw, n, lens):
+    """Codes far from the zero-point overflow fp32 and are infinite, those beside it are large numbers (bf16 has the exponents for both)."""
+    c = Case(saw, n, lens, h=1, seed=23)
+    at = lens[0] - n[0]                               # seen by every query
+    for ref in (c.ref["v_meta"], c.cache.v_meta):
+        ref[c.pt[0, at // 16], :, at % 16] = torch.tensor([1e38, 8.0]) if ref is c.cache.v_meta else (1e38, 8.0)
+    with np.errstate(over="ignore"):
+        v = O._gather(c.ref, "v", c.pt[0], 0, lens[0]).astype(np.float32).astype(np.float64)
+    want, tol = np.zeros(c.q.shape), np.zeros(c.q.shape)
+    rest = np.where(np.isfinite(v), v, 0)
+    for b, rows, g, j, w, top, big in c.weights():
+        want[rows, j] = w @ rest[:, g]
+        # (half a step of the output, of the query and of nothing else: these rows are worked out in fp32)
+        tol[rows, j] = pc.bound(want[rows, j], w @ np.abs(rest[:, g]), top, big, lens[0], c.d, pc.U[BF], 2.0 ** -10, 2.0 ** -10 + 2.0 ** -18)
+    pc.check_odd(saw.paged_prompt_attn(c.cache, *c.args), want, tol, v, c.cu, pc.offsets(lens), True, c.G)
+
+
 def test_page_ids_out_of_range_read_page_0(saw):
     c = Case(saw, [20], [60])
     pt = c.args[2].clone()
