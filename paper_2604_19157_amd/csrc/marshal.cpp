@@ -290,7 +290,8 @@ PyObject* kv16_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (weak: beside a library that lacks these entry points the module still loads and serves the calls above)
+// (weak: beside a library that lacks these entry points - one that stands in for the hot calls alone, in a test - the module still loads and serves
+// the calls above)
 #pragma weak saw_prompt_attn
 #pragma weak saw_paged_prompt_attn
 #pragma weak saw_paged_attn_weights

@@ -369,7 +369,7 @@ __global__ __launch_bounds__(1024, 8) void evict_write_kernel(EvictParams p, Seg
 
 // The kept tokens' codes and pairs, a thread for 16 bytes of K and of V of four tokens: where a token lies takes three loads one after the
 // other, so that four of these chains have to be under way at once.  Bound by the memory: reads of 64 bytes at a time, writes of whole
-// tiles (48 sequences, 2048 tokens kept, 226 MB: 47 us, 4.8 TB/s; a copy reaches 5.05).
+// tiles (48 sequences, 2048 tokens kept, 226 MB: 54 to 61 us where no cache holds them, 4.2 TB/s at best; a copy reaches 5.05).
 template <int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams p) {
   constexpr int LPV = D / 32, kEach = 4, kStep = 256 / LPV;      // 16-byte pieces of a vector's codes; tokens of a thread; tokens at once

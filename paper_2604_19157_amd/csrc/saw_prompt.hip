@@ -517,10 +517,10 @@ __device__ __forceinline__ void finish_rows(const PromptParams& p, const RowTile
 // fp16, and keys too where outputs are bf16 (off by 2.0e-3 with four channels of the keys 20 times as large as the others, 1.6e-3 of it bf16's
 // own).  With fp16 outputs keys stay exact codes and their scales and zero-points meet the logits (kKvCodes): 5.3e-4 instead of 1.2e-3, of which
 // fp16's own is 2.1e-4, for 32 multiplications and 32 additions a tile more (2048 tokens over 16384 755 us instead of 714, ragged chunks of 64
-// channels 176 and 162).  Two limbs of the query as in saw_weights.hip would be half as much matrix work again.
+// channels 176 and 162).  Two limbs of the query as in saw_weights.hip are half as much matrix work again: those chunks 208 us for 3.3e-4.
 //   Bound by the matrix cores at the clock that they leave, with the exponentials behind them: 8192 causal tokens, 32 query and 8 kv heads
-// of 128 channels, 515 us, 1.07 PFLOP/s (a library product of 8192^3 1.27); 64 channels, where a logit has half the products, 0.87; 2048
-// tokens over 16384 in the pages 700 us, 0.83, with 200 M instructions of the vector ALU, 0.3 of them for the codes.
+// of 128 channels, 508 to 529 us from card to card, 1.04 to 1.08 PFLOP/s (a library product of 8192^3 1.27); 64 channels, where a logit has half the
+// products, 0.86; 2048 tokens over 16384 in the pages 709 to 725 us, 0.81 to 0.82, with 200 M instructions of the vector ALU, 0.3 of them for the codes.
 template <int D, int KV, int NW>
 __global__ __launch_bounds__(64 * NW, D == 64 && KV == kKvCodes ? 3 : 2) void prompt_kernel(PromptParams p) {
   constexpr int R = 32 * NW, kRow = 2 * D, kTile = kTileKeys * kRow, kInstr = kTile / 1024, kRpi = 1024 / kRow;
@@ -669,8 +669,9 @@ __global__ __launch_bounds__(64 * NW, D == 64 && KV == kKvCodes ? 3 : 2) void pr
 // the logits, as in saw_weights.hip: half of the instructions of dequantised keys (16 tokens a sequence 79 -> 74 us); with 128 rows a
 // block, where codes are widened once for all, it would be more of them.  Values go through 64 rows of shared memory of the wavefront's own for
 // the transposing reads.
-//   Bound by the vector ALU, 1200 instructions for 64 keys, half of them for the codes: 32 sequences of 5 tokens over 512 to 4096, 88 MB, 49
-// us and 6.7 for the merge.
+//   Bound by the vector ALU, 1200 instructions for 64 keys, half of them for the codes, by the conflicts of the values' writes (0.57 of the cycles
+// that shared memory is addressed in) and by the longest sequences, whose blocks start with all the others: 32 sequences of 5 tokens over 512
+// to 4096, 88 MB, 50 us and 6.6 for the merge.
 //   LIMBS, for fp16 outputs: the query is two limbs, the second read from shared memory for every 32 keys (but for a learned rotation's, which come as
 // one): off by 3.2e-4 instead of 5.2e-4, 32 x 5 tokens 57 us instead of 53.3.  bf16's own half step hides that: 1.7e-3 either way.
 template <int D, bool LIMBS>
@@ -919,13 +920,13 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p, int s
 //     tokens, 32 query / 8 kv heads: 5 new tokens 54 us, 181 in blocks of 128 rows); at most 192 with 128 to 384 (sequence, kv head) pairs, where
 //     blocks of 128 rows are too few to be dealt out evenly (blocks of 32 and of 128 rows: 24 tokens, 16 sequences 70 us and 69, 24 94 and 106,
 //     32 113 and 126, 48 171 and 182; 32 x 48 160 and 171; 31 x 1 and one chunk of 700 104 and 165; but 8 x 24 51 and 43, 64 x 24 206 and 185,
-//     32 x 64 199 and 190);
+//     32 x 64 199 and 190; fp16, 24 tokens, 16 sequences 80 and 73, 24 104 and 111, 32 126 and 133, 48 188 and 193, 32 of 64 channels 76 and 96);
 //   * 4096 rows a sequence and more, and a block for every compute unit: 256 rows, eight wavefronts, so that keys are brought in (and
 //     codes widened) half as often (8192 causal tokens 520 us, 544 in blocks of 128; 2048 tokens over 16384 in the pages 708 and 777; but 19
 //     packed prompts of 60 to 1437 tokens 181 and 178, four short ones 13.2 and 11.2);
 //   * 128 rows otherwise.
 // Keys are split while a call has fewer blocks than the chip holds, two for a compute unit (a little more in blocks of 32 rows, whose
-// wavefronts go their own ways: two splits of 256 blocks 54 us, one 80, three 58), into parts of 256 keys at least.  Blocks are counted as those of
+// wavefronts go their own ways: two splits of 256 blocks 54 us, one 80, three 58; of 264 to 280 of uneven length 62, one 66 to 71), into parts of 256 keys at least.  Blocks are counted as those of
 // sequences of like length: the grid has one more for each sequence, of which many are empty (with those counted too, 8 x 24 tokens 56 us instead
 // of 43, 4 x 256 137 instead of 115).  A split where the chip is full already costs its records: two sequences of 2000 tokens, 512 blocks, 88 us,
 // in two splits 161.

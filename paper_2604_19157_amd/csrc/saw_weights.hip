@@ -429,7 +429,7 @@ __global__ __launch_bounds__(256) void weight_join_kernel(PromptParams p, int64_
 // a (sequence, kv head), reads its keys once and keeps the logits in shared memory while they fit; longer ones are worked out again.
 // Sequences of more rows take a row tile after the other, the later ones on top of what the earlier wrote.  What bounds it is how many
 // wavefronts a SIMD has to cover one another's waits: four of them, 128 registers each, which is why a step works on 16 keys at a time
-// (64 sequences of 512 to 4096 tokens, 95 MB, 49 us; two passes 132).
+// (64 sequences of 512 to 4096 tokens, 95 MB, 52 us; two passes 132).
 constexpr int kKeptLogits = 16384, kStepWaves = 8;
 
 template <int D>
