@@ -434,7 +434,8 @@ int saw_paged_prompt_attn(const saw_cache_t* cache, const void* q, int32_t dtype
  *   score_stride  floats between rows, at least max_seq_len (its value where <= 0 stands for it).
  *   workspace   at least saw_attn_weights_workspace_bytes(...) bytes, 16-byte aligned.
  * All in fp32 (queries as two fp16 limbs, 2^-22 of a row's largest channel); the sums have a fixed order.  A query that sees
- * nothing adds nothing.  T == 0 leaves prev + 0.  T n_q_heads / n_kv_heads + 16 B up to 2^24 - 2^9.
+ * nothing adds nothing.  Logits are scale (q~ . code - zero sum q~): an infinite scale makes them infinite by the sign of that difference, one of
+ * -infinity weighs nothing, and a query with one of NaN or +infinity makes every position that it sees NaN.  T == 0 leaves prev + 0.  T n_q_heads / n_kv_heads + 16 B up to 2^24 - 2^9.
  */
 size_t saw_attn_weights_workspace_bytes(const saw_cache_t* cache, int32_t n_q_heads, int64_t T, int32_t B, int64_t max_seq_len);
 int saw_paged_attn_weights(const saw_cache_t* cache, const void* q, int32_t dtype, int64_t T, int64_t q_stride, int32_t n_q_heads,

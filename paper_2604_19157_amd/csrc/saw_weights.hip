@@ -242,10 +242,13 @@ __device__ __forceinline__ void row_allsum4(float (&v)[4]) { asm(ROW_ALL4("v_add
 // chunk; otherwise the weights of the chunk's keys over all rows.  The wavefronts of a block share out the chunk's keys, or, SHARE_ROWS, the row
 // tiles, and then add up their weights.
 template <int D, bool STATS, bool SHARE_ROWS>
-__global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int64_t tiles, int chunk_keys) {
+__global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int64_t tiles, int chunk_keys, bool search) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = blockIdx.x % p.n_kv_heads, chunk = blockIdx.x / p.n_kv_heads, b = blockIdx.y;
+  const int h = blockIdx.x % p.n_kv_heads, chunk = blockIdx.x / p.n_kv_heads;
   const WeightSpace<D> ws(p.ws, tiles, p.n_kv_heads);
+  RowTile group;                // (STATS) of the batch's groups of row tiles, or number blockIdx.z of sequence blockIdx.y
+  if (STATS && search && !find_row_tile(p, (int64_t)blockIdx.z * gridDim.y + blockIdx.y, kGroupTiles * kWeightRows, lane, group)) return;
+  const int b = STATS && search ? group.b : (int)blockIdx.y;
   const int len = min(max(p.seq_lens[b], 0), p.bound);
   int begin, n;
   packed_range(p.cu_q, b, p.T_q, begin, n);
@@ -253,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void weight_pass_kernel(PromptParams p, int
   const int shift = __builtin_ctz(p.group), first_hidden = len - n + 1;
   const int64_t rows = (int64_t)n * p.group;
   const int all = (int)((rows + kWeightRows - 1) / kWeightRows);
-  const int g0 = STATS ? (int)blockIdx.z * kGroupTiles : 0, g1 = STATS ? min(all, g0 + kGroupTiles) : all;
+  const int g0 = !STATS ? 0 : search ? group.row0 / kWeightRows : (int)blockIdx.z * kGroupTiles, g1 = STATS ? min(all, g0 + kGroupTiles) : all;
   const int k0 = chunk * chunk_keys, k1 = min(len, k0 + chunk_keys);
   if (STATS && g0 >= g1) return;
   __shared__ float2 stats[4][STATS ? kGroupTiles * kWeightRows : 1];
@@ -630,13 +633,19 @@ size_t weights_bytes(int D, int Hq, int Hkv, int64_t T, int B, int64_t bound) {
 
 template <int D, bool SHARE_ROWS>
 static void launch_passes(const PromptParams& p, int64_t tiles, const WeightPlan& plan, hipStream_t st) {
-  const int groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles), wide = p.n_kv_heads * plan.chunks;
+  const int wide = p.n_kv_heads * plan.chunks;
   if (p.T_q) {
     weight_query_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(1024), 0, st>>>(p, tiles);
-    weight_pass_kernel<D, true, SHARE_ROWS><<<dim3(wide, p.B, groups), dim3(256), 0, st>>>(p, tiles, plan.chunk_keys);
+    // Which groups of row tiles a sequence has is known on the device alone.  As many blocks for each sequence as the whole batch has groups,
+    // while that is few blocks, an empty one 0.4 ns; otherwise the blocks search for their sequence, some 4 us (10 x 131 tokens of 32 heads over 135
+    // keys 52.6 us and 55, 24 x 60 over 75, 9216 blocks, 52.5 and 57.4; 64 x 200 over 3000 1965 and 1842, 1024 x 16 over 40 1720 and 649).
+    const int64_t each = (tiles + kGroupTiles - 1) / kGroupTiles, groups = row_tiles(p.T_q, p.group, kGroupTiles * kWeightRows, p.B);
+    const bool search = each * p.B * wide > 16384;
+    const int64_t high = search ? (groups < 32768 ? groups : 32768) : p.B, deep = search ? (groups + high - 1) / high : each;
+    weight_pass_kernel<D, true, SHARE_ROWS><<<dim3(wide, (unsigned)high, (unsigned)deep), dim3(256), 0, st>>>(p, tiles, plan.chunk_keys, search);
     weight_join_kernel<D><<<dim3((unsigned)tiles, p.n_kv_heads), dim3(256), 0, st>>>(p, tiles, plan.chunks);
   }
-  weight_pass_kernel<D, false, SHARE_ROWS><<<dim3(wide, p.B), dim3(256), 0, st>>>(p, tiles, plan.chunk_keys);
+  weight_pass_kernel<D, false, SHARE_ROWS><<<dim3(wide, p.B), dim3(256), 0, st>>>(p, tiles, plan.chunk_keys, false);
 }
 
 // One launch where a sequence has about one query: short contexts, whose four launches take longer than a block of one compute unit for each

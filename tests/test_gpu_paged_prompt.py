@@ -633,6 +633,19 @@ def test_weights_of_many_queries_over_few_keys(saw, n, lens, d, G):
         pc.check(got[b, :, :L], want[b, :, :L], tol[b, :, :L], b)
 
 
+def test_weights_of_many_sequences_take_time_with_their_number(saw):
+    """Four times the sequences: not sixteen times the blocks.  (Four times the work; eight leaves room for the clock.)"""
+    took = []
+    for B in (512, 2048):
+        c = Case(saw, [16] * B, [40] * B, G=8, seed=2)
+        ws = torch.empty(saw.attn_weights_workspace_bytes(c.cache, c.args[0], B, 48), dtype=torch.uint8, device="cuda")
+        scores = torch.zeros((B, 2, 48), device="cuda")
+        took.append(pc.milliseconds(lambda: saw.paged_attn_weights(c.cache, *c.args, scores=scores, max_seq_len=48, workspace=ws)))
+        total = scores[..., :40].double().sum(-1)
+        assert bool((total - 16 * 8).abs().max() < 1e-3)          # every row's weights sum to one
+    assert took[1] < 8 * took[0], took
+
+
 def test_weights_of_many_queries_over_one_long_sequence(saw):
     """A single head: wavefronts that share out the rows go over several steps of keys."""
     c = Case(saw, [90], [20000], Hkv=1, G=8, seed=9)
