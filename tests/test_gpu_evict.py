@@ -204,6 +204,34 @@ def test_captured_and_replayed(saw):
         c.check([new_lens.cpu().numpy(), kept.cpu().numpy(), out.cpu().numpy()])
 
 
+def test_long_rows_captured_and_replayed_with_lengths_in_place(saw):
+    """The launches of few long rows in a graph, lengths replaced by each replay and set back before the next."""
+    lens, budget = [40000, 17000, 300], 2000
+    c = Case(saw, lens, budget, 100)
+    ws = torch.empty(saw.evict_workspace_bytes(c.cache, 3, 40000), dtype=torch.uint8, device="cuda")
+    kept, out = torch.zeros((3, 2, budget), dtype=torch.int32, device="cuda"), torch.zeros((3, 2, budget), device="cuda")
+
+    def run():
+        saw.evict_pages(c.cache, *c.args, budget, recent=100, max_seq_len=40000, new_lens=c.args[2], kept=kept, scores_out=out, workspace=ws)
+
+    old = c.args[2].clone()
+    run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for i in range(3):
+        c.scores = np.random.default_rng(60 + i).random(c.scores.shape).astype(np.float32)
+        c.args[0].copy_(torch.from_numpy(c.scores))
+        c.args[2].copy_(old)
+        ws.fill_(0xff)
+        kept.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        c.check([c.args[2].cpu().numpy(), kept.cpu().numpy(), out.cpu().numpy()])
+
+
 @pytest.mark.parametrize("d,dtype", [(128, torch.bfloat16), (64, torch.float16)])
 def test_prompt_weights_eviction_and_decode_together(saw, d, dtype):
     """Prompts are attended to and stored, a chunk of new tokens follows, its weights decide what is kept, decode goes on over the kept

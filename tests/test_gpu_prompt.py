@@ -210,6 +210,21 @@ def test_no_queries_is_a_no_op(saw):
     assert saw.prompt_attn(q, k, k, torch.zeros(2, dtype=torch.int32, device="cuda"), torch.tensor([0, 5], dtype=torch.int32).cuda()).shape == (0, 4, 128)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+def test_no_keys_at_all(saw, causal):
+    q, k = pc.rand((7, 4, 128), 1, BF).cuda(), torch.empty((0, 2, 128), dtype=BF, device="cuda")
+    cu = torch.tensor([0, 3, 7], dtype=torch.int32, device="cuda")
+    assert torch.count_nonzero(saw.prompt_attn(q, k, k, cu, torch.zeros_like(cu), causal=causal, out=torch.full_like(q, 4.0))) == 0
+
+
+@pytest.mark.parametrize("bound", [-1, 10 ** 12])
+def test_bounds_below_zero_and_beyond_the_keys(saw, bound):
+    """They stand for the number of keys."""
+    q, k, v = pc.rand((3, 4, 128), 1, BF).cuda(), pc.rand((5000, 2, 128), 2, BF).cuda(), pc.rand((5000, 2, 128), 3, BF).cuda()
+    cu_q, cu_k = torch.tensor([0, 3], dtype=torch.int32, device="cuda"), torch.tensor([0, 5000], dtype=torch.int32, device="cuda")
+    assert torch.equal(saw.prompt_attn(q, k, v, cu_q, cu_k, max_k_len=bound), saw.prompt_attn(q, k, v, cu_q, cu_k))
+
+
 def test_many_sequences(saw):
     rng = np.random.default_rng(3)
     n = rng.integers(0, 9, 300).tolist()
